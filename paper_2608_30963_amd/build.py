@@ -45,8 +45,8 @@ def _check(r, what):
 
 def build(out: str = LIB, verbose: bool = False) -> str:
     """Compile the host library, the translator fit, the translator-variant
-    composition, the staged (unfused) translation and the fused kernel's
-    three precision variants as separate objects (in parallel), then link
+    composition, the staged (unfused) translation, decoding on the translated
+    cache and the fused kernel's three precision variants as separate objects (in parallel), then link
     libkvx.so."""
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
@@ -54,6 +54,8 @@ def build(out: str = LIB, verbose: bool = False) -> str:
              ("fit", os.path.join(CSRC, "fit.hip"), []),
              ("compose", os.path.join(CSRC, "compose.hip"), []),
              ("staged", os.path.join(CSRC, "staged.hip"), [])]
+    units += [(name, os.path.join(CSRC, name + ".hip"), [])
+              for name in ("attn", "attn_forward", "attn_mass", "attn_evict")]
     for i, name in enumerate(("bf16x2", "bf16", "f16")):
         units.append((f"fused_{name}", os.path.join(CSRC, "fused_launch.hip"),
                       [f"-DKVX_LAUNCH_PREC={i}"]))

@@ -1,0 +1,148 @@
+// attn.h -- what the kernels of decoding on a translated cache share
+// (kvx_attn.h): their arguments, cache addressing and visibility.
+#pragma once
+
+#include "common.h"
+#include "kvx_attn.h"
+
+struct kvx_attn {
+  int device = 0;
+  int n_cu = 0;
+  kvx_model model{};
+  int32_t n_heads = 0, group = 0;  // query heads, and per KV head
+  int32_t dtype = KVX_BF16;
+  double scale = 0.0, softcap = 0.0;
+  int32_t n_axes = 1;
+  void* tables = nullptr;          // device: the two tables below
+  const double* freq = nullptr;    // [head_dim/2] theta / (2 pi)
+  const uint8_t* axis = nullptr;   // [head_dim/2]
+};
+
+namespace kvx {
+
+// floor(n / d) for 0 <= n < 2^31 by a product: mul = floor(2^(31+l) / d) + 1,
+// l = ceil(log2 d); its excess over 2^(31+l)/d is at most 1, and n < 2^31
+// times that stays below 2^(31+l) / d, less than a quotient's step.
+struct FastDiv {
+  uint32_t mul, shift, d;
+};
+
+inline FastDiv fast_div(int32_t d) {
+  uint32_t l = 0;
+  while ((int64_t(1) << l) < d) ++l;
+  return FastDiv{static_cast<uint32_t>((uint64_t(1) << (31 + l)) / uint32_t(d) + 1), 31 + l,
+                 static_cast<uint32_t>(d)};
+}
+
+__device__ __forceinline__ int fdiv(const FastDiv& f, int n) {
+  return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(n)) * f.mul) >> f.shift);
+}
+
+// One layer's cache (or the first layer's, sl elements a layer): the row of
+// slot j of context b and head h starts at element block * sb + h * sh +
+// (j % block_size) * st, block the table's entry; without a table (contiguous)
+// the block is the context and block_size exceeds every slot.
+struct CacheArgs {
+  char* k;
+  char* v;
+  int64_t sl, sb, sh, st;
+  const int32_t* table;
+  int32_t max_blocks;
+  int32_t capacity;  // slots of a context
+  FastDiv bs;
+};
+
+__device__ __forceinline__ int32_t cache_block(const CacheArgs& c, int b, int j) {
+  return c.table ? c.table[static_cast<int64_t>(b) * c.max_blocks + fdiv(c.bs, j)] : b;
+}
+
+// Element offset of slot j within its block's rows of one head.
+__device__ __forceinline__ int64_t cache_offset(const CacheArgs& c, int32_t block, int j) {
+  const int slot = c.table ? j - fdiv(c.bs, j) * static_cast<int>(c.bs.d) : j;
+  return static_cast<int64_t>(block) * c.sb + static_cast<int64_t>(slot) * c.st;
+}
+
+// One layer's append, forward or mass.
+struct AttnArgs {
+  CacheArgs c;
+  const int32_t* q_start;  // NULL: one row per context
+  const int32_t* tokens;
+  const int32_t* prefix;   // NULL: none
+  const int32_t* pos;      // append: [axes][rows], NULL: slots
+  int32_t batch, rows, hq, hkv, group, d;
+  int32_t window;          // 0: none
+  float scale2;            // score scale * log2(e); with a cap scale / cap
+  float cap2;              // cap * log2(e), 0: none
+  const char* q;           // forward, mass
+  int64_t q_sr, q_sh;      // elements
+  char* out;
+  int64_t o_sr, o_sh;
+  float* lse;              // [rows][hq]
+  const float* mass_in;
+  float* mass;
+  int32_t mass_capacity;
+};
+
+// A context's rows and slots, clamped to what the caller's buffers hold.
+struct Context {
+  int q0, m, n;  // first row, new tokens, cached tokens
+  int prefix;    // slots that every new token sees
+};
+
+__device__ __forceinline__ Context context(const AttnArgs& a, int b) {
+  Context c;
+  c.q0 = a.q_start ? min(max(a.q_start[b], 0), a.rows) : b;
+  const int q1 = a.q_start ? min(max(a.q_start[b + 1], c.q0), a.rows) : b + 1;
+  c.m = q1 - c.q0;
+  c.n = min(max(a.tokens[b], 0), a.c.capacity);
+  c.prefix = a.prefix ? min(max(a.prefix[b], 0), c.n) : 0;
+  return c;
+}
+
+// Slots [lo, hi) that the new token of slot p sees; empty for p < 0.
+__device__ __forceinline__ int first_seen(const AttnArgs& a, int p) {
+  return a.window && p >= a.window ? p - a.window + 1 : 0;
+}
+__device__ __forceinline__ int end_seen(const Context& c, int p) {
+  return p < 0 ? 0 : max(p + 1, c.prefix);
+}
+
+// Score in units of log2: x is the dot product q.k.  tanh(y) = 1 - 2 / (1 +
+// exp(2y)); its absolute error is that of 1, 2^-24, times the cap.
+__device__ __forceinline__ float score2(const AttnArgs& a, float x) {
+  if (a.cap2 == 0.f) return x * a.scale2;
+  const float e = __builtin_amdgcn_exp2f(x * a.scale2 * 2.885390081777927f);
+  return a.cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + e));
+}
+
+// Launchers; each returns the launch's own status.
+hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, void* workspace,
+                          hipStream_t st);
+size_t forward_workspace(const kvx_attn* at);
+hipError_t launch_mass(const kvx_attn* at, const AttnArgs& a, int max_new, hipStream_t st);
+
+struct EvictArgs {
+  CacheArgs src, dst;
+  const int32_t* tokens;
+  int32_t layers, batch, heads, row_bytes;
+  int32_t keep, sink, recent;
+  bool in_place;
+  const float* mass;
+  float* mass_out;
+  int32_t mass_capacity;
+  int32_t* kept;
+  int32_t* tokens_out;
+};
+hipError_t launch_evict(const kvx_attn* at, const EvictArgs& a, hipStream_t st);
+
+// A launch with its own status: the runtime's last error may be another
+// call's.  Each argument is converted to the kernel's parameter type.
+template <typename... P, typename... A>
+hipError_t launch_on(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, const A&... a) {
+  return [&](P... p) {
+    void* args[] = {&p...};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, args, 0, st);
+  }(static_cast<P>(a)...);
+}
+
+}  // namespace kvx

@@ -4,10 +4,12 @@ The entry points carry the C names -- ``kvx_plan_create``,
 ``kvx_plan_create_factored``, ``kvx_translate``, ``kvx_plan_destroy``
 (include/kvx.h) and ``kvx_fit_create``,
 ``kvx_fit_accumulate``, ``kvx_fit_solve``, ``kvx_fit_reset``,
-``kvx_fit_destroy`` (include/kvx_fit.h) -- and take torch tensors for device
-buffers (torch provides device memory and streams; it computes nothing here).
-Every step of the translation and of the fit runs in the library's HIP
-kernels.
+``kvx_fit_destroy`` (include/kvx_fit.h), ``kvx_attn_create``,
+``kvx_attn_append``, ``kvx_attn_forward``, ``kvx_attn_mass``,
+``kvx_attn_evict``, ``kvx_attn_destroy`` (include/kvx_attn.h) -- and take torch
+tensors for device buffers (torch provides device memory and streams; it
+computes nothing here).  Every step of the translation, of the fit and of
+decoding on the translated cache runs in the library's HIP kernels.
 
 The library must have been built (``python -m paper_2608_30963_amd.build``);
 loading fails loudly otherwise -- there is no fallback path.
@@ -28,13 +30,15 @@ KVX_PREC_BF16X2, KVX_PREC_BF16, KVX_PREC_F16, KVX_PREC_BF16X2_OUTLIER = 0, 1, 2,
 KVX_FACTORS_LOWRANK, KVX_FACTORS_MIXTURE = 1, 2
 KVX_STAGE_POOL, KVX_STAGE_PROJECT, KVX_STAGE_STORE, KVX_STAGE_ALL = 1, 2, 4, 7
 
-# Exported C symbols, as declared in include/kvx.h and include/kvx_fit.h.
+# Exported C symbols, as declared in include/kvx.h, kvx_fit.h and kvx_attn.h.
 SYMBOLS = ("kvx_plan_create", "kvx_plan_create_factored", "kvx_translate", "kvx_plan_destroy",
            "kvx_status_string",
            "kvx_last_hip_error", "kvx_plan_query", "kvx_staged_workspace_bytes",
            "kvx_translate_staged", "kvx_fit_create", "kvx_fit_accumulate",
            "kvx_fit_solve", "kvx_fit_solve_noalloc", "kvx_fit_reset", "kvx_fit_rows",
-           "kvx_fit_query", "kvx_fit_destroy")
+           "kvx_fit_query", "kvx_fit_destroy", "kvx_attn_create", "kvx_attn_destroy",
+           "kvx_attn_append", "kvx_attn_workspace_bytes", "kvx_attn_forward", "kvx_attn_mass",
+           "kvx_attn_evict")
 
 
 class KvxError(RuntimeError):
@@ -100,6 +104,37 @@ class PlanInfo(C.Structure):
                 ("tile_order", C.c_int32)]
 
 
+class AttnDesc(C.Structure):
+    _fields_ = [("model", Model), ("n_heads", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_double), ("softcap", C.c_double), ("n_axes", C.c_int32),
+                ("pair_axis", C.c_void_p)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride", C.c_int64 * 4),
+                ("capacity", C.c_int32), ("block_table", C.c_void_p), ("block_size", C.c_int32),
+                ("max_blocks", C.c_int32), ("num_blocks", C.c_int32)]
+
+
+class AttnIO(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("layer", C.c_int32), ("rows", C.c_int32),
+                ("max_new", C.c_int32), ("q_start", C.c_void_p), ("tokens", C.c_void_p),
+                ("cache", Cache), ("new_q", C.c_void_p), ("new_k", C.c_void_p),
+                ("new_v", C.c_void_p), ("new_q_stride", C.c_int64 * 2),
+                ("new_k_stride", C.c_int64 * 2), ("new_v_stride", C.c_int64 * 2),
+                ("pos", C.c_void_p), ("q", C.c_void_p), ("q_stride", C.c_int64 * 2),
+                ("window", C.c_int32), ("prefix", C.c_void_p), ("out", C.c_void_p),
+                ("out_stride", C.c_int64 * 2), ("lse", C.c_void_p), ("mass_in", C.c_void_p),
+                ("mass", C.c_void_p), ("mass_capacity", C.c_int32)]
+
+
+class EvictIO(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("tokens", C.c_void_p), ("keep", C.c_int32),
+                ("sink", C.c_int32), ("recent", C.c_int32), ("src", Cache), ("dst", Cache),
+                ("mass", C.c_void_p), ("mass_out", C.c_void_p), ("mass_capacity", C.c_int32),
+                ("kept", C.c_void_p), ("tokens_out", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -153,6 +188,21 @@ def load(path: str = LIB_PATH):
     lib.kvx_fit_query.restype = C.c_int
     lib.kvx_fit_destroy.argtypes = [C.c_void_p]
     lib.kvx_fit_destroy.restype = None
+    lib.kvx_attn_create.argtypes = [C.POINTER(AttnDesc), C.POINTER(C.c_void_p)]
+    lib.kvx_attn_create.restype = C.c_int
+    lib.kvx_attn_destroy.argtypes = [C.c_void_p]
+    lib.kvx_attn_destroy.restype = None
+    lib.kvx_attn_append.argtypes = [C.c_void_p, C.POINTER(AttnIO), C.c_void_p]
+    lib.kvx_attn_append.restype = C.c_int
+    lib.kvx_attn_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+    lib.kvx_attn_workspace_bytes.restype = C.c_int
+    lib.kvx_attn_forward.argtypes = [C.c_void_p, C.POINTER(AttnIO), C.c_void_p, C.c_size_t,
+                                     C.c_void_p]
+    lib.kvx_attn_forward.restype = C.c_int
+    lib.kvx_attn_mass.argtypes = [C.c_void_p, C.POINTER(AttnIO), C.c_void_p]
+    lib.kvx_attn_mass.restype = C.c_int
+    lib.kvx_attn_evict.argtypes = [C.c_void_p, C.POINTER(EvictIO), C.c_void_p]
+    lib.kvx_attn_evict.restype = C.c_int
     _lib = lib
     return lib
 
@@ -551,6 +601,174 @@ class Fitter:
     def close(self):
         if self.handle:
             kvx_fit_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------------------
+# Decoding on a translated cache (include/kvx_attn.h)
+# ---------------------------------------------------------------------------
+
+def kvx_attn_create(model, n_heads: int, dtype: int, softcap: float = 0.0, scale: float = 0.0,
+                    inv_freq=None, pair_axis: Optional[Sequence[int]] = None,
+                    n_axes: Optional[int] = None) -> int:
+    """Create the attention side of a target model; returns the handle.
+    ``pair_axis``: position axis of each of the head_dim/2 rotary pairs (all
+    axis 0 without it); ``n_axes`` defaults to the axes it names."""
+    keep = []
+    axes = None
+    if pair_axis is not None:
+        axes = _host_array([int(x) for x in pair_axis], C.c_uint8)
+        if len(pair_axis) != int(model.head_dim) // 2:
+            raise ValueError(f"pair_axis has {len(pair_axis)} entries, "
+                             f"expected {int(model.head_dim) // 2}")
+        if n_axes is None:
+            n_axes = max(int(x) for x in pair_axis) + 1
+    desc = AttnDesc(_model(model, inv_freq, keep), int(n_heads), int(dtype), float(scale),
+                    float(softcap), 1 if n_axes is None else int(n_axes),
+                    C.cast(axes, C.c_void_p).value if axes is not None else None)
+    h = C.c_void_p()
+    st = load().kvx_attn_create(C.byref(desc), C.byref(h))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_create")
+    return h.value
+
+
+def make_cache(k, v, block_table=None, stride=(0, 0, 0, 0), block_size: Optional[int] = None,
+               num_blocks: Optional[int] = None, capacity: Optional[int] = None) -> Cache:
+    """The kvx_cache struct of device tensors ``k``/``v``: contiguous
+    [L][B][H][capacity][D], or with ``block_table`` ([B][max_blocks] int32)
+    paged [L][num_blocks][H][block_size][D].  Other layouts: give ``stride``
+    and the sizes that the shape does not show."""
+    if block_table is None:
+        c = Cache(_ptr(k), _ptr(v), (C.c_int64 * 4)(*[int(x) for x in stride]),
+                  int(k.shape[3] if capacity is None else capacity), None, 0, 0, 0)
+    else:
+        c = Cache(_ptr(k), _ptr(v), (C.c_int64 * 4)(*[int(x) for x in stride]), 0,
+                  _ptr(block_table), int(k.shape[3] if block_size is None else block_size),
+                  int(block_table.shape[1]),
+                  int(k.shape[1] if num_blocks is None else num_blocks))
+    c.tensors = (k, v, block_table)
+    return c
+
+
+def _row_stride(t):
+    if t is None:
+        return (C.c_int64 * 2)(0, 0)
+    if t.stride(-1) != 1:
+        raise ValueError("head_dim must be unit-stride")
+    return (C.c_int64 * 2)(t.stride(0), t.stride(1))
+
+
+def make_attn_io(cache: Cache, tokens, q=None, *, layer: int = 0, q_start=None, max_new: int = 1,
+                 new_q=None, new_k=None, new_v=None, pos=None, window: int = 0, prefix=None,
+                 out=None, lse=None, mass_in=None, mass=None) -> AttnIO:
+    """Build the kvx_attn_io struct of one layer's append, forward and mass
+    calls: ``q``, ``new_q``, ``new_k``, ``new_v``, ``out`` are [rows][heads][D]
+    tensors (any row and head strides); ``mass`` [B][Hkv][mass_capacity].  The
+    struct keeps its tensors alive."""
+    first = next(t for t in (q, new_q, new_k) if t is not None)
+    io = AttnIO(int(tokens.shape[0]), int(layer), int(first.shape[0]), int(max_new),
+                _ptr(q_start), _ptr(tokens), cache, _ptr(new_q), _ptr(new_k), _ptr(new_v),
+                _row_stride(new_q), _row_stride(new_k), _row_stride(new_v), _ptr(pos), _ptr(q),
+                _row_stride(q), int(window), _ptr(prefix), _ptr(out), _row_stride(out), _ptr(lse),
+                _ptr(mass_in), _ptr(mass), 0 if mass is None else int(mass.shape[-1]))
+    io.tensors = (cache, tokens, q, q_start, new_q, new_k, new_v, pos, prefix, out, lse, mass_in,
+               mass)
+    return io
+
+
+def make_evict_io(cache: Cache, tokens, mass, kept, keep: int, *, sink: int = 0, recent: int = 0,
+                  mass_out=None, tokens_out=None, dst: Optional[Cache] = None) -> EvictIO:
+    """Build the kvx_evict_io struct: ``mass`` [L][B][Hkv][mass_capacity],
+    ``kept`` int32 [L][B][Hkv][keep]; ``dst`` None compacts in place."""
+    io = EvictIO(int(tokens.shape[0]), _ptr(tokens), int(keep), int(sink), int(recent), cache,
+                 Cache() if dst is None else dst, _ptr(mass), _ptr(mass_out),
+                 int(mass.shape[-1]), _ptr(kept), _ptr(tokens_out))
+    io.tensors = (cache, tokens, mass, kept, mass_out, tokens_out, dst)
+    return io
+
+
+def kvx_attn_append(attn: int, io: AttnIO, stream=None) -> int:
+    st = load().kvx_attn_append(attn, C.byref(io), _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_append")
+    return st
+
+
+def kvx_attn_workspace_bytes(attn: int) -> int:
+    n = C.c_size_t(0)
+    st = load().kvx_attn_workspace_bytes(C.c_void_p(attn), C.byref(n))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_workspace_bytes")
+    return int(n.value)
+
+
+def kvx_attn_forward(attn: int, io: AttnIO, workspace, stream=None) -> int:
+    """``workspace``: a device tensor of at least kvx_attn_workspace_bytes."""
+    st = load().kvx_attn_forward(attn, C.byref(io), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(),
+                                 _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_forward")
+    return st
+
+
+def kvx_attn_mass(attn: int, io: AttnIO, stream=None) -> int:
+    st = load().kvx_attn_mass(attn, C.byref(io), _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_mass")
+    return st
+
+
+def kvx_attn_evict(attn: int, io: EvictIO, stream=None) -> int:
+    st = load().kvx_attn_evict(attn, C.byref(io), _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_evict")
+    return st
+
+
+def kvx_attn_destroy(attn: Optional[int]) -> None:
+    load().kvx_attn_destroy(C.c_void_p(attn) if attn else None)
+
+
+class Attention:
+    """RAII wrapper around the attention side of a target model.  The calls
+    take structs of make_attn_io / make_evict_io, which a decoding loop builds
+    once per layer."""
+
+    def __init__(self, model, n_heads, dtype, softcap=0.0, scale=0.0, inv_freq=None,
+                 pair_axis=None, n_axes=None):
+        self.handle = None
+        self.handle = kvx_attn_create(model, n_heads, dtype, softcap, scale, inv_freq, pair_axis,
+                                      n_axes)
+
+    def workspace(self, io=None):
+        """A workspace for forward calls (any of this handle's, one at a time)."""
+        import torch
+        return torch.empty(kvx_attn_workspace_bytes(self.handle), dtype=torch.uint8,
+                           device="cuda")
+
+    def append(self, io, stream=None):
+        kvx_attn_append(self.handle, io, stream)
+
+    def forward(self, io, workspace, stream=None):
+        kvx_attn_forward(self.handle, io, workspace, stream)
+
+    def mass(self, io, stream=None):
+        kvx_attn_mass(self.handle, io, stream)
+
+    def evict(self, io, stream=None):
+        kvx_attn_evict(self.handle, io, stream)
+
+    def close(self):
+        if self.handle:
+            kvx_attn_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

@@ -1,0 +1,640 @@
+"""Decoding on a translated cache on the GPU, against the fp64 reference.
+
+Tolerances.  A score is an fp32 sum of D products and a few more roundings:
+its error is at most delta = (D + 8) 2^-24 times the sum of its terms'
+magnitudes, and with a tanh cap another 2^-22 cap.  A relative error of the
+weights moves an output by that part of sum_j p_j |v_j|; sums over n slots add
+n 2^-24.  bf16 (8 significant bits) rounds by up to 2^-8 of a number: weights
+once before their product with bf16 values, the output once.
+"""
+import numpy as np
+import pytest
+
+from oracle import attn as R
+from paper_2608_30963_amd import kvx
+from tests import gpu_util as U
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+
+
+def _dt(dtype):
+    T = U.torch()
+    return T.bfloat16 if dtype == "bf16" else T.float32
+
+
+def _f64(t):
+    return t.double().cpu().numpy()
+
+
+class Cache:
+    """A cache of `layers` layers whose contexts hold lens tokens: rows in
+    order (k, v [layer][context][n, H, D]) and their places on the device.
+    Slots past a context's tokens, and the spare block that unused table
+    entries name, hold NaN."""
+
+    def __init__(self, lens, hkv, d, dtype, page, layers=2, flash=False, seed=0, extra=0):
+        T = U.torch()
+        g = T.Generator().manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        self.lens, self.page, self.flash, self.layers = lens, page, flash, layers
+        batch, cap = len(lens), max(max(lens) + extra, 1)
+        self.rows = [[[T.randn(n, hkv, d, generator=g).to(_dt(dtype)) for n in lens]
+                      for _ in range(layers)] for _ in range(2)]
+        if page:
+            per = -(-cap // page)
+            nb = batch * per + 1
+            perm = rng.permutation(nb)
+            self.spare = int(perm[-1])
+            table = np.full((batch, per), self.spare, np.int32)
+            k = 0
+            for b, n in enumerate(lens):
+                used = -(-(n + extra) // page)
+                table[b, :used] = perm[k:k + used]
+                k += used
+            self.host_table = table
+            self.table = T.from_numpy(table).cuda()
+            shape = (layers, nb, page, hkv, d) if flash else (layers, nb, hkv, page, d)
+        else:
+            self.host_table = self.table = None
+            shape = (layers, batch, cap, hkv, d) if flash else (layers, batch, hkv, cap, d)
+        self.dev = []
+        for kv in range(2):
+            t = T.full(shape, float("nan"), dtype=_dt(dtype))
+            view = t.transpose(2, 3) if flash else t  # [L][block][H][slot][D]
+            for l in range(layers):
+                for b, n in enumerate(lens):
+                    blk, slot = self.place(b, np.arange(n))
+                    view[l, blk, :, slot] = self.rows[kv][l][b]
+            self.dev.append(t.cuda())
+        s = self.dev[0].stride()
+        stride = (s[0], s[1], s[3], s[2]) if flash else (0, 0, 0, 0)
+        size = dict(block_size=page, num_blocks=shape[1]) if page else dict(capacity=cap)
+        self.struct = kvx.make_cache(self.dev[0], self.dev[1], self.table, stride, **size)
+
+    def place(self, b, j):
+        j = np.asarray(j)
+        if self.page:
+            return self.host_table[b][j // self.page].astype(np.int64), j % self.page
+        return np.full_like(j, b), j
+
+    def read(self, kv, l, b, n):
+        """Rows [n, H, D] of a context from the device."""
+        t = self.dev[kv].transpose(2, 3) if self.flash else self.dev[kv]
+        blk, slot = self.place(b, np.arange(n))
+        return t.cpu()[l][blk, :, slot]
+
+    def f64(self, kv, l, b):
+        return _f64(self.rows[kv][l][b])
+
+
+def _rows(total, heads, d, dtype, seed, scale=1.0, pad=0):
+    """[total, heads, d] drawn; with pad, a slice of wider rows (strided)."""
+    T = U.torch()
+    g = T.Generator().manual_seed(seed)
+    x = (T.randn(total, heads + pad, d, generator=g) * scale).to(_dt(dtype)).cuda()
+    return x[:, pad:]
+
+
+def _int(values):
+    T = U.torch()
+    return T.tensor(list(values), dtype=T.int32, device="cuda")
+
+
+def _starts(new):
+    return np.concatenate([[0], np.cumsum(new)]).astype(int)
+
+
+FORWARD = [
+    # name, dtype, hq, hkv, d, page, (new, cached) of each context, options
+    ("one", "bf16", 12, 2, 128, 16, [(1, 300)], {}),
+    ("one_slot", "bf16", 4, 4, 64, 16, [(1, 1)], {}),
+    ("decode_ragged", "bf16", 28, 4, 128, 16, [(1, 700), (1, 1), (1, 64), (1, 65), (1, 1023)], {}),
+    ("decode_long", "bf16", 7, 1, 128, 64, [(1, 9001)], {}),
+    ("decode_group_33", "bf16", 33, 1, 64, 16, [(1, 500), (1, 40)], {}),
+    ("decode_group_64", "bf16", 64, 1, 128, 32, [(1, 333)], {}),
+    ("decode_window", "bf16", 8, 4, 256, 32, [(1, 900), (1, 30), (1, 129)], dict(window=128)),
+    ("decode_cap", "bf16", 8, 4, 256, 16, [(1, 400), (1, 33)], dict(cap=50.0)),
+    ("decode_f32", "f32", 12, 2, 128, 16, [(1, 600), (1, 31)], {}),
+    ("decode_f32_256", "f32", 8, 4, 256, 0, [(1, 300), (1, 7)], dict(cap=30.0)),
+    ("few", "bf16", 12, 2, 128, 16, [(3, 200), (5, 5), (2, 77)], {}),
+    ("chunk", "bf16", 12, 2, 128, 16, [(150, 400)], {}),
+    ("chunk_from_zero", "bf16", 4, 2, 64, 16, [(260, 260)], {}),
+    ("chunk_ragged", "bf16", 14, 2, 128, 48, [(100, 333), (1, 50), (0, 20), (37, 37)], {}),
+    ("chunk_group_1", "bf16", 2, 2, 80, 7, [(131, 200)], {}),
+    ("chunk_window", "bf16", 8, 4, 256, 32, [(140, 500), (64, 64)], dict(window=50, cap=50.0)),
+    ("chunk_window_1", "bf16", 2, 1, 64, 16, [(70, 300)], dict(window=1)),
+    ("chunk_prefix", "bf16", 6, 2, 96, 16, [(90, 120), (60, 61)], dict(prefix=[70, 61])),
+    ("chunk_prefix_window", "bf16", 6, 2, 128, 16, [(90, 220)], dict(prefix=[200], window=64)),
+    ("chunk_f32", "f32", 6, 2, 128, 16, [(75, 210), (20, 33)], dict(prefix=[30, 33])),
+    ("chunk_f32_64", "f32", 7, 1, 64, 0, [(40, 170)], dict(window=33)),
+    ("chunk_f32_256", "f32", 4, 2, 256, 16, [(70, 140)], dict(cap=50.0)),
+    ("d16", "bf16", 3, 1, 16, 5, [(33, 100), (1, 9)], {}),
+    ("d48_f32", "f32", 3, 1, 48, 1, [(9, 70)], {}),
+    ("d192", "bf16", 4, 2, 192, 16, [(40, 130)], {}),
+    ("before_first_slot", "bf16", 4, 2, 64, 16, [(20, 12), (5, 0), (6, 6)], {}),
+    ("nothing_cached", "f32", 2, 1, 64, 16, [(1, 0), (1, 3)], {}),
+    ("strided", "bf16", 4, 2, 64, 16, [(30, 90), (1, 40)], dict(flash=True, pad=3)),
+    ("strided_decode", "bf16", 4, 2, 128, 0, [(1, 90), (1, 40)], dict(flash=True, pad=5)),
+    ("large_scores", "bf16", 4, 2, 128, 16, [(40, 200), (1, 150)], dict(scale=30.0)),
+    ("many_contexts", "bf16", 4, 1, 64, 16, [(1, 1 + 13 * i % 97) for i in range(300)], {}),
+]
+
+
+def _problem(dtype, hq, hkv, d, page, spec, opt, seed=0):
+    """Cache, queries, lengths and io keywords of one forward or mass call."""
+    new, lens = [m for m, _ in spec], [n for _, n in spec]
+    cache = Cache(lens, hkv, d, dtype, page, flash=opt.get("flash", False), seed=seed)
+    starts = _starts(new)
+    q = _rows(starts[-1], hq, d, dtype, seed + 1, opt.get("scale", 1.0), opt.get("pad", 0))
+    kw = dict(layer=1, max_new=max(new), window=opt.get("window", 0),
+              q_start=None if all(m == 1 for m in new) else _int(starts),
+              prefix=_int(opt["prefix"]) if "prefix" in opt else None)
+    return cache, q, starts, _int(lens), kw
+
+
+def _delta(size, d, cap):
+    return (d + 8) * EPS * size + (2.0 ** -22 * cap if cap else 0.0)
+
+
+@pytest.mark.parametrize("case", FORWARD, ids=[c[0] for c in FORWARD])
+def test_forward(case):
+    name, dtype, hq, hkv, d, page, spec, opt = case
+    T = U.torch()
+    print(f"[attn] {name}", flush=True)
+    cache, q, starts, tokens, kw = _problem(dtype, hq, hkv, d, page, spec, opt)
+    cap = opt.get("cap", 0.0)
+    att = kvx.Attention(kvx.ModelShape(2, hkv, d, 1e4), hq,
+                        kvx.KVX_BF16 if dtype == "bf16" else kvx.KVX_F32, softcap=cap)
+    pad = opt.get("pad", 0)
+    wide = T.full((starts[-1], hq + pad, d), 7.0, dtype=_dt(dtype), device="cuda")
+    out = wide[:, :hq]
+    lse = T.full((starts[-1], hq), float("nan"), device="cuda")
+    io = kvx.make_attn_io(cache.struct, tokens, q, out=out, lse=lse, **kw)
+    ws = att.workspace(io)
+    ws.fill_(0xFF)  # NaN wherever read before written
+    att.forward(io, ws)
+    T.cuda.synchronize()
+    if pad:
+        assert (wide[:, hq:] == 7.0).all(), "wrote outside its rows"
+    first = out.clone()
+    first_lse = lse.clone()
+    ws.fill_(0)
+    att.forward(io, ws)
+    T.cuda.synchronize()
+    assert T.equal(first.view(-1, d), out.reshape(-1, d)) and T.equal(first_lse, lse), "bits differ"
+    qh, oh, lh = _f64(q), _f64(out), _f64(lse)
+    for b, (m, n) in enumerate(spec):
+        sl = slice(starts[b], starts[b + 1])
+        prefix = min(opt["prefix"][b], n) if "prefix" in opt else 0
+        ro, rl, mag, size = R.attend(qh[sl], cache.f64(0, 1, b), cache.f64(1, 1, b), d ** -0.5,
+                                     cap, opt.get("window", 0), prefix)
+        delta = _delta(size, d, cap)
+        rel = 2 * delta + (n + 64) * EPS
+        if dtype == "bf16":
+            rel = rel + 2.0 ** -8
+        tol = mag * rel[..., None] + (2.0 ** -8 * np.abs(ro) if dtype == "bf16" else 0.0)
+        assert np.isfinite(oh[sl]).all(), f"{name} context {b}: non-finite output"
+        worst = np.abs(oh[sl] - ro) - tol
+        assert worst.max(initial=-1) <= 0, f"{name} context {b}: {worst.max()} over"
+        seen = np.isfinite(rl)
+        assert (lh[sl][~seen] == -np.inf).all(), f"{name} context {b}: lse of an empty row"
+        ltol = delta + (n + 64) * EPS + 2.0 ** -22 * (1 + np.abs(np.where(seen, rl, 0.0)))
+        err = np.abs(np.where(seen, lh[sl], 0.0) - np.where(seen, rl, 0.0))
+        assert (err <= ltol).all(), f"{name} context {b}: lse off by {err.max()}"
+    att.close()
+
+
+@pytest.mark.parametrize("case", FORWARD, ids=[c[0] for c in FORWARD])
+def test_mass(case):
+    name, dtype, hq, hkv, d, page, spec, opt = case
+    T = U.torch()
+    print(f"[mass] {name}", flush=True)
+    cache, q, starts, tokens, kw = _problem(dtype, hq, hkv, d, page, spec, opt, seed=5)
+    cap = opt.get("cap", 0.0)
+    att = kvx.Attention(kvx.ModelShape(2, hkv, d, 1e4), hq,
+                        kvx.KVX_BF16 if dtype == "bf16" else kvx.KVX_F32, softcap=cap)
+    room = max(n for _, n in spec) + 5
+    qh, window = _f64(q), opt.get("window", 0)
+    lse = np.full((starts[-1], hq), -np.inf)
+    for b, (m, n) in enumerate(spec):
+        prefix = min(opt["prefix"][b], n) if "prefix" in opt else 0
+        sl = slice(starts[b], starts[b + 1])
+        lse[sl] = R.attend(qh[sl], cache.f64(0, 1, b), cache.f64(1, 1, b), d ** -0.5, cap, window,
+                           prefix)[1]
+    lse_d = T.from_numpy(lse.astype(np.float32)).cuda()
+    lse = _f64(lse_d)
+    g = T.Generator().manual_seed(3)
+    before = T.rand(len(spec), hkv, room, generator=g).cuda()
+    for given in (True, False):
+        got = T.full_like(before, float("nan"))
+        io = kvx.make_attn_io(cache.struct, tokens, q, lse=lse_d, mass_in=before if given else None,
+                              mass=got, **kw)
+        att.mass(io)
+        T.cuda.synchronize()
+        again = before.clone()
+        io2 = kvx.make_attn_io(cache.struct, tokens, q, lse=lse_d,
+                               mass_in=again if given else None, mass=again, **kw)
+        att.mass(io2)  # in place
+        T.cuda.synchronize()
+        assert T.equal(got, again), "bits differ"
+        gh, base = _f64(got), _f64(before) if given else np.zeros(before.shape)
+        for b, (m, n) in enumerate(spec):
+            prefix = min(opt["prefix"][b], n) if "prefix" in opt else 0
+            sl = slice(starts[b], starts[b + 1])
+            ref, size = R.mass(qh[sl], cache.f64(0, 1, b), lse[sl], d ** -0.5, cap, window, prefix)
+            # the log-sum-exp enters as log2 units: one more rounding of it
+            lmax = np.abs(lse[sl][np.isfinite(lse[sl])]).max(initial=0.0)
+            rel = 2 * _delta(size, d, cap) + (m * hq + 64) * EPS + 4 * EPS * (lmax + 1)
+            # 2^-126: below it fp32 holds no relative precision
+            tol = ref * rel + 2 * EPS * (base[b, :, :n] + ref) + 2.0 ** -126
+            err = np.abs(gh[b, :, :n] - base[b, :, :n] - ref)
+            assert (err <= tol).all(), f"{name} context {b}: {(err - tol).max()} over"
+            assert (gh[b, :, n:] == base[b, :, n:]).all()
+    att.close()
+
+
+def test_masked_values_may_be_anything():
+    """NaN and infinities in slots that a row does not see change no bit of it;
+    rows that see them get what the softmax of 64-bit numbers gives."""
+    T = U.torch()
+    for dtype, m, n, window, prefix in (("bf16", 40, 100, 0, 0), ("f32", 40, 100, 0, 0),
+                                        ("bf16", 40, 100, 30, 0), ("bf16", 1, 100, 40, 0),
+                                        ("bf16", 130, 300, 0, 190)):
+        print(f"[attn] masked {dtype} {m} of {n}, window {window}", flush=True)
+        cache = Cache([n], 2, 64, dtype, 16)
+        q = _rows(m, 4, 64, dtype, 3)
+        att = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4,
+                            kvx.KVX_BF16 if dtype == "bf16" else kvx.KVX_F32)
+        kw = dict(layer=1, max_new=m, q_start=_int([0, m]), window=window,
+                  prefix=_int([prefix]) if prefix else None)
+        ws = att.workspace()
+        outs = []
+        bad = {n - 1: float("nan"), n - 2: float("inf"), n - 20: -float("inf")} if m > 1 else {}
+        if window:
+            bad[n - m - window] = float("nan")  # no row sees it
+        if m == 1:
+            bad[n - window - 1] = float("inf")
+        for spoiled in (False, True):
+            if spoiled:
+                for j, x in bad.items():
+                    blk, slot = cache.place(0, [j])
+                    cache.dev[1][1, int(blk[0]), :, int(slot[0])] = x
+                    if x != x or j < n - m:
+                        cache.dev[0][1, int(blk[0]), :, int(slot[0])] = x
+            out = T.zeros_like(q)
+            io = kvx.make_attn_io(cache.struct, _int([n]), q, out=out, **kw)
+            att.forward(io, ws)
+            T.cuda.synchronize()
+            outs.append(_f64(out))
+        for i in range(m):
+            see = R.visible(n - m + i, n, window, prefix)
+            seen = [x for j, x in bad.items() if see[j]]
+            if not seen:
+                assert (outs[0][i] == outs[1][i]).all(), (dtype, i)
+            elif any(x != x for x in seen) or len({x > 0 for x in seen}) == 2:
+                assert np.isnan(outs[1][i]).all(), (dtype, i)
+            else:
+                assert (outs[1][i] == seen[0]).all(), (dtype, i)
+        att.close()
+
+
+APPEND = [
+    # name, dtype, hq, hkv, d, page, (new, cached), axes, options
+    ("one", "bf16", 12, 2, 128, 16, [(1, 300)], 1, {}),
+    ("decode", "bf16", 28, 4, 128, 16, [(1, 17 * i + 1) for i in range(9)], 1, {}),
+    ("chunk_axes", "bf16", 4, 2, 128, 16, [(33, 100), (0, 8), (70, 70)], 3, {}),
+    ("f32", "f32", 3, 1, 80, 7, [(21, 60), (2, 2)], 2, {}),
+    ("f32_256", "f32", 8, 4, 256, 0, [(5, 5), (1, 9)], 1, {}),
+    ("by_slot", "bf16", 4, 4, 64, 16, [(10, 45), (3, 3)], 1, dict(pos=None)),
+    ("far", "bf16", 2, 1, 128, 16, [(6, 50)], 1, dict(pos=2 ** 30)),
+    ("before_first_slot", "bf16", 4, 2, 64, 16, [(9, 4), (3, 0)], 1, {}),
+    ("strided", "bf16", 4, 2, 64, 16, [(8, 40), (4, 4)], 1, dict(flash=True, pad=3)),
+    ("d16", "bf16", 2, 1, 16, 3, [(5, 9)], 4, {}),
+]
+
+
+@pytest.mark.parametrize("case", APPEND, ids=[c[0] for c in APPEND])
+def test_append(case):
+    name, dtype, hq, hkv, d, page, spec, axes, opt = case
+    T = U.torch()
+    print(f"[append] {name}", flush=True)
+    new, lens = [m for m, _ in spec], [n for _, n in spec]
+    starts = _starts(new)
+    rows = int(starts[-1])
+    cache = Cache(lens, hkv, d, dtype, page, flash=opt.get("flash", False))
+    before = [t.clone() for t in cache.dev]
+    pad = opt.get("pad", 0)
+    x = [_rows(rows, h, d, dtype, 10 + i, pad=pad) for i, h in enumerate((hq, hkv, hkv))]
+    rng = np.random.default_rng(1)
+    axis = [e % axes for e in range(d // 2)]
+    slots = np.concatenate([np.arange(n - m, n) for m, n in spec])
+    pos = None
+    if opt.get("pos", 0) is not None:
+        pos = rng.integers(0, 5000, (axes, rows)).astype(np.int32) + np.int32(opt.get("pos", 0))
+    att = kvx.Attention(kvx.ModelShape(2, hkv, d, 1e4), hq,
+                        kvx.KVX_BF16 if dtype == "bf16" else kvx.KVX_F32, pair_axis=axis)
+    q = T.zeros((rows, hq, d), dtype=_dt(dtype), device="cuda")
+    io = kvx.make_attn_io(cache.struct, _int(lens), q, layer=1, q_start=_int(starts),
+                          max_new=max(new), new_q=x[0], new_k=x[1], new_v=x[2],
+                          pos=None if pos is None else T.from_numpy(pos).cuda())
+    att.append(io)
+    T.cuda.synchronize()
+    at = np.broadcast_to(slots, (axes, rows)) if pos is None else pos
+    freq = 1e4 ** (-2.0 * np.arange(d // 2) / d)
+    rq, rk = (R.rotate(_f64(t), at, freq, axis) for t in x[:2])
+
+    def close(got, ref, src, what):
+        # two products and their sum, with the sine's and cosine's own 1.2e-7
+        pair = np.abs(src[..., :d // 2]) + np.abs(src[..., d // 2:])
+        tol = np.concatenate([pair, pair], -1) * (2 * 1.2e-7 + 4 * EPS)
+        if dtype == "bf16":
+            tol = tol + 2.0 ** -8 * np.abs(ref)
+        assert (np.abs(got - ref) <= tol).all(), f"{name} {what}"
+
+    close(_f64(q), rq, _f64(x[0]), "q")
+    written = np.zeros(cache.dev[0].shape[1:3], bool)
+    for b, (m, n) in enumerate(spec):
+        for i in range(m):
+            j = n - m + i
+            if j < 0:
+                continue
+            blk, slot = (int(t[0]) for t in cache.place(b, [j]))
+            r = starts[b] + i
+            if cache.flash:
+                written[blk, slot] = True
+                k, v = cache.dev[0][1, blk, slot], cache.dev[1][1, blk, slot]
+            else:
+                k, v = cache.dev[0][1, blk, :, slot], cache.dev[1][1, blk, :, slot]
+            close(_f64(k), rk[r], _f64(x[1][r]), f"k of row {r}")
+            assert T.equal(v, x[2][r]), f"{name} v of row {r}"
+            (cache.dev[0][1, blk, slot] if cache.flash else cache.dev[0][1, blk, :, slot])[:] = 0
+            (cache.dev[1][1, blk, slot] if cache.flash else cache.dev[1][1, blk, :, slot])[:] = 0
+            for t in before:
+                (t[1, blk, slot] if cache.flash else t[1, blk, :, slot])[:] = 0
+    for t, o in zip(cache.dev, before):
+        assert T.equal(t.view(T.int16 if dtype == "bf16" else T.int32),
+                       o.view(T.int16 if dtype == "bf16" else T.int32)), "wrote elsewhere"
+    att.close()
+
+
+def test_append_parts_and_in_place():
+    """Only queries, only keys and values, and queries rotated where they are:
+    the same bits as the whole call's."""
+    T = U.torch()
+    spec = [(12, 40), (3, 20)]
+    starts, lens = _starts([m for m, _ in spec]), [n for _, n in spec]
+    x = [_rows(15, h, 64, "bf16", 30 + h) for h in (4, 2, 2)]
+    att = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_BF16)
+
+    def run(q, **new):
+        cache = Cache(lens, 2, 64, "bf16", 16)
+        io = kvx.make_attn_io(cache.struct, _int(lens), q, q_start=_int(starts), max_new=12, **new)
+        att.append(io)
+        T.cuda.synchronize()
+        return [t.view(T.int16) for t in cache.dev]
+
+    q = T.zeros_like(x[0])
+    k, v = run(q, new_q=x[0], new_k=x[1], new_v=x[2])
+    q2 = x[0].clone()
+    k2, v2 = run(q2, new_q=q2)
+    assert T.equal(q, q2) and not T.equal(k, k2)
+    k3, v3 = run(None, new_k=x[1], new_v=x[2])
+    assert T.equal(k, k3) and T.equal(v, v3)
+    att.close()
+
+
+EVICT = [
+    # name, dtype, layers, hkv, d, page, lens, keep, sink, recent
+    ("half", "bf16", 3, 2, 128, 16, [200, 61], 100, 4, 16),
+    ("nothing_to_do", "bf16", 2, 2, 64, 16, [50, 10, 0], 64, 4, 16),
+    ("one", "bf16", 2, 1, 64, 16, [90], 1, 0, 0),
+    ("one_recent", "f32", 2, 1, 64, 7, [90, 1], 1, 0, 1),
+    ("all_protected", "bf16", 2, 2, 80, 16, [300], 40, 10, 30),
+    ("long", "bf16", 2, 2, 256, 32, [3000, 2999, 77], 1500, 0, 0),
+    ("longer", "f32", 1, 1, 64, 0, [40001], 20000, 4, 100),
+    ("contiguous", "f32", 2, 3, 128, 0, [500, 499], 129, 1, 2),
+]
+
+
+@pytest.mark.parametrize("values", ["plain", "ties", "special"])
+@pytest.mark.parametrize("in_place", [False, True], ids=["out", "in_place"])
+@pytest.mark.parametrize("case", EVICT, ids=[c[0] for c in EVICT])
+def test_evict(case, in_place, values):
+    name, dtype, layers, hkv, d, page, lens, keep, sink, recent = case
+    T = U.torch()
+    print(f"[evict] {name} {values} in_place={in_place}", flush=True)
+    cache = Cache(lens, hkv, d, dtype, page, layers=layers)
+    rng = np.random.default_rng(4)
+    room = max(max(lens), keep) + 3
+    w = rng.exponential(size=(layers, len(lens), hkv, room)).astype(np.float32)
+    if values == "ties":
+        w = np.floor(w * 2).astype(np.float32) * rng.choice([1.0, -1.0], w.shape).astype(np.float32)
+    elif values == "special":
+        w = rng.choice(np.array([np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-42, -1e-42, 1.0, 3e38],
+                                np.float32), w.shape)
+    mass = T.from_numpy(w.copy()).cuda()
+    out = mass if in_place else T.full_like(mass, 5.0)
+    kept = T.full((layers, len(lens), hkv, keep), -7, dtype=T.int32, device="cuda")
+    tokens = _int(lens)
+    tokens_out = T.full_like(tokens, -7)
+    dst = None if in_place else Cache([min(n, keep) for n in lens], hkv, d, dtype, page,
+                                      layers=layers, seed=9)
+    att = kvx.Attention(kvx.ModelShape(layers, hkv, d, 1e4), hkv,
+                        kvx.KVX_BF16 if dtype == "bf16" else kvx.KVX_F32)
+    io = kvx.make_evict_io(cache.struct, tokens, mass, kept, keep, sink=sink, recent=recent,
+                           mass_out=out, tokens_out=tokens_out, dst=dst and dst.struct)
+    unused = None if in_place else [int(t.isnan().sum()) for t in dst.dev]
+    att.evict(io)
+    T.cuda.synchronize()
+    assert tokens_out.tolist() == [min(n, keep) for n in lens]
+    got, wo = kept.cpu().numpy(), out.cpu().numpy()
+    at = cache if in_place else dst
+    host = [t.cpu() for t in at.dev]
+    for b, n in enumerate(lens):
+        r = min(n, keep)
+        blk, slot = at.place(b, np.arange(r))
+        for l in range(layers):
+            for h in range(hkv):
+                ref = R.keep(w[l, b, h, :n], keep, sink, recent)
+                assert (got[l, b, h, :r] == ref).all(), (name, l, b, h)
+                assert (got[l, b, h, r:] == -1).all()
+                assert (wo[l, b, h, :r].view(np.int32) == w[l, b, h, ref].view(np.int32)).all()
+                assert (wo[l, b, h, r:max(n, keep)] == 0).all()
+                for kv in range(2):
+                    rows = host[kv][l][blk, h, slot]
+                    assert T.equal(rows, cache.rows[kv][l][b][ref, h]), (name, l, b, h, kv)
+    if not in_place:  # the other rows hold their NaN as before
+        assert [int(t.isnan().sum()) for t in host] == unused
+    att.close()
+
+
+def _step(att, cache, lens, new, hq, hkv, d, seed):
+    """One decoding step's tensors and io."""
+    T = U.torch()
+    starts = _starts(new)
+    x = [_rows(int(starts[-1]), h, d, "bf16", seed + i) for i, h in enumerate((hq, hkv, hkv))]
+    t = dict(q=T.zeros_like(x[0]), out=T.zeros_like(x[0]),
+             lse=T.zeros(int(starts[-1]), hq, device="cuda"),
+             mass=T.zeros(len(lens), hkv, max(lens) + 40, device="cuda"), tokens=_int(lens))
+    io = kvx.make_attn_io(cache.struct, t["tokens"], t["q"], layer=1, max_new=max(new),
+                          q_start=_int(starts), new_q=x[0], new_k=x[1], new_v=x[2], out=t["out"],
+                          lse=t["lse"], mass_in=t["mass"], mass=t["mass"])
+    return t, io, x
+
+
+def test_streams_and_graph():
+    """A captured step (append, forward, mass) replayed at other lengths and
+    inputs gives the eager call's bits, on another stream than the tensors'."""
+    T = U.torch()
+    hq, hkv, d = 12, 2, 128
+    for new in ([1, 1, 1], [40, 3, 17]):
+        att = kvx.Attention(kvx.ModelShape(2, hkv, d, 1e4), hq, kvx.KVX_BF16)
+        ws = att.workspace()
+        lens = [100, 333, 64]
+        cache = Cache(lens, hkv, d, "bf16", 16, extra=30)
+        eager = Cache(lens, hkv, d, "bf16", 16, extra=30)
+        t, io, x = _step(att, cache, lens, new, hq, hkv, d, 1)
+        e, eio, ex = _step(att, eager, lens, new, hq, hkv, d, 1)
+        side = T.cuda.Stream()
+        side.wait_stream(T.cuda.current_stream())
+        graph = T.cuda.CUDAGraph()
+        with T.cuda.graph(graph, stream=side):
+            att.append(io)
+            att.forward(io, ws)
+            att.mass(io)
+        for step in range(4):
+            for a, b in zip(x, ex):
+                fresh = T.randn_like(a)
+                a.copy_(fresh)
+                b.copy_(fresh)
+            graph.replay()
+            T.cuda.synchronize()
+            att.append(eio)
+            att.forward(eio, ws)
+            att.mass(eio)
+            T.cuda.synchronize()
+            for k in t:
+                assert T.equal(t[k], e[k]), (new, step, k)
+            t["tokens"] += min(new)  # every slot below stays filled
+            e["tokens"] += min(new)
+        att.close()
+
+
+def test_handoff_then_decode():
+    """A translated paged cache, decoded on: what append and forward give on
+    the cache that kvx_translate wrote equals the reference on its rows."""
+    from paper_2608_30963_amd import synth as S
+    T = U.torch()
+    spec = S.config(2, src_tokens=100)
+    prob = S.make_problem(spec)
+    dev = U.DevProblem(prob, cap=1)
+    tgt, bs, hq = spec.tgt, 16, 12
+    per = 8
+    table = T.randperm(per, generator=T.Generator().manual_seed(1)).to(T.int32).view(1, per).cuda()
+    shape = (tgt.n_layers, per, tgt.n_kv_heads, bs, tgt.head_dim)
+    k = T.full(shape, float("nan"), dtype=T.bfloat16, device="cuda")
+    v = T.full_like(k, float("nan"))
+    dev.tr(dev.src_k, dev.src_v, k, v, None, block_table=table, block_size=bs)
+    att = kvx.Attention(tgt, hq, kvx.KVX_BF16)
+    cache = kvx.make_cache(k, v, table)
+    ws = att.workspace()
+    tokens = _int([100])
+    x = [_rows(3, h, tgt.head_dim, "bf16", 50 + h) for h in (hq, 2, 2)]
+    tokens += 3
+    q, out = T.zeros_like(x[0]), T.zeros_like(x[0])
+    io = kvx.make_attn_io(cache, tokens, q, layer=5, max_new=3, q_start=_int([0, 3]), new_q=x[0],
+                          new_k=x[1], new_v=x[2], out=out)
+    att.append(io)
+    att.forward(io, ws)
+    T.cuda.synchronize()
+    j = np.arange(103)
+    blk = table.cpu().numpy()[0][j // bs].astype(np.int64)
+    kk, vv = (_f64(t[5].cpu()[blk, :, j % bs]) for t in (k, v))
+    assert np.isfinite(kk).all() and np.isfinite(vv).all()
+    ro, _, mag, size = R.attend(_f64(q), kk, vv, tgt.head_dim ** -0.5)
+    tol = mag * (2 * _delta(size, 128, 0.0) + 2.0 ** -8 + 200 * EPS)[..., None] + 2.0 ** -8 * np.abs(ro)
+    assert (np.abs(_f64(out) - ro) <= tol).all()
+    att.close()
+    dev.close()
+
+
+def test_validation_and_faults(monkeypatch):
+    T = U.torch()
+    lens, new = [40, 20], [3, 1]
+    cache = Cache(lens, 2, 64, "bf16", 16)
+    att = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_BF16)
+    ws = att.workspace()
+    t, io, _ = _step(att, cache, lens, new, 4, 2, 64, 1)
+    monkeypatch.setenv("KVX_VALIDATE", "1")
+    att.append(io)
+    att.forward(io, ws)
+    att.mass(io)
+
+    def refused(call, status):
+        with pytest.raises(kvx.KvxError) as e:
+            call()
+        assert e.value.status == status
+
+    calls = (lambda: att.append(io), lambda: att.forward(io, ws), lambda: att.mass(io))
+    for bad in (-1, cache.table.shape[1] * 16 + 1):
+        t["tokens"][0] = bad
+        for call in calls:
+            refused(call, kvx.KVX_EDATA)
+    t["tokens"][0] = 40
+    keep = cache.table.clone()
+    cache.table[0, 2] = 10 ** 6  # the block of slots 32..39
+    for call in calls:
+        refused(call, kvx.KVX_EDATA)
+    kept = T.zeros((2, 2, 2, 8), dtype=T.int32, device="cuda")
+    mass = T.zeros(2, 2, 2, 64, device="cuda")
+    ev = kvx.make_evict_io(cache.struct, t["tokens"], mass, kept, 8)
+    refused(lambda: att.evict(ev), kvx.KVX_EDATA)
+    cache.table.copy_(keep)
+    io.tensors[3][1] = 9  # q_start not rising
+    for call in calls:
+        refused(call, kvx.KVX_EDATA)
+    io.tensors[3][1] = 3
+    monkeypatch.delenv("KVX_VALIDATE")
+    monkeypatch.setenv("KVX_FAULT", "launch")
+    for call in calls + (lambda: att.evict(ev),):
+        refused(call, kvx.KVX_EHIP)
+    monkeypatch.delenv("KVX_FAULT")
+    for call in calls:
+        call()
+    T.cuda.synchronize()
+    att.close()
+
+
+def test_offsets_past_32_bits():
+    """A cache whose last layer starts past 2^32 bytes, and blocks past 2^31
+    elements of it."""
+    T = U.torch()
+    hkv, d, bs, nb = 2, 128, 16, 600_000  # 2.46e9 elements a layer
+    k = T.zeros((1, nb, hkv, bs, d), dtype=T.bfloat16, device="cuda")
+    v = T.zeros_like(k)
+    table = _int([3, nb - 1, nb // 2 + 5, nb - 9]).view(1, 4)
+    n = 60
+    j = T.arange(n)
+    rows = [T.randn(n, hkv, d).bfloat16() for _ in range(2)]
+    blk = table[0].cpu().long()[j // bs]
+    for t, r in zip((k, v), rows):
+        for i in range(n):
+            t[0, blk[i], :, j[i] % bs] = r[i].cuda()
+    att = kvx.Attention(kvx.ModelShape(1, hkv, d, 1e4), 4, kvx.KVX_BF16)
+    cache = kvx.make_cache(k, v, table)
+    for m in (1, 20):
+        q = _rows(m, 4, d, "bf16", 3)
+        out = T.zeros_like(q)
+        io = kvx.make_attn_io(cache, _int([n]), q, out=out, max_new=m, q_start=_int([0, m]))
+        att.forward(io, att.workspace())
+        T.cuda.synchronize()
+        ro, _, mag, _ = R.attend(_f64(q), _f64(rows[0]), _f64(rows[1]), d ** -0.5)
+        assert (np.abs(_f64(out) - ro) <= mag * 2.0 ** -7).all()
+    x = [_rows(1, 2, d, "bf16", 8 + i) for i in range(2)]
+    io = kvx.make_attn_io(cache, _int([n + 1]), None, new_k=x[0], new_v=x[1])
+    att.append(io)
+    T.cuda.synchronize()
+    assert T.equal(v[0, nb - 9, :, n % bs], x[1][0])
+    att.close()
