@@ -50,6 +50,8 @@ struct CacheArgs {
   int32_t max_blocks;
   int32_t capacity;  // slots of a context
   FastDiv bs;
+  bool aligned;      // any 8 slots from a multiple of 8 on lie in one block, row
+                     // strides of 8 rows within 31 bits
 };
 
 __device__ __forceinline__ int32_t cache_block(const CacheArgs& c, int b, int j) {
@@ -70,6 +72,7 @@ struct AttnArgs {
   const int32_t* prefix;   // NULL: none
   const int32_t* pos;      // append: [axes][rows], NULL: slots
   int32_t batch, rows, hq, hkv, group, d;
+  FastDiv by_group;        // division by group
   int32_t window;          // 0: none
   float scale2;            // score scale * log2(e); with a cap scale / cap
   float cap2;              // cap * log2(e), 0: none

@@ -67,6 +67,7 @@ kvx_status prepare_cache(const kvx_attn* at, const kvx_cache& in, int32_t batch,
   c.max_blocks = paged ? in.max_blocks : 1;
   c.capacity = static_cast<int32_t>(cap);
   c.bs = fast_div(paged ? in.block_size : in.capacity);
+  c.aligned = (!paged || in.block_size % 8 == 0) && s[3] * es < (int64_t(1) << 28);
   return KVX_OK;
 }
 
@@ -104,6 +105,7 @@ kvx_status prepare(const kvx_attn* at, const kvx_attn_io* io, AttnArgs& a) {
   a.hq = at->n_heads;
   a.hkv = at->model.n_kv_heads;
   a.group = at->group;
+  a.by_group = fast_div(at->group);
   a.d = at->model.head_dim;
   a.window = io->window;
   const double log2e = 1.4426950408889634;

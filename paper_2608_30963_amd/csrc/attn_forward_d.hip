@@ -1,0 +1,595 @@
+// attn_forward_d.hip -- the attention kernels of one padded head_dim
+// (KVX_ATTN_DP = 64, 128 or 256), both dtypes.
+#include "attn_forward.h"
+#include "attn_tile.h"
+
+namespace kvx {
+namespace {
+
+// Query rows of a unit are (new token, head of the group), the group fastest:
+// all heads that share a KV head share its tiles.
+struct QueryRow {
+  int row, g;    // row of the new tokens, head within the group
+  int lo, hi;    // slots that it sees
+};
+
+__device__ __forceinline__ QueryRow query_row(const AttnArgs& a, const Context& c, int r) {
+  QueryRow q;
+  const int i = fdiv(a.by_group, r);
+  q.row = c.q0 + i;
+  q.g = r - i * a.group;
+  const int p = c.n - c.m + i;
+  q.lo = first_seen(a, p);
+  q.hi = r < c.m * a.group ? end_seen(c, p) : 0;
+  return q;
+}
+
+// Slots that query rows r0 .. r1 of a context see together.
+__device__ __forceinline__ void seen_by(const AttnArgs& a, const Context& c, int r0, int r1,
+                                        int& lo, int& hi) {
+  const int p0 = c.n - c.m + fdiv(a.by_group, r0), p1 = c.n - c.m + fdiv(a.by_group, r1);
+  hi = end_seen(c, p1);
+  lo = min(first_seen(a, max(p0, 0)), hi);
+}
+
+// Query rows from r0 on that see nothing: their slots are negative.
+__device__ __forceinline__ int unseeing(const AttnArgs& a, const Context& c, int r0) {
+  return max(0, (c.m - c.n) * a.group - r0);
+}
+
+// out row of query (row, head) from O^T registers and its sum; lane (n, h) has
+// 4 columns of each 8.
+template <typename T, int NB>
+__device__ __forceinline__ void store_out(const AttnArgs& a, const QueryRow& q, int h,
+                                          const f32x16 (&acc)[NB], const Softmax& st) {
+  const int half = (threadIdx.x % 64) / 32;
+  const float l = half_sum(st.l);
+  const bool sees = q.lo < q.hi;
+  T* o = reinterpret_cast<T*>(a.out) + q.row * a.o_sr + (h * a.group + q.g) * a.o_sh;
+#pragma unroll
+  for (int db = 0; db < NB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4) {
+      const int e = 32 * db + 2 * v + 4 * half;
+      if (e >= a.d) continue;
+      T x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = store_cvt<T>(sees ? acc[db][v + i] / l : 0.f);
+      if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint2*>(o + e) = __builtin_bit_cast(uint2, x);
+      else
+        *reinterpret_cast<uint4*>(o + e) = __builtin_bit_cast(uint4, x);
+    }
+  if (a.lse && half == 0)
+    a.lse[static_cast<int64_t>(q.row) * a.hq + h * a.group + q.g] =
+        sees ? (st.m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------
+// Chunks: 4 waves of 32 query rows share tiles of kTile slots, copied straight
+// into one of two LDS buffers while the other is computed on; one barrier per
+// tile.
+// ---------------------------------------------------------------------------
+
+template <typename T, int DP>
+constexpr int chunk_tile() { return DP * sizeof(T) <= 512 ? 64 : 32; }
+
+template <typename T, int DP, bool CAP>
+__global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
+    forward_chunk(AttnArgs a, ForwardPlan fp) {
+  using L = Tile<T, DP>;
+  constexpr int TK = chunk_tile<T, DP>(), NS = TK / 32, NB = DP / 32;
+  constexpr int kBytes = TK * L::kRowBytes;  // keys or values of a tile
+  constexpr int kCopies = kBytes / 1024 / 4; // of a wave, keys or values
+  __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];  // [buffer][K, V]
+  const int lane = threadIdx.x % 64, n = lane % 32;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+
+  // (head, piece, strip): consecutive units of an XCD share a head's cache;
+  // later strips, which see more, first
+  int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int h = id / (fp.strips * fp.splits);
+  id -= h * fp.strips * fp.splits;
+  const int split = id / fp.strips, strip = fp.strips - 1 - id % fp.strips;
+
+  // the strip's context: 64 contexts a step
+  int b = -1, qt = 0, before = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    int cnt = 0;
+    if (b0 + lane < a.batch) {
+      const Context c = context(a, b0 + lane);
+      cnt = (c.m * a.group + kChunkRows - 1) / kChunkRows;
+    }
+    int sum = cnt;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+      const int y = __shfl_up(sum, i);
+      if (lane >= i) sum += y;
+    }
+    const uint64_t past = __ballot(before + sum > strip);
+    if (past) {
+      const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      b = b0 + f;
+      qt = strip - before - (__shfl(sum, f) - __shfl(cnt, f));
+      break;
+    }
+    before += __shfl(sum, 63);
+  }
+  JoinHead* head = fp.heads + h * fp.strips + strip;
+  if (b < 0) {
+    if (fp.splits > 1 && split == 0 && threadIdx.x == 0) head->pieces = 0;
+    return;
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  qt = __builtin_amdgcn_readfirstlane(qt);
+  const Context c = context(a, b);
+  const int r0 = qt * kChunkRows, valid = min(kChunkRows, c.m * a.group - r0);
+  int lo, hi;
+  seen_by(a, c, r0, r0 + valid - 1, lo, hi);
+  const int tiles = (hi + TK - 1) / TK - lo / TK;
+  const int per = (tiles + fp.splits - 1) / fp.splits;
+  const int t0 = lo / TK + split * per, t1 = min(t0 + per, lo / TK + tiles);
+
+  const QueryRow qr = query_row(a, c, r0 + w * 32 + n);
+  // what the wave's rows see: together, and all of them
+  const int rows_w = min(32, valid - w * 32);
+  int wlo = 0, whi = 0, alo = 0, ahi = 0;
+  if (rows_w > 0) {
+    const int rw = r0 + w * 32;
+    seen_by(a, c, rw, rw + rows_w - 1, wlo, whi);
+    seen_by(a, c, rw, rw, alo, ahi);
+    seen_by(a, c, rw + rows_w - 1, rw + rows_w - 1, alo, whi);
+  }
+  uint4 q[L::kQ];
+  const T* qp = reinterpret_cast<const T*>(a.q) + qr.row * a.q_sr + (h * a.group + qr.g) * a.q_sh;
+  L::load_q(q, r0 + w * 32 + n < c.m * a.group ? qp : nullptr, a.d);
+
+  f32x16 acc[NB];
+#pragma unroll
+  for (int db = 0; db < NB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
+  Softmax st;
+
+  if (a.d < DP) {
+    for (int i = threadIdx.x; i < 4 * kBytes / 16; i += 256)
+      reinterpret_cast<uint4*>(lds)[i] = uint4{0, 0, 0, 0};
+    __syncthreads();
+  }
+  lds_char* const l3 = (lds_char*)(lds);
+  const char* kb = a.c.k + h * a.c.sh * static_cast<int64_t>(sizeof(T));
+  const char* vb = a.c.v + h * a.c.sh * static_cast<int64_t>(sizeof(T));
+  const int64_t stride = a.c.st * static_cast<int64_t>(sizeof(T));
+  int block = 0;
+  auto fetch_block = [&](int t) __attribute__((always_inline)) {
+    block = row_block(a.c, b, t * TK + lane % TK, lo, hi);
+  };
+  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+    const RowOffset off = row_offset<T>(a.c, block, t * TK + lane % TK, lo, hi);
+    const bool uniform = a.c.aligned && t * TK >= lo && t * TK + TK <= hi;
+    lds_char* to = l3 + buf * 2 * kBytes;
+    if (uniform) {
+#pragma unroll
+      for (int i = 0; i < 2 * kCopies; ++i)
+        copy_rows<T, DP, true>(i < kCopies ? kb : vb, off, i % kCopies * 4 + w, stride, a.d,
+                               to + i / kCopies * kBytes);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2 * kCopies; ++i)
+        copy_rows<T, DP, false>(i < kCopies ? kb : vb, off, i % kCopies * 4 + w, stride, a.d,
+                                to + i / kCopies * kBytes);
+    }
+  };
+  if (t0 < t1) {
+    fetch_block(t0);
+    copy_tile(t0, 0);
+    if (t0 + 1 < t1) fetch_block(t0 + 1);
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    // the tile has landed, and every wave is done with the other buffer
+    __builtin_amdgcn_s_waitcnt(vm_le(0));
+    tile_barrier();
+    if (t + 1 < t1) copy_tile(t + 1, buf ^ 1);
+    if (t + 2 < t1) fetch_block(t + 2);
+    const int j0 = t * TK;
+    if (j0 >= whi || j0 + TK <= wlo) continue;
+    const char* k = lds + buf * 2 * kBytes;
+    const char* v = k + kBytes;
+    f32x16 s[NS];
+#pragma unroll
+    for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, q);
+    if constexpr (CAP) cap_scores(a, s);
+    const bool masked = j0 < alo || j0 + TK > ahi;
+    if (masked)
+#pragma unroll
+      for (int u = 0; u < NS; ++u) mask_scores(s[u], j0 + 32 * u, qr.lo, qr.hi);
+    softmax_step(CAP ? 1.f : a.scale2, s, st, acc);
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+      const char* vu = v + u * 32 * L::kRowBytes;
+      if (masked && L::any_odd(vu)) {
+        L::template add_values<true>(vu, s[u], acc);
+        L::add_odd_values(a, k + u * 32 * L::kRowBytes, vu, q, st.m2, qr.lo, qr.hi, j0 + 32 * u, acc);
+      } else {
+        L::template add_values<false>(vu, s[u], acc);
+      }
+    }
+  }
+
+  if (fp.splits == 1) {
+    if (r0 + w * 32 + n < c.m * a.group) store_out<T, NB>(a, qr, h, acc, st);
+    return;
+  }
+  const int unit = h * fp.strips + strip;
+  float* part = fp.pieces + (static_cast<size_t>(unit) * fp.splits + split) * piece_floats(kChunkRows, DP);
+  const float l = half_sum(st.l);
+  if (w * 32 + n < valid) {
+    if (lane < 32) reinterpret_cast<float2*>(part)[w * 32 + n] = float2{st.m2, l};
+    float* o = part + 2 * kChunkRows + static_cast<size_t>(w * 32 + n) * DP;
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4)
+        *reinterpret_cast<float4*>(o + 32 * db + 2 * v + 4 * (lane / 32)) =
+            float4{acc[db][v], acc[db][v + 1], acc[db][v + 2], acc[db][v + 3]};
+  }
+  if (split == 0 && threadIdx.x == 0)
+    *head = JoinHead{fp.splits, valid, c.q0, r0, h, unit * fp.splits, unseeing(a, c, r0)};
+}
+
+// ---------------------------------------------------------------------------
+// Single tokens (and few): 32 query rows; the waves take different slots, each
+// with its own ring of tiles in LDS and no barrier between them.
+// ---------------------------------------------------------------------------
+
+template <typename T, int DP>
+struct Decode {
+  static constexpr int kStage = 2 * 32 * DP * sizeof(T);  // keys and values of 32 slots
+  static constexpr int kWaves = kStage <= 16384 ? 4 : kStage <= 32768 ? 2 : 1;
+  static constexpr int kStages = 131072 / kWaves / kStage;
+  static constexpr int kStep = kWaves * 32;  // slots of a workgroup's step
+};
+
+// Steps of a context's q tile: at least one, so that every row is written.
+template <int STEP>
+__device__ __forceinline__ int decode_steps(const AttnArgs& a, const Context& c, int qt) {
+  int lo, hi;
+  const int r0 = qt * kDecodeRows;
+  seen_by(a, c, r0, min(r0 + kDecodeRows, c.m * a.group) - 1, lo, hi);
+  lo &= ~31;
+  return max(1, (hi - lo + STEP - 1) / STEP);
+}
+
+template <typename T, int DP, bool CAP>
+__global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
+    forward_decode(AttnArgs a, ForwardPlan fp) {
+  using L = Tile<T, DP>;
+  using D = Decode<T, DP>;
+  constexpr int NW = D::kWaves, NT = 64 * NW, NST = D::kStages, NB = DP / 32;
+  constexpr int kBytes = 32 * L::kRowBytes;
+  constexpr int kCopies = kBytes / 1024;
+  __shared__ __attribute__((aligned(16))) char lds[NW * NST * D::kStage];
+  __shared__ int64_t scan[NW];
+  __shared__ int found[3];
+  const int tid = threadIdx.x, lane = tid % 64, n = lane % 32;
+  const int w = __builtin_amdgcn_readfirstlane(tid / 64);
+  JoinHead* head = fp.heads + blockIdx.x;
+
+  // steps of all contexts' q tiles of one head, and this workgroup's share of
+  // all heads': an equal range of the line (head, context, q tile, step)
+  auto steps_of = [&](int b) __attribute__((always_inline)) {
+    const Context c = context(a, b);
+    const int qts = (c.m * a.group + kDecodeRows - 1) / kDecodeRows;
+    int64_t s = 0;
+    for (int qt = 0; qt < qts; ++qt) s += decode_steps<D::kStep>(a, c, qt);
+    return s;
+  };
+  // sum over the workgroup's threads before this one, and over all
+  auto block_sum = [&](int64_t x, int64_t& total) __attribute__((always_inline)) {
+    int64_t s = x;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+      const int64_t y = __shfl_up(s, i);
+      if (lane >= i) s += y;
+    }
+    __syncthreads();
+    if (lane == 63) scan[w] = s;
+    __syncthreads();
+    int64_t base = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      if (i < w) base += scan[i];
+      total += scan[i];
+    }
+    return base + s - x;
+  };
+  int64_t line = 0;  // of one head
+  int64_t mine = 0, mine_before = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += NT) {
+    int64_t total;
+    mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
+    mine_before = block_sum(mine, total);
+    line += total;
+  }
+  const int64_t whole = line * a.hkv;
+  const int64_t per = (whole + gridDim.x - 1) / gridDim.x;
+  const int64_t s0 = blockIdx.x * per, s1 = min(whole, s0 + per);
+  if (tid == 0) head->pieces = 0;
+  if (s0 >= s1) return;
+  int h = static_cast<int>(s0 / line);
+  // the context that holds the first step
+  int64_t at = s0 - h * line;
+  if (a.batch <= NT) {
+    if (mine_before <= at && at < mine_before + mine) {
+      found[0] = tid;
+      found[1] = static_cast<int>(at - mine_before);
+    }
+    __syncthreads();
+  } else {
+    int64_t before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += NT) {
+      int64_t total;
+      mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
+      mine_before = before + block_sum(mine, total);
+      if (mine_before <= at && at < mine_before + mine) {
+        found[0] = b0 + tid;
+        found[1] = static_cast<int>(at - mine_before);
+      }
+      before += total;
+      if (before > at) break;
+    }
+    __syncthreads();
+  }
+  int b = __builtin_amdgcn_readfirstlane(found[0]);
+  int step = __builtin_amdgcn_readfirstlane(found[1]);
+  Context c = context(a, b);
+  int qt = 0;
+  for (int x; step >= (x = decode_steps<D::kStep>(a, c, qt)); ++qt) step -= x;
+
+  char* const ring = lds + w * NST * D::kStage;
+  lds_char* const ring3 = (lds_char*)(ring);
+  const int64_t stride = a.c.st * static_cast<int64_t>(sizeof(T));
+
+  for (int64_t s = s0; s < s1;) {
+    // one unit: steps [step, step + cnt) of its `all`
+    const int all = decode_steps<D::kStep>(a, c, qt);
+    const int cnt = static_cast<int>(min<int64_t>(all - step, s1 - s));
+    const int r0 = qt * kDecodeRows, valid = min(kDecodeRows, c.m * a.group - r0);
+    int lo, hi, alo, ahi, xlo, xhi;
+    seen_by(a, c, r0, r0 + valid - 1, lo, hi);
+    seen_by(a, c, r0, r0, xlo, ahi);                          // the least that any row's end is
+    seen_by(a, c, r0 + valid - 1, r0 + valid - 1, alo, xhi);  // the most that any row's start is
+    const int j_first = (lo & ~31) + (step * NW + w) * 32;
+    // tiles of this wave: every NW-th of the range, as far as slots are seen
+    const int tiles = min(cnt, hi > j_first ? (hi - j_first + NW * 32 - 1) / (NW * 32) : 0);
+    const QueryRow qr = query_row(a, c, r0 + n);
+    uint4 q[L::kQ];
+    const T* qp = reinterpret_cast<const T*>(a.q) + qr.row * a.q_sr + (h * a.group + qr.g) * a.q_sh;
+    L::load_q(q, n < valid ? qp : nullptr, a.d);
+    const char* kb = a.c.k + h * a.c.sh * static_cast<int64_t>(sizeof(T));
+    const char* vb = a.c.v + h * a.c.sh * static_cast<int64_t>(sizeof(T));
+    f32x16 acc[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
+    Softmax st;
+    __syncthreads();  // LDS is free of the last unit's join
+    if (a.d < DP) {
+      // copies leave the chunks past head_dim alone: zeros
+      for (int i = lane; i < NST * D::kStage / 16; i += 64)
+        reinterpret_cast<uint4*>(ring)[i] = uint4{0, 0, 0, 0};
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+
+    int block = 0;
+    auto slot_of = [&](int t) __attribute__((always_inline)) { return j_first + t * NW * 32; };
+    auto fetch_block = [&](int t) __attribute__((always_inline)) {
+      block = row_block(a.c, b, slot_of(t) + n, lo, hi);
+    };
+    auto copy_tile = [&](int t) __attribute__((always_inline)) {
+      const int j0 = slot_of(t);
+      const RowOffset off = row_offset<T>(a.c, block, j0 + n, lo, hi);
+      const bool uniform = a.c.aligned && j0 >= lo && j0 + 32 <= hi;
+      lds_char* to = ring3 + t % NST * D::kStage;
+      if (uniform) {
+#pragma unroll
+        for (int i = 0; i < 2 * kCopies; ++i)
+          copy_rows<T, DP, true>(i < kCopies ? kb : vb, off, i % kCopies, stride, a.d,
+                                 to + i / kCopies * kBytes);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2 * kCopies; ++i)
+          copy_rows<T, DP, false>(i < kCopies ? kb : vb, off, i % kCopies, stride, a.d,
+                                  to + i / kCopies * kBytes);
+      }
+    };
+    if (tiles > 0) fetch_block(0);
+    for (int t = 0; t < NST - 1 && t < tiles; ++t) {
+      const int cur = block;
+      if (t + 1 < tiles) fetch_block(t + 1);
+      const int nxt = block;
+      block = cur;
+      copy_tile(t);
+      block = nxt;
+    }
+    for (int t = 0; t < tiles; ++t) {
+      // the stage that tile t + NST - 1 takes was read a tile ago
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (t + NST - 1 < tiles) {
+        const int cur = block;
+        if (t + NST < tiles) fetch_block(t + NST);
+        const int nxt = block;
+        block = cur;
+        copy_tile(t + NST - 1);
+        block = nxt;
+        // all but the last NST - 1 tiles' copies have landed
+        __builtin_amdgcn_s_waitcnt(vm_le((NST - 1) * 2 * kCopies));
+      } else {
+        __builtin_amdgcn_s_waitcnt(vm_le(0));
+      }
+      asm volatile("" ::: "memory");
+      const char* k = ring + t % NST * D::kStage;
+      const char* v = k + kBytes;
+      const int j0 = slot_of(t);
+      f32x16 sc[1];
+      sc[0] = L::scores(k, q);
+      if constexpr (CAP) cap_scores(a, sc);
+      const bool edge = j0 < alo || j0 + 32 > ahi;
+      if (edge) mask_scores(sc[0], j0, qr.lo, qr.hi);
+      softmax_step(CAP ? 1.f : a.scale2, sc, st, acc);
+      if (edge && L::any_odd(v)) {
+        L::template add_values<true>(v, sc[0], acc);
+        L::add_odd_values(a, k, v, q, st.m2, qr.lo, qr.hi, j0, acc);
+      } else {
+        L::template add_values<false>(v, sc[0], acc);
+      }
+    }
+
+    // the waves' results through LDS: each in its own ring, rows of DP floats,
+    // 16-byte pieces swizzled by the row; then (m2, l)
+    const float l = half_sum(st.l);
+    if (n < valid) {
+      float4* o = reinterpret_cast<float4*>(ring) + n * (DP / 4);
+#pragma unroll
+      for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          o[(8 * db + 2 * x + lane / 32) ^ (n & 7)] =
+              float4{acc[db][4 * x], acc[db][4 * x + 1], acc[db][4 * x + 2], acc[db][4 * x + 3]};
+      if (lane < 32)
+        reinterpret_cast<float2*>(ring + 32 * DP * 4)[n] = float2{st.m2, l};
+    }
+    __syncthreads();
+    const bool begins = step == 0, ends = step + cnt == all;
+    float* part = fp.pieces + (2 * static_cast<size_t>(blockIdx.x) + (begins ? 1 : 0)) * piece_floats(kDecodeRows, DP);
+    for (int i = tid; i < valid * (DP / 4); i += NT) {
+      const int r = i / (DP / 4), e = i % (DP / 4);
+      float2 ml[NW];
+      float m2 = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < NW; ++x) {
+        ml[x] = reinterpret_cast<const float2*>(lds + x * NST * D::kStage + 32 * DP * 4)[r];
+        m2 = fmaxf(m2, ml[x].x);
+      }
+      float lsum = 0.f;
+      float4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < NW; ++x) {
+        const float f = ml[x].x == m2 ? 1.f : __builtin_amdgcn_exp2f(ml[x].x - m2);
+        const float4 y = reinterpret_cast<const float4*>(lds + x * NST * D::kStage)[r * (DP / 4) + (e ^ (r & 7))];
+        lsum += f * ml[x].y;
+        o.x += f * y.x;
+        o.y += f * y.y;
+        o.z += f * y.z;
+        o.w += f * y.w;
+      }
+      if (begins && ends) {
+        const QueryRow u = query_row(a, c, r0 + r);
+        const bool sees = u.lo < u.hi;
+        if (4 * e < a.d) {
+          T* to = reinterpret_cast<T*>(a.out) + u.row * a.o_sr + (h * a.group + u.g) * a.o_sh + 4 * e;
+          const float x[4] = {o.x, o.y, o.z, o.w};
+          T y[4];
+#pragma unroll
+          for (int z = 0; z < 4; ++z) y[z] = store_cvt<T>(sees ? x[z] / lsum : 0.f);
+          if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, y);
+          else
+            *reinterpret_cast<uint4*>(to) = __builtin_bit_cast(uint4, y);
+        }
+        if (a.lse && e == 0)
+          a.lse[static_cast<int64_t>(u.row) * a.hq + h * a.group + u.g] =
+              sees ? (m2 + __builtin_amdgcn_logf(lsum)) * kLn2 : -INFINITY;
+      } else {
+        reinterpret_cast<float4*>(part + 2 * kDecodeRows)[i] = o;
+        if (e == 0) reinterpret_cast<float2*>(part)[r] = float2{m2, lsum};
+      }
+    }
+    if (begins && !ends && tid == 0) {
+      // the unit's other pieces are the first ones of the next workgroups
+      const int64_t end = s - step + all;
+      *head = JoinHead{static_cast<int32_t>((end - 1) / per - blockIdx.x + 1), valid, c.q0, r0, h,
+                       static_cast<int32_t>(2 * blockIdx.x + 1), unseeing(a, c, r0)};
+    }
+    s += cnt;
+    step = 0;
+    if (s < s1) {
+      // the next q tile, of this context or one with new tokens after it
+      ++qt;
+      while (qt * kDecodeRows >= c.m * a.group) {
+        qt = 0;
+        if (++b == a.batch) {
+          b = 0;
+          ++h;
+        }
+        c = context(a, b);
+      }
+    }
+  }
+}
+
+// Joins the pieces of units in their order: one wave a query row.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) forward_join(AttnArgs a, ForwardPlan fp) {
+  const JoinHead hd = fp.heads[blockIdx.x];
+  const int r = blockIdx.y * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
+  if (hd.pieces == 0 || r >= hd.rows) return;
+  const int unit_rows = fp.decode ? kDecodeRows : kChunkRows;
+  const size_t size = piece_floats(unit_rows, DP);
+  constexpr int PER = DP / 64;
+  float m2 = -INFINITY, l = 0.f, o[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) o[i] = 0.f;
+  for (int p = 0; p < hd.pieces; ++p) {
+    // decode: piece 0 is slot 1 of its workgroup, the others slot 0 of the next ones
+    const size_t at = fp.decode ? (p == 0 ? hd.first : hd.first - 1 + 2 * static_cast<size_t>(p)) : hd.first + p;
+    const float* part = fp.pieces + at * size;
+    const float2 ml = reinterpret_cast<const float2*>(part)[r];
+    const float* x = part + 2 * unit_rows + static_cast<size_t>(r) * DP + lane * PER;
+    const float m = fmaxf(m2, ml.x);
+    const float f0 = m2 == m ? 1.f : __builtin_amdgcn_exp2f(m2 - m);
+    const float f1 = ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m);
+    m2 = m;
+    l = l * f0 + ml.y * f1;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) o[i] = o[i] * f0 + x[i] * f1;
+  }
+  const int rr = hd.g0 + r, tok = fdiv(a.by_group, rr), g = rr - tok * a.group;
+  const int64_t row = hd.row0 + tok;
+  const int head = hd.h * a.group + g;
+  const bool sees = r >= hd.empty;
+  T* to = reinterpret_cast<T*>(a.out) + row * a.o_sr + head * a.o_sh + lane * PER;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (lane * PER + i < a.d) to[i] = store_cvt<T>(sees ? o[i] / l : 0.f);
+  if (a.lse && lane == 0)
+    a.lse[row * a.hq + head] = sees ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
+}  // namespace
+
+template <typename T, int DP>
+hipError_t run_forward(const AttnArgs& a, const ForwardPlan& p, hipStream_t st) {
+  const bool cap = a.cap2 != 0.f;
+  hipError_t e;
+  if (p.decode) {
+    const dim3 block(64 * Decode<T, DP>::kWaves);
+    e = cap ? launch_on(forward_decode<T, DP, true>, dim3(p.grid), block, st, a, p)
+            : launch_on(forward_decode<T, DP, false>, dim3(p.grid), block, st, a, p);
+  } else {
+    e = cap ? launch_on(forward_chunk<T, DP, true>, dim3(p.grid), dim3(256), st, a, p)
+            : launch_on(forward_chunk<T, DP, false>, dim3(p.grid), dim3(256), st, a, p);
+    if (p.splits == 1) return e;
+  }
+  if (e != hipSuccess) return e;
+  const int units = p.decode ? p.grid : p.strips * a.hkv;
+  return launch_on(forward_join<T, DP>, dim3(units, (p.join_rows + 3) / 4), dim3(256), st, a, p);
+}
+
+template hipError_t run_forward<float, KVX_ATTN_DP>(const AttnArgs&, const ForwardPlan&, hipStream_t);
+template hipError_t run_forward<bf16_t, KVX_ATTN_DP>(const AttnArgs&, const ForwardPlan&, hipStream_t);
+
+}  // namespace kvx
