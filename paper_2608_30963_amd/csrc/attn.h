@@ -50,8 +50,8 @@ struct CacheArgs {
   int32_t max_blocks;
   int32_t capacity;  // slots of a context
   FastDiv bs;
-  bool aligned;      // any 8 slots from a multiple of 8 on lie in one block, row
-                     // strides of 8 rows within 31 bits
+  int32_t run;       // power of two up to 64: that many slots, from a multiple of
+                     // it on, lie in one block, at 32-bit offsets; 1 otherwise
 };
 
 __device__ __forceinline__ int32_t cache_block(const CacheArgs& c, int b, int j) {

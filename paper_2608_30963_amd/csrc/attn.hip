@@ -67,7 +67,9 @@ kvx_status prepare_cache(const kvx_attn* at, const kvx_cache& in, int32_t batch,
   c.max_blocks = paged ? in.max_blocks : 1;
   c.capacity = static_cast<int32_t>(cap);
   c.bs = fast_div(paged ? in.block_size : in.capacity);
-  c.aligned = (!paged || in.block_size % 8 == 0) && s[3] * es < (int64_t(1) << 28);
+  c.run = 64;
+  while (paged && in.block_size % c.run) c.run /= 2;
+  if (s[3] * es >= (int64_t(1) << 25)) c.run = 1;
   return KVX_OK;
 }
 

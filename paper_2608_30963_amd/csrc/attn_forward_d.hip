@@ -80,7 +80,6 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   using L = Tile<T, DP>;
   constexpr int TK = chunk_tile<T, DP>(), NS = TK / 32, NB = DP / 32;
   constexpr int kBytes = TK * L::kRowBytes;  // keys or values of a tile
-  constexpr int kCopies = kBytes / 1024 / 4; // of a wave, keys or values
   __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];  // [buffer][K, V]
   const int lane = threadIdx.x % 64, n = lane % 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -156,86 +155,97 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
       reinterpret_cast<uint4*>(lds)[i] = uint4{0, 0, 0, 0};
     __syncthreads();
   }
-  lds_char* const l3 = (lds_char*)(lds);
+  const uint32_t l3 = lds_address(lds);
   const char* kb = a.c.k + h * a.c.sh * static_cast<int64_t>(sizeof(T));
   const char* vb = a.c.v + h * a.c.sh * static_cast<int64_t>(sizeof(T));
-  const int64_t stride = a.c.st * static_cast<int64_t>(sizeof(T));
-  int block = 0;
-  auto fetch_block = [&](int t) __attribute__((always_inline)) {
-    block = row_block(a.c, b, t * TK + lane % TK, lo, hi);
-  };
-  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
-    const RowOffset off = row_offset<T>(a.c, block, t * TK + lane % TK, lo, hi);
-    const bool uniform = a.c.aligned && t * TK >= lo && t * TK + TK <= hi;
-    lds_char* to = l3 + buf * 2 * kBytes;
-    if (uniform) {
-#pragma unroll
-      for (int i = 0; i < 2 * kCopies; ++i)
-        copy_rows<T, DP, true>(i < kCopies ? kb : vb, off, i % kCopies * 4 + w, stride, a.d,
-                               to + i / kCopies * kBytes);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2 * kCopies; ++i)
-        copy_rows<T, DP, false>(i < kCopies ? kb : vb, off, i % kCopies * 4 + w, stride, a.d,
-                                to + i / kCopies * kBytes);
-    }
-  };
+  Copies<T, DP, TK, 4> blocks;
+  bool odd = false;
+  const typename L::LaneAt at = L::lane_at();
+  // the queries are here: the compiler must not wait for them in the loop
+  __builtin_amdgcn_s_waitcnt(0);
   if (t0 < t1) {
-    fetch_block(t0);
-    copy_tile(t0, 0);
-    if (t0 + 1 < t1) fetch_block(t0 + 1);
+    fetch_blocks(a.c, b, t0 * TK, hi, w, blocks);
+    copy_tile<T, DP, TK, 4>(a.c, kb, vb, b, t0 * TK, lo, hi, blocks, a.d, w, l3);
+    fetch_blocks(a.c, b, t0 * TK + TK, hi, w, blocks);
   }
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1;
     // the tile has landed, and every wave is done with the other buffer
-    __builtin_amdgcn_s_waitcnt(vm_le(0));
+    vm_wait<0>();
     tile_barrier();
-    if (t + 1 < t1) copy_tile(t + 1, buf ^ 1);
-    if (t + 2 < t1) fetch_block(t + 2);
     const int j0 = t * TK;
+    if (t + 1 < t1) {
+      copy_tile<T, DP, TK, 4>(a.c, kb, vb, b, j0 + TK, lo, hi, blocks, a.d, w, l3 + (buf ^ 1) * 2 * kBytes);
+      fetch_blocks(a.c, b, j0 + 2 * TK, hi, w, blocks);
+    }
     if (j0 >= whi || j0 + TK <= wlo) continue;
     const char* k = lds + buf * 2 * kBytes;
     const char* v = k + kBytes;
-    f32x16 s[NS];
+    if (j0 >= alo && j0 + TK <= ahi) {
+      f32x16 s[NS];
 #pragma unroll
-    for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, q);
-    if constexpr (CAP) cap_scores(a, s);
-    const bool masked = j0 < alo || j0 + TK > ahi;
-    if (masked)
+      for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, at, q);
+      if constexpr (CAP) cap_scores(a, s);
+      softmax_step(CAP ? 1.f : a.scale2, s, st, acc);
 #pragma unroll
-      for (int u = 0; u < NS; ++u) mask_scores(s[u], j0 + 32 * u, qr.lo, qr.hi);
-    softmax_step(CAP ? 1.f : a.scale2, s, st, acc);
-#pragma unroll
-    for (int u = 0; u < NS; ++u) {
-      const char* vu = v + u * 32 * L::kRowBytes;
-      if (masked && L::any_odd(vu)) {
-        L::template add_values<true>(vu, s[u], acc);
-        L::add_odd_values(a, k + u * 32 * L::kRowBytes, vu, q, st.m2, qr.lo, qr.hi, j0 + 32 * u, acc);
-      } else {
-        L::template add_values<false>(vu, s[u], acc);
+      for (int u = 0; u < NS; ++u) L::template add_values<false>(v + u * 32 * L::kRowBytes, at, s[u], acc);
+    } else {
+      // 32 slots at a time: the masks' and checks' registers are not the
+      // loop's above
+#pragma unroll 1
+      for (int u = 0; u < NS; ++u) {
+        odd |= edge_step<T, DP, CAP>(a, k + u * 32 * L::kRowBytes, v + u * 32 * L::kRowBytes, at, q,
+                                     j0 + 32 * u, qr.lo, qr.hi, st, acc);
       }
     }
   }
 
-  if (fp.splits == 1) {
-    if (r0 + w * 32 + n < c.m * a.group) store_out<T, NB>(a, qr, h, acc, st);
-    return;
-  }
   const int unit = h * fp.strips + strip;
   float* part = fp.pieces + (static_cast<size_t>(unit) * fp.splits + split) * piece_floats(kChunkRows, DP);
-  const float l = half_sum(st.l);
-  if (w * 32 + n < valid) {
-    if (lane < 32) reinterpret_cast<float2*>(part)[w * 32 + n] = float2{st.m2, l};
-    float* o = part + 2 * kChunkRows + static_cast<size_t>(w * 32 + n) * DP;
-#pragma unroll
-    for (int db = 0; db < NB; ++db)
-#pragma unroll
-      for (int v = 0; v < 16; v += 4)
-        *reinterpret_cast<float4*>(o + 32 * db + 2 * v + 4 * (lane / 32)) =
-            float4{acc[db][v], acc[db][v + 1], acc[db][v + 2], acc[db][v + 3]};
-  }
-  if (split == 0 && threadIdx.x == 0)
+  if (fp.splits > 1 && split == 0 && threadIdx.x == 0)
     *head = JoinHead{fp.splits, valid, c.q0, r0, h, unit * fp.splits, unseeing(a, c, r0)};
+  if (fp.splits == 1) {
+    if (w * 32 + n < valid) store_out<T, NB>(a, qr, h, acc, st);
+  } else {
+    const float l = half_sum(st.l);
+    if (w * 32 + n < valid) {
+      if (lane < 32) reinterpret_cast<float2*>(part)[w * 32 + n] = float2{st.m2, l};
+      float* o = part + 2 * kChunkRows + static_cast<size_t>(w * 32 + n) * DP;
+#pragma unroll
+      for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<float4*>(o + 32 * db + 2 * v + 4 * (lane / 32)) =
+              float4{acc[db][v], acc[db][v + 1], acc[db][v + 2], acc[db][v + 3]};
+    }
+  }
+  if (!odd) return;
+  vm_wait<0>();  // the rows that change are written again
+#pragma unroll 1
+  for (int r = 0; r < rows_w; ++r) {
+    const QueryRow u = query_row(a, c, r0 + w * 32 + r);
+    float o[DP / 64];
+    Softmax sm;
+    if (!careful_row<T, DP>(
+            a, b, h, reinterpret_cast<const T*>(a.q) + u.row * a.q_sr + (h * a.group + u.g) * a.q_sh,
+            u.lo, u.hi, (t1 - t0) * NS, [&](int t) { return t0 * TK + t * 32; }, sm, o))
+      continue;
+    const int pr = w * 32 + r;
+    if (fp.splits > 1) {
+      if (lane == 0) reinterpret_cast<float2*>(part)[pr] = float2{sm.m2, sm.l};
+#pragma unroll
+      for (int i = 0; i < DP / 64; ++i)
+        part[2 * kChunkRows + static_cast<size_t>(pr) * DP + i * 64 + lane] = o[i];
+    } else {
+      T* to = reinterpret_cast<T*>(a.out) + u.row * a.o_sr + (h * a.group + u.g) * a.o_sh;
+#pragma unroll
+      for (int i = 0; i < DP / 64; ++i)
+        if (i * 64 + lane < a.d) to[i * 64 + lane] = store_cvt<T>(o[i] / sm.l);
+      if (a.lse && lane == 0)
+        a.lse[static_cast<int64_t>(u.row) * a.hq + h * a.group + u.g] =
+            (sm.m2 + __builtin_amdgcn_logf(sm.l)) * kLn2;
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -320,11 +330,11 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
   if (s0 >= s1) return;
   int h = static_cast<int>(s0 / line);
   // the context that holds the first step
-  int64_t at = s0 - h * line;
+  const int64_t into = s0 - h * line;
   if (a.batch <= NT) {
-    if (mine_before <= at && at < mine_before + mine) {
+    if (mine_before <= into && into < mine_before + mine) {
       found[0] = tid;
-      found[1] = static_cast<int>(at - mine_before);
+      found[1] = static_cast<int>(into - mine_before);
     }
     __syncthreads();
   } else {
@@ -333,12 +343,12 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
       int64_t total;
       mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
       mine_before = before + block_sum(mine, total);
-      if (mine_before <= at && at < mine_before + mine) {
+      if (mine_before <= into && into < mine_before + mine) {
         found[0] = b0 + tid;
-        found[1] = static_cast<int>(at - mine_before);
+        found[1] = static_cast<int>(into - mine_before);
       }
       before += total;
-      if (before > at) break;
+      if (before > into) break;
     }
     __syncthreads();
   }
@@ -348,9 +358,9 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
   int qt = 0;
   for (int x; step >= (x = decode_steps<D::kStep>(a, c, qt)); ++qt) step -= x;
 
+  const typename L::LaneAt at = L::lane_at();
   char* const ring = lds + w * NST * D::kStage;
-  lds_char* const ring3 = (lds_char*)(ring);
-  const int64_t stride = a.c.st * static_cast<int64_t>(sizeof(T));
+  const uint32_t ring3 = lds_address(lds) + w * NST * D::kStage;
 
   for (int64_t s = s0; s < s1;) {
     // one unit: steps [step, step + cnt) of its `all`
@@ -384,67 +394,38 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 
-    int block = 0;
     auto slot_of = [&](int t) __attribute__((always_inline)) { return j_first + t * NW * 32; };
-    auto fetch_block = [&](int t) __attribute__((always_inline)) {
-      block = row_block(a.c, b, slot_of(t) + n, lo, hi);
+    Copies<T, DP, 32, 1> blocks;
+    auto copy = [&](int t) __attribute__((always_inline)) {
+      copy_tile<T, DP, 32, 1>(a.c, kb, vb, b, slot_of(t), lo, hi, blocks, a.d, 0,
+                              ring3 + t % NST * D::kStage);
+      fetch_blocks(a.c, b, slot_of(t + 1), hi, 0, blocks);
     };
-    auto copy_tile = [&](int t) __attribute__((always_inline)) {
-      const int j0 = slot_of(t);
-      const RowOffset off = row_offset<T>(a.c, block, j0 + n, lo, hi);
-      const bool uniform = a.c.aligned && j0 >= lo && j0 + 32 <= hi;
-      lds_char* to = ring3 + t % NST * D::kStage;
-      if (uniform) {
-#pragma unroll
-        for (int i = 0; i < 2 * kCopies; ++i)
-          copy_rows<T, DP, true>(i < kCopies ? kb : vb, off, i % kCopies, stride, a.d,
-                                 to + i / kCopies * kBytes);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 2 * kCopies; ++i)
-          copy_rows<T, DP, false>(i < kCopies ? kb : vb, off, i % kCopies, stride, a.d,
-                                  to + i / kCopies * kBytes);
-      }
-    };
-    if (tiles > 0) fetch_block(0);
-    for (int t = 0; t < NST - 1 && t < tiles; ++t) {
-      const int cur = block;
-      if (t + 1 < tiles) fetch_block(t + 1);
-      const int nxt = block;
-      block = cur;
-      copy_tile(t);
-      block = nxt;
-    }
+    bool odd = false;
+    // the queries are here: the compiler must not wait for them in the loop
+    __builtin_amdgcn_s_waitcnt(0);
+    if (tiles > 0) fetch_blocks(a.c, b, slot_of(0), hi, 0, blocks);
+    for (int t = 0; t < NST - 1 && t < tiles; ++t) copy(t);
     for (int t = 0; t < tiles; ++t) {
       // the stage that tile t + NST - 1 takes was read a tile ago
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (t + NST - 1 < tiles) {
-        const int cur = block;
-        if (t + NST < tiles) fetch_block(t + NST);
-        const int nxt = block;
-        block = cur;
-        copy_tile(t + NST - 1);
-        block = nxt;
+        copy(t + NST - 1);
         // all but the last NST - 1 tiles' copies have landed
-        __builtin_amdgcn_s_waitcnt(vm_le((NST - 1) * 2 * kCopies));
+        vm_wait<(NST - 1) * 2 * kCopies>();
       } else {
-        __builtin_amdgcn_s_waitcnt(vm_le(0));
+        vm_wait<0>();
       }
-      asm volatile("" ::: "memory");
       const char* k = ring + t % NST * D::kStage;
       const char* v = k + kBytes;
       const int j0 = slot_of(t);
-      f32x16 sc[1];
-      sc[0] = L::scores(k, q);
-      if constexpr (CAP) cap_scores(a, sc);
-      const bool edge = j0 < alo || j0 + 32 > ahi;
-      if (edge) mask_scores(sc[0], j0, qr.lo, qr.hi);
-      softmax_step(CAP ? 1.f : a.scale2, sc, st, acc);
-      if (edge && L::any_odd(v)) {
-        L::template add_values<true>(v, sc[0], acc);
-        L::add_odd_values(a, k, v, q, st.m2, qr.lo, qr.hi, j0, acc);
+      if (j0 >= alo && j0 + 32 <= ahi) {
+        f32x16 sc[1] = {L::scores(k, at, q)};
+        if constexpr (CAP) cap_scores(a, sc);
+        softmax_step(CAP ? 1.f : a.scale2, sc, st, acc);
+        L::template add_values<false>(v, at, sc[0], acc);
       } else {
-        L::template add_values<false>(v, sc[0], acc);
+        odd |= edge_step<T, DP, CAP>(a, k, v, at, q, j0, qr.lo, qr.hi, st, acc);
       }
     }
 
@@ -461,6 +442,24 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
               float4{acc[db][4 * x], acc[db][4 * x + 1], acc[db][4 * x + 2], acc[db][4 * x + 3]};
       if (lane < 32)
         reinterpret_cast<float2*>(ring + 32 * DP * 4)[n] = float2{st.m2, l};
+    }
+    if (odd) {
+#pragma unroll 1
+      for (int r = 0; r < valid; ++r) {
+        const QueryRow u = query_row(a, c, r0 + r);
+        float o[DP / 64];
+        Softmax sm;
+        if (!careful_row<T, DP>(
+                a, b, h, reinterpret_cast<const T*>(a.q) + u.row * a.q_sr + (h * a.group + u.g) * a.q_sh,
+                u.lo, u.hi, tiles, slot_of, sm, o))
+          continue;
+#pragma unroll
+        for (int i = 0; i < DP / 64; ++i) {
+          const int e = i * 64 + lane;
+          reinterpret_cast<float*>(ring)[r * DP + ((e / 4) ^ (r & 7)) * 4 + e % 4] = o[i];
+        }
+        if (lane == 0) reinterpret_cast<float2*>(ring + 32 * DP * 4)[r] = float2{sm.m2, sm.l};
+      }
     }
     __syncthreads();
     const bool begins = step == 0, ends = step + cnt == all;

@@ -22,10 +22,10 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// s_waitcnt immediate: at most n vector-memory operations outstanding.
-constexpr int vm_le(int n) {
-  const int m = n > 63 ? 63 : n;
-  return (m & 15) | ((m >> 4) << 14) | (7 << 4) | (15 << 8);
+// Waits until at most N vector-memory operations of this wave are outstanding.
+template <int N>
+__device__ __forceinline__ void vm_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N > 63 ? 63 : N) : "memory");
 }
 
 // Workgroup barrier for LDS that leaves vector-memory operations in flight.
@@ -55,20 +55,37 @@ __device__ __forceinline__ bool finite(float x) {
 }
 
 // Rows of head_dim DP (padded with zeros past a.d) in LDS: 16-byte chunk c of
-// row r lies at chunk c ^ (r % 16) of its row (r % 8 where a row has 8
-// chunks), which spreads the rows that one read instruction touches over the
-// banks.
+// row r lies at chunk c ^ (r % 8) of its row, which spreads the rows that one
+// read instruction touches over the banks.  A lane's address is one of a few
+// that are formed once (LaneAt) and a constant: the swizzle is within 128 bytes.
 template <typename T, int DP>
 struct Tile {
   static constexpr int kChunks = DP * sizeof(T) / 16;
-  static constexpr int kSwz = (kChunks < 16 ? kChunks : 16) - 1;
+  static constexpr int kSwz = 7;
   static constexpr int kRowBytes = DP * sizeof(T);
   static constexpr int kRowsPerCopy = 64 / kChunks;  // rows of one wave's copy instruction
   static constexpr bool kBf16 = sizeof(T) == 2;
   static constexpr int kQ = kBf16 ? DP / 16 : DP / 8;  // 16-byte query pieces of a lane
 
-  static __device__ __forceinline__ int chunk_at(int r, int c) {
-    return r * kRowBytes + ((c ^ (r & kSwz)) * 16);
+  struct LaneAt {
+    int k[4];  // keys: row n, chunk 2 i + h is at k[i % 4] + i / 4 * 128
+    int v[4];  // values: see value_frag (bf16: two) and add_values
+  };
+  static __device__ __forceinline__ LaneAt lane_at() {
+    const int lane = threadIdx.x % 64, n = lane % 32, h = lane / 32, i = lane % 16;
+    LaneAt at;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      at.k[x] = n * kRowBytes + ((2 * x + h) ^ (n & 7)) * 16;
+      if constexpr (kBf16) {
+        const int row = 4 * h + i / 4, c = 4 * (x & 1) + 2 * (lane / 16 % 2) + i % 4 / 2;
+        at.v[x] = row * kRowBytes + (c ^ row) * 16 + i % 2 * 8;
+      } else {
+        const int row = 4 * h + x;
+        at.v[x] = row * kRowBytes + (n / 4 ^ row) * 16 + n % 4 * 4;
+      }
+    }
+    return at;
   }
 
   // The query operand: lane (n, h) holds chunks 2 s + h of query row n.
@@ -83,18 +100,17 @@ struct Tile {
   }
 
   // Scores of the 32 slots whose keys start at LDS address k.
-  static __device__ __forceinline__ f32x16 scores(const char* k, const uint4 (&q)[kQ]) {
-    const int lane = threadIdx.x % 64, n = lane % 32, h = lane / 32;
+  static __device__ __forceinline__ f32x16 scores(const char* k, const LaneAt& at, const uint4 (&q)[kQ]) {
     f32x16 s;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
       if constexpr (kBf16) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + chunk_at(n, 2 * i + h));
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + at.k[i % 4] + i / 4 * 128);
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, q[i]), s, 0, 0, 0);
       } else {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(k + chunk_at(n, 2 * i + h));
+        const f32x4 a = *reinterpret_cast<const f32x4*>(k + at.k[i % 4] + i / 4 * 128);
         const f32x4 b = __builtin_bit_cast(f32x4, q[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], s, 0, 0, 0);
@@ -107,16 +123,12 @@ struct Tile {
   // (block db): lane (m, h) holds column 32 db + m of slots 16 ks + 4 h + 0..3
   // and 16 ks + 8 + 4 h + 0..3.  The transposing read hands lane i of 16 the
   // i-th column of the 4 rows whose 16 columns the lanes' addresses name.
-  static __device__ __forceinline__ bf16x8 value_frag(const char* v, int ks, int db) {
-    const int lane = threadIdx.x % 64, i = lane % 16, h = lane / 32;
-    const int c = 4 * db + 2 * (lane / 16 % 2) + i % 4 / 2;
+  static __device__ __forceinline__ bf16x8 value_frag(const char* v, const LaneAt& at, int ks, int db) {
     s16x4 r[2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int row = 16 * ks + 8 * e + 4 * h + i / 4;
+    for (int e = 0; e < 2; ++e)
       r[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_s16x4*)(v + chunk_at(row, c) + i % 2 * 8));
-    }
+          (lds_s16x4*)(v + at.v[db % 2] + (16 * ks + 8 * e) * kRowBytes + db / 2 * 128));
     union {
       s16x4 s[2];
       bf16x8 b;
@@ -127,11 +139,10 @@ struct Tile {
   }
 
   // acc += P V over the tile's 32 slots; CLEAN: values that are not finite
-  // count as zero (add_odd_values has them).
+  // count as zero.
   template <bool CLEAN>
-  static __device__ __forceinline__ void add_values(const char* v, const f32x16& p,
+  static __device__ __forceinline__ void add_values(const char* v, const LaneAt& at, const f32x16& p,
                                                     f32x16 (&acc)[DP / 32]) {
-    const int lane = threadIdx.x % 64;
     if constexpr (kBf16) {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
@@ -142,11 +153,12 @@ struct Tile {
         for (int e = 0; e < 8; ++e) b[e] = static_cast<__bf16>(p[8 * ks + e]);
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) {
-          bf16x8 a = value_frag(v, ks, db);
+          bf16x8 a = value_frag(v, at, ks, db);
           if constexpr (CLEAN) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               if (!finite(static_cast<float>(a[e]))) a[e] = static_cast<__bf16>(0.f);
+            __builtin_amdgcn_sched_barrier(0);  // rare: few registers rather than speed
           }
           acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc[db], 0, 0, 0);
         }
@@ -154,11 +166,9 @@ struct Tile {
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int row = 8 * (i / 4) + 4 * (lane / 32) + i % 4;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) {
-          const int e = 32 * db + lane % 32;
-          float a = *reinterpret_cast<const float*>(v + chunk_at(row, e / 4) + e % 4 * 4);
+          float a = *reinterpret_cast<const float*>(v + at.v[i % 4] + 8 * (i / 4) * kRowBytes + db * 128);
           if constexpr (CLEAN) a = finite(a) ? a : 0.f;
           acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[i], acc[db], 0, 0, 0);
         }
@@ -166,7 +176,10 @@ struct Tile {
     }
   }
 
-  // Whether any of the 32 rows' values is not finite (uniform over the wave).
+  // Whether any of 32 rows' values is not finite (uniform over the wave).  The
+  // matrix instructions multiply a value with the zero weights of the queries
+  // that do not see it too, so a tile with hidden slots leaves it out, and rows
+  // that see it are computed again (careful_row).
   static __device__ __forceinline__ bool any_odd(const char* v) {
     const int lane = threadIdx.x % 64;
     bool odd = false;
@@ -182,89 +195,120 @@ struct Tile {
     }
     return __any(odd);
   }
+};
 
-  // The products of values that are not finite with the weights of the
-  // queries that see them; a matrix instruction would multiply them with the
-  // zero weights of the others too.  `m2` is the queries' reference of the
-  // exponentials, [lo, hi) what they see, j0 the tile's first slot.  Rare: a
-  // slot at a time, the score formed again.
-  static __device__ __forceinline__ void add_odd_values(const AttnArgs& a, const char* k,
-                                                        const char* v, const uint4 (&q)[kQ],
-                                                        float m2, int lo, int hi, int j0,
-                                                        f32x16 (&acc)[DP / 32]) {
-    const int lane = threadIdx.x % 64, h = lane / 32;
-    constexpr int per = 16 / sizeof(T);
-#pragma unroll 1
-    for (int r = 0; r < 32; ++r) {
-      float x = 0.f;
+// The LDS address of a shared array, as M0 takes it.
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+  return __builtin_amdgcn_readfirstlane(
+      static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char*)(p))));
+}
+
+// Copies 16 bytes per lane from global memory into LDS: lane i's go to
+// lds + 16 i.  Written out, because the compiler would make every LDS read
+// wait for all copies in flight; its own waits for loads only grow by what it
+// does not count.  Nothing else here uses M0.  The base is scalar; the no-ops are the wait states between
+// a write of M0, or of an SGPR by a vector instruction, and its use.
+__device__ __forceinline__ void copy16(const char* from, uint32_t offset, uint32_t lds) {
+  const uint64_t p = reinterpret_cast<uint64_t>(from);
+  const uint64_t base = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p >> 32))) << 32 |
+                        static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p)));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
+               "v"(offset), "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void copy16(const char* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds),
+               "v"(from)
+               : "memory");
+}
+
+// Where the rows of a wave's copies start, of a tile of TK slots that WAVES
+// waves copy: the blocks, read by the scalar unit a tile ahead of their use.
+// One copy instruction moves kRowsPerCopy rows, which lie in one block where
+// runs of 8 slots do.
+template <typename T, int DP, int TK, int WAVES>
+struct Copies {
+  static constexpr int kN = TK * Tile<T, DP>::kRowBytes / 1024 / WAVES;  // keys or values
+  static constexpr int kRows = Tile<T, DP>::kRowsPerCopy;
+  int32_t id[kN];
+};
+
+template <typename T, int DP, int TK, int WAVES>
+__device__ __forceinline__ void fetch_blocks(const CacheArgs& c, int b, int j0, int hi, int w,
+                                             Copies<T, DP, TK, WAVES>& out) {
+  using C = Copies<T, DP, TK, WAVES>;
+  if (!c.table || c.run < 8) return;
+  const __attribute__((address_space(4))) int32_t* t =
+      (const __attribute__((address_space(4))) int32_t*)(c.table) +
+      static_cast<int64_t>(b) * c.max_blocks;
+  if (c.run >= TK) {
+    out.id[0] = t[fdiv(c.bs, min(j0, hi - 1))];
+  } else {
 #pragma unroll
-      for (int i = 0; i < kQ; ++i) {
-        const uint4 y = *reinterpret_cast<const uint4*>(k + chunk_at(r, 2 * i + h));
-        const uint32_t kw[4] = {y.x, y.y, y.z, y.w}, qw[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+    for (int i = 0; i < C::kN; ++i)
+      out.id[i] = t[fdiv(c.bs, min(j0 + (i * WAVES + w) * C::kRows, hi - 1))];
+  }
+}
+
+// Copies rows j0 .. j0 + TK - 1 of a cache (keys at kb, values at vb of one
+// head) into LDS at `lds` and `lds + TK rows`, each wave w of WAVES its share,
+// each lane the chunk that belongs at its place.  Slots outside [lo, hi) are
+// replaced by the nearest inside.
+template <typename T, int DP, int TK, int WAVES>
+__device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, const char* vb, int b,
+                                          int j0, int lo, int hi,
+                                          const Copies<T, DP, TK, WAVES>& blocks, int d, int w,
+                                          uint32_t lds) {
+  using L = Tile<T, DP>;
+  constexpr int kCopies = Copies<T, DP, TK, WAVES>::kN, R = L::kRowsPerCopy;
+  const int lane = threadIdx.x % 64, sub = lane / L::kChunks;
+  const uint32_t st = static_cast<uint32_t>(c.st) * sizeof(T);
+  const bool full = d == DP;
+  auto copies = [&](int i, uint32_t rows, const char* k, const char* v) __attribute__((always_inline)) {
+    // rows: of the tile, by which k and v are short of the instruction's first
+    const int row = (i * WAVES + w) * R + sub;
+    const int chunk = (lane % L::kChunks) ^ (row & L::kSwz);
+    const uint32_t off = (rows + sub) * st + chunk * 16;
+    const uint32_t to = lds + (i * WAVES + w) * 1024;
+    if (full || chunk * 16 < d * static_cast<int>(sizeof(T))) {
+      copy16(k, off, to);
+      copy16(v, off, to + TK * L::kRowBytes);
+    }
+  };
+  const int64_t sb = c.sb * static_cast<int64_t>(sizeof(T));
+  if (j0 >= lo && j0 + TK <= hi && c.run >= TK) {
+    // the whole tile lies in one block
+    const int32_t id = c.table ? blocks.id[0] : b;
+    const uint32_t slot = c.table ? j0 - fdiv(c.bs, j0) * c.bs.d : j0;
+    const int64_t at = id * sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (kBf16)
-            x += __uint_as_float(kw[e] << 16) * __uint_as_float(qw[e] << 16) +
-                 __uint_as_float(kw[e] & 0xffff0000u) * __uint_as_float(qw[e] & 0xffff0000u);
-          else
-            x += __uint_as_float(kw[e]) * __uint_as_float(qw[e]);
-        }
+    for (int i = 0; i < kCopies; ++i) copies(i, (i * WAVES + w) * R, kb + at, vb + at);
+  } else if (j0 >= lo && j0 + TK <= hi && c.run >= 8) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int j = j0 + (i * WAVES + w) * R;
+      const uint32_t slot = j - fdiv(c.bs, j) * c.bs.d;
+      const int64_t at = blocks.id[i] * sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
+      copies(i, 0, kb + at, vb + at);
+    }
+  } else {
+    // lane i finds row i's place
+    const int j = min(max(j0 + lane % TK, lo), hi - 1);
+    const int64_t at = cache_offset(c, cache_block(c, b, j), j) * static_cast<int64_t>(sizeof(T));
+    const uint32_t at_lo = static_cast<uint32_t>(at), at_hi = static_cast<uint32_t>(at >> 32);
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int row = (i * WAVES + w) * R + sub;
+      const int chunk = (lane % L::kChunks) ^ (row & L::kSwz);
+      const int64_t o = static_cast<int64_t>(static_cast<uint64_t>(__shfl(at_hi, row)) << 32 |
+                                             __shfl(at_lo, row)) + chunk * 16;
+      const uint32_t to = lds + (i * WAVES + w) * 1024;
+      if (full || chunk * 16 < d * static_cast<int>(sizeof(T))) {
+        copy16(kb + o, to);
+        copy16(vb + o, to + TK * L::kRowBytes);
       }
-      const float s = score2(a, half_sum(x));
-      // a seen slot's weight is positive, however small
-      const float p = fmaxf(__builtin_amdgcn_exp2f(s - (m2 == -INFINITY ? 0.f : m2)), 1e-30f);
-      const bool sees = j0 + r >= lo && j0 + r < hi;
-#pragma unroll
-      for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int e = 32 * db + 8 * (i / 4) + 4 * h + i % 4;
-          const float y = load_f32<T>(
-              reinterpret_cast<const T*>(v + chunk_at(r, e / per)) + e % per);
-          if (sees && !finite(y)) acc[db][i] += s != s ? s : p * y;
-        }
     }
   }
-};
-
-// Offsets (bytes) of a tile's rows: lane i has row i's.
-struct RowOffset {
-  uint32_t lo, hi;
-};
-
-// The block of a tile's row, one row per lane: slot j, clamped to [lo, hi).
-__device__ __forceinline__ int row_block(const CacheArgs& c, int b, int j, int lo, int hi) {
-  return cache_block(c, b, min(max(j, lo), hi - 1));
-}
-
-template <typename T>
-__device__ __forceinline__ RowOffset row_offset(const CacheArgs& c, int block, int j, int lo,
-                                                int hi) {
-  const int64_t o = cache_offset(c, block, min(max(j, lo), hi - 1)) * static_cast<int64_t>(sizeof(T));
-  return RowOffset{static_cast<uint32_t>(o), static_cast<uint32_t>(static_cast<uint64_t>(o) >> 32)};
-}
-
-// Copies instruction g's rows (g * kRowsPerCopy on) of a tile into LDS at dst:
-// 16 bytes per lane, lane-linear, so the lane picks the chunk that belongs at
-// its place.  UNIFORM: the rows lie in one block, at the cache's row stride.
-template <typename T, int DP, bool UNIFORM>
-__device__ __forceinline__ void copy_rows(const char* base, const RowOffset& off, int g,
-                                          int64_t row_stride, int d, lds_char* dst) {
-  using L = Tile<T, DP>;
-  const int lane = threadIdx.x % 64;
-  const int sub = lane / L::kChunks, row = g * L::kRowsPerCopy + sub;
-  const int c = (lane % L::kChunks) ^ (row & L::kSwz);
-  const char* p;
-  if constexpr (UNIFORM) {
-    const uint32_t lo = __builtin_amdgcn_readlane(off.lo, g * L::kRowsPerCopy);
-    const uint32_t hi = __builtin_amdgcn_readlane(off.hi, g * L::kRowsPerCopy);
-    p = base + (static_cast<uint64_t>(hi) << 32 | lo) + (sub * static_cast<uint32_t>(row_stride) + c * 16);
-  } else {
-    const uint32_t lo = __shfl(off.lo, row), hi = __shfl(off.hi, row);
-    p = base + (static_cast<uint64_t>(hi) << 32 | lo) + c * 16;
-  }
-  if (c * 16 < d * static_cast<int>(sizeof(T)))
-    __builtin_amdgcn_global_load_lds(p, dst + g * 1024, 16, 0, 0);
 }
 
 // Running softmax of a wave's 32 query rows: reference m2 (log2 units; -inf:
@@ -326,6 +370,87 @@ __device__ __forceinline__ void mask_scores(f32x16& s, int j0, int lo, int hi) {
     const int j = j0 + 8 * (v / 4) + 4 * h + v % 4;
     if (static_cast<uint32_t>(j - lo) >= len) s[v] = -INFINITY;
   }
+}
+
+// A tile of 32 slots that not all of the wave's queries see.  Returns whether
+// it holds values that are not finite, which it leaves out.
+template <typename T, int DP, bool CAP>
+__device__ __forceinline__ bool edge_step(const AttnArgs& a, const char* k, const char* v,
+                                          const typename Tile<T, DP>::LaneAt& at,
+                                          const uint4 (&q)[Tile<T, DP>::kQ], int j0, int lo, int hi,
+                                          Softmax& st, f32x16 (&acc)[DP / 32]) {
+  using L = Tile<T, DP>;
+  const bool odd = L::any_odd(v);
+  f32x16 s[1] = {L::scores(k, at, q)};
+  if constexpr (CAP) cap_scores(a, s);
+  mask_scores(s[0], j0, lo, hi);
+  softmax_step(CAP ? 1.f : a.scale2, s, st, acc);
+  if (odd)
+    L::template add_values<true>(v, at, s[0], acc);
+  else
+    L::template add_values<false>(v, at, s[0], acc);
+  return odd;
+}
+
+// What the weights and values of one query row give over a list of tiles of 32
+// slots, one slot at a time: lane e holds columns e, e + 64, .. of the sum.
+// Products with slots that the row does not see are never formed.  `slot(t)`
+// is tile t's first slot.  Returns whether a sum is not finite: then the row
+// sees such a value, and only then is this its result (a row that does not
+// keeps the bits that it has without them).
+template <typename T, int DP, typename Slot>
+__device__ __forceinline__ bool careful_row(const AttnArgs& a, int b, int h, const T* q, int lo,
+                                            int hi, int tiles, Slot slot, Softmax& st,
+                                            float (&o)[DP / 64]) {
+  const int lane = threadIdx.x % 64, n = lane % 32, half = lane / 32;
+  const T* kc = reinterpret_cast<const T*>(a.c.k) + h * a.c.sh;
+  const T* vc = reinterpret_cast<const T*>(a.c.v) + h * a.c.sh;
+  st = Softmax{};
+#pragma unroll
+  for (int i = 0; i < DP / 64; ++i) o[i] = 0.f;
+#pragma unroll 1
+  for (int t = 0; t < tiles; ++t) {
+    const int j = slot(t) + n;
+    const bool sees = j >= lo && j < hi;
+    if (!__any(sees)) continue;
+    const int jc = min(max(j, lo), hi - 1);
+    const int64_t at = cache_offset(a.c, cache_block(a.c, b, jc), jc);
+    float x = 0.f;
+#pragma unroll 1
+    for (int e = half; e < a.d; e += 2) x += load_f32<T>(q + e) * load_f32<T>(kc + at + e);
+    x = half_sum(x);
+    const float s = sees ? score2(a, x) : -INFINITY;
+    float top = s;
+#pragma unroll
+    for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+    const float m = fmaxf(st.m2, top);
+    const float alpha = m == st.m2 ? 1.f : __builtin_amdgcn_exp2f(st.m2 - m);
+    st.m2 = m;
+    // a seen slot's weight is positive, however small
+    float p = __builtin_amdgcn_exp2f(s - (m == -INFINITY ? 0.f : m));
+    if (sees && p == 0.f && s > -INFINITY) p = 1e-30f;
+    float sum = p;
+#pragma unroll
+    for (int i = 16; i; i >>= 1) sum += __shfl_xor(sum, i);
+    st.l = st.l * alpha + sum;
+#pragma unroll
+    for (int i = 0; i < DP / 64; ++i) o[i] *= alpha;
+#pragma unroll 1
+    for (int r = 0; r < 32; ++r) {
+      if (!__shfl(static_cast<int>(sees), r)) continue;
+      const float pr = __shfl(p, r);
+      const int64_t vr = static_cast<int64_t>(
+          static_cast<uint64_t>(__shfl(static_cast<uint32_t>(at >> 32), r)) << 32 |
+          __shfl(static_cast<uint32_t>(at), r));
+#pragma unroll
+      for (int i = 0; i < DP / 64; ++i)
+        if (i * 64 + lane < a.d) o[i] += pr * load_f32<T>(vc + vr + i * 64 + lane);
+    }
+  }
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < DP / 64; ++i) odd |= !finite(o[i]);
+  return __any(odd);
 }
 
 }  // namespace kvx
