@@ -56,8 +56,8 @@ def build(out: str = LIB, verbose: bool = False) -> str:
              ("staged", os.path.join(CSRC, "staged.hip"), [])]
     units += [(name, os.path.join(CSRC, name + ".hip"), [])
               for name in ("attn", "attn_forward", "attn_mass", "attn_evict")]
-    units += [(f"attn_forward_{dp}", os.path.join(CSRC, "attn_forward_d.hip"),
-               [f"-DKVX_ATTN_DP={dp}"]) for dp in (64, 128, 256)]
+    units += [(f"{name}_{dp}", os.path.join(CSRC, name + "_d.hip"), [f"-DKVX_ATTN_DP={dp}"])
+              for name in ("attn_forward", "attn_mass") for dp in (64, 128, 256)]
     for i, name in enumerate(("bf16x2", "bf16", "f16")):
         units.append((f"fused_{name}", os.path.join(CSRC, "fused_launch.hip"),
                       [f"-DKVX_LAUNCH_PREC={i}"]))

@@ -152,6 +152,7 @@ kvx_status validate(const kvx_attn_io* io, const AttnArgs& a, bool reads_cache, 
   for (int64_t b = 0; b < io->batch; ++b) {
     const int32_t m = qs ? qs[b + 1] - qs[b] : 1, n = tok[b];
     if (m < 0 || n < 0 || n > a.c.capacity || (pre && pre[b] < 0)) return KVX_EDATA;
+    if (a.mass && n > a.mass_capacity) return KVX_EDATA;
     if (!tab || m == 0) continue;
     int64_t lo = n - m;
     if (reads_cache) lo = io->window ? lo - io->window + 1 : 0;

@@ -6,32 +6,6 @@
 namespace kvx {
 namespace {
 
-// Query rows of a unit are (new token, head of the group), the group fastest:
-// all heads that share a KV head share its tiles.
-struct QueryRow {
-  int row, g;    // row of the new tokens, head within the group
-  int lo, hi;    // slots that it sees
-};
-
-__device__ __forceinline__ QueryRow query_row(const AttnArgs& a, const Context& c, int r) {
-  QueryRow q;
-  const int i = fdiv(a.by_group, r);
-  q.row = c.q0 + i;
-  q.g = r - i * a.group;
-  const int p = c.n - c.m + i;
-  q.lo = first_seen(a, p);
-  q.hi = r < c.m * a.group ? end_seen(c, p) : 0;
-  return q;
-}
-
-// Slots that query rows r0 .. r1 of a context see together.
-__device__ __forceinline__ void seen_by(const AttnArgs& a, const Context& c, int r0, int r1,
-                                        int& lo, int& hi) {
-  const int p0 = c.n - c.m + fdiv(a.by_group, r0), p1 = c.n - c.m + fdiv(a.by_group, r1);
-  hi = end_seen(c, p1);
-  lo = min(first_seen(a, max(p0, 0)), hi);
-}
-
 // Query rows from r0 on that see nothing: their slots are negative.
 __device__ __forceinline__ int unseeing(const AttnArgs& a, const Context& c, int r0) {
   return max(0, (c.m - c.n) * a.group - r0);
@@ -256,8 +230,8 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
 template <typename T, int DP>
 struct Decode {
   static constexpr int kStage = 2 * 32 * DP * sizeof(T);  // keys and values of 32 slots
-  static constexpr int kWaves = kStage <= 16384 ? 4 : kStage <= 32768 ? 2 : 1;
-  static constexpr int kStages = 131072 / kWaves / kStage;
+  static constexpr int kWaves = ring_waves(kStage);
+  static constexpr int kStages = ring_stages(kStage);
   static constexpr int kStep = kWaves * 32;  // slots of a workgroup's step
 };
 
@@ -280,80 +254,21 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
   constexpr int kBytes = 32 * L::kRowBytes;
   constexpr int kCopies = kBytes / 1024;
   __shared__ __attribute__((aligned(16))) char lds[NW * NST * D::kStage];
-  __shared__ int64_t scan[NW];
-  __shared__ int found[3];
   const int tid = threadIdx.x, lane = tid % 64, n = lane % 32;
   const int w = __builtin_amdgcn_readfirstlane(tid / 64);
   JoinHead* head = fp.heads + blockIdx.x;
 
-  // steps of all contexts' q tiles of one head, and this workgroup's share of
-  // all heads': an equal range of the line (head, context, q tile, step)
-  auto steps_of = [&](int b) __attribute__((always_inline)) {
+  const Share share = line_share<NW>(a, [&](int b) {
     const Context c = context(a, b);
     const int qts = (c.m * a.group + kDecodeRows - 1) / kDecodeRows;
     int64_t s = 0;
     for (int qt = 0; qt < qts; ++qt) s += decode_steps<D::kStep>(a, c, qt);
     return s;
-  };
-  // sum over the workgroup's threads before this one, and over all
-  auto block_sum = [&](int64_t x, int64_t& total) __attribute__((always_inline)) {
-    int64_t s = x;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const int64_t y = __shfl_up(s, i);
-      if (lane >= i) s += y;
-    }
-    __syncthreads();
-    if (lane == 63) scan[w] = s;
-    __syncthreads();
-    int64_t base = 0;
-    total = 0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      if (i < w) base += scan[i];
-      total += scan[i];
-    }
-    return base + s - x;
-  };
-  int64_t line = 0;  // of one head
-  int64_t mine = 0, mine_before = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += NT) {
-    int64_t total;
-    mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
-    mine_before = block_sum(mine, total);
-    line += total;
-  }
-  const int64_t whole = line * a.hkv;
-  const int64_t per = (whole + gridDim.x - 1) / gridDim.x;
-  const int64_t s0 = blockIdx.x * per, s1 = min(whole, s0 + per);
+  });
   if (tid == 0) head->pieces = 0;
+  const int64_t s0 = share.s0, s1 = share.s1, per = share.per;
   if (s0 >= s1) return;
-  int h = static_cast<int>(s0 / line);
-  // the context that holds the first step
-  const int64_t into = s0 - h * line;
-  if (a.batch <= NT) {
-    if (mine_before <= into && into < mine_before + mine) {
-      found[0] = tid;
-      found[1] = static_cast<int>(into - mine_before);
-    }
-    __syncthreads();
-  } else {
-    int64_t before = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += NT) {
-      int64_t total;
-      mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
-      mine_before = before + block_sum(mine, total);
-      if (mine_before <= into && into < mine_before + mine) {
-        found[0] = b0 + tid;
-        found[1] = static_cast<int>(into - mine_before);
-      }
-      before += total;
-      if (before > into) break;
-    }
-    __syncthreads();
-  }
-  int b = __builtin_amdgcn_readfirstlane(found[0]);
-  int step = __builtin_amdgcn_readfirstlane(found[1]);
+  int h = share.h, b = share.b, step = share.step;
   Context c = context(a, b);
   int qt = 0;
   for (int x; step >= (x = decode_steps<D::kStep>(a, c, qt)); ++qt) step -= x;

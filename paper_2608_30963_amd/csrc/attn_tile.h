@@ -99,7 +99,10 @@ struct Tile {
     }
   }
 
-  // Scores of the 32 slots whose keys start at LDS address k.
+  // Products of the 32 rows at LDS address k with the lanes' row pieces q:
+  // lane (n, h) gets its row n's with rows 8 (v / 4) + 4 h + v % 4.  SWAP: its
+  // LDS row n's with the pieces' rows.
+  template <bool SWAP = false>
   static __device__ __forceinline__ f32x16 scores(const char* k, const LaneAt& at, const uint4 (&q)[kQ]) {
     f32x16 s;
 #pragma unroll
@@ -108,12 +111,14 @@ struct Tile {
     for (int i = 0; i < kQ; ++i) {
       if constexpr (kBf16) {
         const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + at.k[i % 4] + i / 4 * 128);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, q[i]), s, 0, 0, 0);
+        const bf16x8 b = __builtin_bit_cast(bf16x8, q[i]);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(SWAP ? b : a, SWAP ? a : b, s, 0, 0, 0);
       } else {
         const f32x4 a = *reinterpret_cast<const f32x4*>(k + at.k[i % 4] + i / 4 * 128);
         const f32x4 b = __builtin_bit_cast(f32x4, q[i]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], s, 0, 0, 0);
+        for (int e = 0; e < 4; ++e)
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(SWAP ? b[e] : a[e], SWAP ? a[e] : b[e], s, 0, 0, 0);
       }
     }
     return s;
@@ -212,13 +217,19 @@ __device__ __forceinline__ void copy16(const char* from, uint32_t offset, uint32
   const uint64_t p = reinterpret_cast<uint64_t>(from);
   const uint64_t base = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p >> 32))) << 32 |
                         static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p)));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds),
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
                "v"(offset), "s"(base)
                : "memory");
 }
 __device__ __forceinline__ void copy16(const char* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds),
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
                "v"(from)
+               : "memory");
+}
+
+// 4 bytes per lane, lane i's to lds + 4 i.
+__device__ __forceinline__ void copy4(const char* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from)
                : "memory");
 }
 
@@ -251,10 +262,10 @@ __device__ __forceinline__ void fetch_blocks(const CacheArgs& c, int b, int j0, 
 }
 
 // Copies rows j0 .. j0 + TK - 1 of a cache (keys at kb, values at vb of one
-// head) into LDS at `lds` and `lds + TK rows`, each wave w of WAVES its share,
+// head, unless VALUES is false) into LDS at `lds` and `lds + TK rows`, each wave w of WAVES its share,
 // each lane the chunk that belongs at its place.  Slots outside [lo, hi) are
 // replaced by the nearest inside.
-template <typename T, int DP, int TK, int WAVES>
+template <typename T, int DP, int TK, int WAVES, bool VALUES = true>
 __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, const char* vb, int b,
                                           int j0, int lo, int hi,
                                           const Copies<T, DP, TK, WAVES>& blocks, int d, int w,
@@ -272,7 +283,7 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
     const uint32_t to = lds + (i * WAVES + w) * 1024;
     if (full || chunk * 16 < d * static_cast<int>(sizeof(T))) {
       copy16(k, off, to);
-      copy16(v, off, to + TK * L::kRowBytes);
+      if constexpr (VALUES) copy16(v, off, to + TK * L::kRowBytes);
     }
   };
   const int64_t sb = c.sb * static_cast<int64_t>(sizeof(T));
@@ -305,10 +316,118 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
       const uint32_t to = lds + (i * WAVES + w) * 1024;
       if (full || chunk * 16 < d * static_cast<int>(sizeof(T))) {
         copy16(kb + o, to);
-        copy16(vb + o, to + TK * L::kRowBytes);
+        if constexpr (VALUES) copy16(vb + o, to + TK * L::kRowBytes);
       }
     }
   }
+}
+
+// Query rows of a KV head's unit are (new token, head of the group), the group
+// fastest: all heads that share a KV head share its tiles.
+struct QueryRow {
+  int row, g;  // row of the new tokens, head within the group
+  int lo, hi;  // slots that it sees; empty past the context's last row
+};
+
+__device__ __forceinline__ QueryRow query_row(const AttnArgs& a, const Context& c, int r) {
+  QueryRow q;
+  const int i = fdiv(a.by_group, r);
+  q.row = c.q0 + i;
+  q.g = r - i * a.group;
+  const int p = c.n - c.m + i;
+  q.lo = first_seen(a, p);
+  q.hi = r < c.m * a.group ? end_seen(c, p) : 0;
+  return q;
+}
+
+// Slots that query rows r0 .. r1 of a context see together.
+__device__ __forceinline__ void seen_by(const AttnArgs& a, const Context& c, int r0, int r1,
+                                        int& lo, int& hi) {
+  const int p0 = c.n - c.m + fdiv(a.by_group, r0), p1 = c.n - c.m + fdiv(a.by_group, r1);
+  hi = end_seen(c, p1);
+  lo = min(first_seen(a, max(p0, 0)), hi);
+}
+
+// A workgroup's equal range of the line (KV head, context, step), where context
+// b has steps_of(b) steps.
+struct Share {
+  int64_t s0, s1;  // of the line; empty: nothing to do
+  int64_t per;     // length of every workgroup's range
+  int h, b, step;  // where s0 lies
+};
+
+// Found by all NW waves together; every thread of the workgroup calls it.
+template <int NW, typename Steps>
+__device__ __forceinline__ Share line_share(const AttnArgs& a, Steps steps_of) {
+  constexpr int NT = 64 * NW;
+  __shared__ int64_t scan[NW];
+  __shared__ int found[2];
+  const int tid = threadIdx.x, lane = tid % 64, w = tid / 64;
+  auto before_of = [&](int64_t x, int64_t& total) __attribute__((always_inline)) {
+    int64_t s = x;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+      const int64_t y = __shfl_up(s, i);
+      if (lane >= i) s += y;
+    }
+    __syncthreads();
+    if (lane == 63) scan[w] = s;
+    __syncthreads();
+    int64_t base = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      if (i < w) base += scan[i];
+      total += scan[i];
+    }
+    return base + s - x;
+  };
+  int64_t line = 0, mine = 0, before = 0;  // line: of one head
+  for (int b0 = 0; b0 < a.batch; b0 += NT) {
+    int64_t total;
+    mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
+    before = before_of(mine, total);
+    line += total;
+  }
+  Share sh{};
+  const int64_t whole = line * a.hkv;
+  sh.per = (whole + gridDim.x - 1) / gridDim.x;
+  sh.s0 = min<int64_t>(whole, blockIdx.x * sh.per);
+  sh.s1 = min(whole, sh.s0 + sh.per);
+  if (sh.s0 >= sh.s1) return sh;
+  sh.h = static_cast<int>(sh.s0 / line);
+  const int64_t into = sh.s0 - sh.h * line;
+  if (a.batch <= NT) {
+    if (before <= into && into < before + mine) {
+      found[0] = tid;
+      found[1] = static_cast<int>(into - before);
+    }
+  } else {
+    int64_t past = 0;
+    for (int b0 = 0; b0 < a.batch && past <= into; b0 += NT) {
+      int64_t total;
+      mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
+      before = past + before_of(mine, total);
+      if (before <= into && into < before + mine) {
+        found[0] = b0 + tid;
+        found[1] = static_cast<int>(into - before);
+      }
+      past += total;
+    }
+  }
+  __syncthreads();
+  sh.b = __builtin_amdgcn_readfirstlane(found[0]);
+  sh.step = __builtin_amdgcn_readfirstlane(found[1]);
+  sh.h = __builtin_amdgcn_readfirstlane(sh.h);
+  return sh;
+}
+
+// Waves and stages of the rings of 32-slot tiles that a workgroup holds in LDS
+// for single tokens, `stage` bytes a tile.
+constexpr int ring_waves(int stage) { return stage <= 16384 ? 4 : stage <= 32768 ? 2 : 1; }
+constexpr int ring_stages(int stage) {
+  const int n = 131072 / ring_waves(stage) / stage;
+  return n < 4 ? n : 4;
 }
 
 // Running softmax of a wave's 32 query rows: reference m2 (log2 units; -inf:
