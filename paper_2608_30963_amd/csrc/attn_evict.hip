@@ -1,5 +1,7 @@
 // attn_evict.hip -- keep the cached tokens of the largest weight
 // (kvx_attn_evict): a selection per (layer, context, KV head), then the rows.
+#include <algorithm>
+
 #include "attn.h"
 
 namespace kvx {
@@ -38,15 +40,19 @@ __device__ __forceinline__ int block_scan(int x, int* sh, int& total) {
   return base + s - x;
 }
 
+constexpr int kBins = 2048;
+
 // One workgroup per (layer, context, KV head).  The key of the last kept slot
-// is found by a radix search over the keys' bits, 8 at a time from the top
-// (counts of the keys that share the prefix found so far); slots above it are
-// kept, of those equal to it the first ones, and a scan in slot order writes
-// the kept slots in rising order.
+// is found by a radix search over the keys' bits, 11, 11 and 10 at a time from
+// the top (counts of the keys that share the prefix found so far); slots above
+// it are kept, of those equal to it the first ones, and a scan in slot order
+// writes the kept slots in rising order.  11 bits: the first hold sign,
+// exponent and two bits of the number, so that counts of like weights fall on
+// more than a few counters.
 __global__ void __launch_bounds__(kSelThreads) evict_select(EvictArgs a) {
-  __shared__ int count[256];
+  __shared__ int count[kBins];
   __shared__ int scan[kSelThreads / 64];
-  __shared__ uint32_t found[2];  // prefix, rank left within it
+  __shared__ int found[3];  // digit, rank left within it, its count
   const int set = blockIdx.x, tid = threadIdx.x;
   const int b = set / a.heads % a.batch;
   const int n = min(min(max(a.tokens[b], 0), a.src.capacity), a.mass_capacity);
@@ -57,49 +63,60 @@ __global__ void __launch_bounds__(kSelThreads) evict_select(EvictArgs a) {
   float* wo = a.mass_out ? a.mass_out + static_cast<int64_t>(set) * a.mass_capacity : nullptr;
   int32_t* kept = a.kept + static_cast<int64_t>(set) * a.keep;
   const int first = min(a.sink, n), last = max(first, n - a.recent);
-  int middle = keep - first - (n - last);  // slots to pick from [first, last)
+  const int middle = keep - first - (n - last);  // slots to pick from [first, last)
   const bool all = keep == n;
   uint32_t key = 0;
-  int equal = 0;  // of the keys equal to `key`, how many are kept
+  int equal = 0;      // of the keys equal to `key`, how many are kept
+  bool some = false;  // and whether not all are
   if (!all && middle > 0) {
-    uint32_t prefix = 0, mask = 0;
+    uint32_t mask = 0;
     int rank = middle;  // looking for the rank-th largest
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kSelThreads) count[i] = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int bits = pass < 2 ? 11 : 10, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      for (int i = tid; i < kBins; i += kSelThreads) count[i] = 0;
       __syncthreads();
       for (int j = first + tid; j < last; j += kSelThreads) {
         const uint32_t k = order_key(w[j]);
-        if ((k & mask) == prefix) atomicAdd(&count[k >> shift & 255], 1);
+        if ((k & mask) == key) atomicAdd(&count[k >> shift & ((1u << bits) - 1)], 1);
       }
       __syncthreads();
-      if (tid == 0) {
-        int d = 255, r = rank;
-        while (d > 0 && count[d] < r) r -= count[d--];
-        found[0] = prefix | static_cast<uint32_t>(d) << shift;
-        found[1] = r;
+      // thread t: counters 2t' and 2t' + 1 from the top, t' = kSelThreads - 1 - t
+      const int d = kBins - 2 - 2 * tid;
+      const int hi = count[d + 1], lo = count[d];
+      int total;
+      const int above = block_scan(hi + lo, scan, total);
+      if (above < rank && rank <= above + hi + lo) {
+        const bool upper = rank <= above + hi;
+        found[0] = upper ? d + 1 : d;
+        found[1] = rank - above - (upper ? 0 : hi);
+        found[2] = upper ? hi : lo;
       }
       __syncthreads();
-      prefix = found[0];
+      key |= static_cast<uint32_t>(found[0]) << shift;
       rank = found[1];
-      mask |= 255u << shift;
+      some = rank < found[2];
+      mask |= ((1u << bits) - 1) << shift;
+      __syncthreads();
     }
-    key = prefix;
     equal = rank;
   }
   int done = 0, ties = 0;
   for (int j0 = 0; j0 < n; j0 += kSelThreads) {
     const int j = j0 + tid;
     const float x = j < n ? w[j] : 0.f;
-    int total, tie = 0;
-    bool keep_j = j < n;
+    int total;
+    bool keep_j = j < n, tie = false;
     if (!all && j >= first && j < last) {
       const uint32_t k = order_key(x);
-      tie = middle > 0 && k == key;
-      keep_j = middle > 0 && k > key;
+      tie = some && k == key;
+      keep_j = middle > 0 && (k > key || (k == key && !some));
     }
-    const int before = block_scan(tie, scan, total);
-    if (tie) keep_j = ties + before < equal;
-    ties += total;
+    if (some) {
+      const int before = block_scan(tie, scan, total);
+      if (tie) keep_j = ties + before < equal;
+      ties += total;
+    }
     const int at = done + block_scan(keep_j, scan, total);
     if (keep_j) {
       kept[at] = j;
@@ -115,36 +132,49 @@ __global__ void __launch_bounds__(kSelThreads) evict_select(EvictArgs a) {
   }
 }
 
-constexpr int kMoveThreads = 256;
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
 
-// One workgroup per (layer, context, KV head, K|V): kept rows in steps, each
-// step's rows all read before any is written.  In place that is safe for every
-// later step too: kept slots rise, so row i comes from slot >= i.
-__global__ void __launch_bounds__(kMoveThreads) evict_move(EvictArgs a) {
+constexpr int kMoveThreads = 256;
+constexpr int kMoveUnroll = 8;  // 16-byte pieces of a thread in flight
+
+// A workgroup per (layer, context, KV head), K|V and part of the rows' pieces
+// (in place) or of the rows (elsewhere).  Steps of 256 x 8 pieces, all read
+// before any is written.  In place that is safe for every later step too: kept
+// slots rise, so row i comes from slot >= i.
+__global__ void __launch_bounds__(kMoveThreads) evict_move(EvictArgs a, int log_pieces, int rows) {
   const int set = blockIdx.x, v = blockIdx.y, tid = threadIdx.x;
   const int h = set % a.heads, b = set / a.heads % a.batch, l = set / a.heads / a.batch;
   const int n = min(min(max(a.tokens[b], 0), a.src.capacity), a.mass_capacity);
   const int keep = min(min(n, a.keep), a.dst.capacity);
   const int32_t* kept = a.kept + static_cast<int64_t>(set) * a.keep;
-  const int pieces = a.row_bytes / 16;
-  const char* src = v ? a.src.v : a.src.k;
-  char* dst = v ? a.dst.v : a.dst.k;
-  const int64_t total = static_cast<int64_t>(keep) * pieces;
-  for (int64_t i0 = 0; i0 < total; i0 += kMoveThreads) {
-    const int64_t i = i0 + tid;
-    const bool on = i < total;
-    uint4 x{};
-    const int r = static_cast<int>(i / pieces), p = static_cast<int>(i % pieces);
-    if (on) {
-      const int j = kept[r];
-      const int64_t o = l * a.src.sl + h * a.src.sh + cache_offset(a.src, cache_block(a.src, b, j), j);
-      x = *reinterpret_cast<const uint4*>(src + o + p * 16);
+  const int pieces = 1 << log_pieces;
+  const int per = a.row_bytes / 16 >> log_pieces;  // parts that a row is in
+  const int p0 = blockIdx.z % per * pieces;
+  const int r_first = blockIdx.z / per * rows;
+  const int r_end = min(keep, a.in_place ? keep : r_first + rows);
+  // the pointers by value: chosen by address they would be kept in memory
+  const char *sk = a.src.k, *sv = a.src.v;
+  char *dk = a.dst.k, *dv = a.dst.v;
+  const char* src = (v ? sv : sk) + l * a.src.sl + h * a.src.sh;
+  char* dst = (v ? dv : dk) + l * a.dst.sl + h * a.dst.sh;
+  const int step = kMoveThreads * kMoveUnroll >> log_pieces;  // rows
+  for (int r0 = r_first; r0 < r_end; r0 += step) {
+    u32x4 x[kMoveUnroll];
+    int64_t to[kMoveUnroll];
+    bool on[kMoveUnroll];
+#pragma unroll
+    for (int u = 0; u < kMoveUnroll; ++u) {
+      // past the end: the last row again, not stored
+      const int i = u * kMoveThreads + tid, p = (p0 + (i & (pieces - 1))) * 16;
+      const int r = min(r0 + (i >> log_pieces), r_end - 1), j = kept[r];
+      on[u] = r0 + (i >> log_pieces) < r_end && !(a.in_place && j == r);
+      to[u] = cache_offset(a.dst, cache_block(a.dst, b, r), r) + p;
+      x[u] = *reinterpret_cast<const u32x4*>(src + cache_offset(a.src, cache_block(a.src, b, j), j) + p);
     }
-    __syncthreads();
-    if (on) {
-      const int64_t o = l * a.dst.sl + h * a.dst.sh + cache_offset(a.dst, cache_block(a.dst, b, r), r);
-      *reinterpret_cast<uint4*>(dst + o + p * 16) = x;
-    }
+    if (a.in_place) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kMoveUnroll; ++u)
+      if (on[u]) *reinterpret_cast<u32x4*>(dst + to[u]) = x[u];
   }
 }
 
@@ -167,7 +197,20 @@ hipError_t launch_evict(const kvx_attn* at, const EvictArgs& args, hipStream_t s
   const int sets = a.layers * a.batch * a.heads;
   const hipError_t e = launch_on(evict_select, dim3(sets), dim3(kSelThreads), st, a);
   if (e != hipSuccess) return e;
-  return launch_on(evict_move, dim3(sets, 2), dim3(kMoveThreads), st, a);
+  // pieces of a workgroup: a power of two that divides a row's, of at least 128
+  // bytes (a memory line)
+  const int whole = a.row_bytes / 16;
+  int pieces = whole & -whole, rows = a.keep, parts;
+  if (a.in_place) {
+    pieces = std::min(pieces, 8);
+    parts = whole / pieces;
+  } else {
+    pieces = std::min(pieces, 64);
+    rows = kMoveThreads * kMoveUnroll / pieces;
+    parts = whole / pieces * ((a.keep + rows - 1) / rows);
+  }
+  if (parts > 65535) return hipErrorInvalidValue;
+  return launch_on(evict_move, dim3(sets, 2, parts), dim3(kMoveThreads), st, a, __builtin_ctz(pieces), rows);
 }
 
 }  // namespace kvx

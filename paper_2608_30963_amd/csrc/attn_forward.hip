@@ -31,6 +31,7 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
   if (p.decode) {
     p.grid = at->n_cu;
     p.splits = 1;
+    // a context with more new tokens than it was said to have fills its units
     p.join_rows = kDecodeRows;
   } else {
     const int64_t strips = (int64_t(a.rows) * at->group + kChunkRows - 1) / kChunkRows +

@@ -445,42 +445,55 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
   }
 }
 
-// Joins the pieces of units in their order: one wave a query row.
+// Joins the pieces of units: a workgroup per query row, wave w the pieces w,
+// w + 4, .., whose sums are then added in the waves' order.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) forward_join(AttnArgs a, ForwardPlan fp) {
+  constexpr int PER = DP / 64;
+  __shared__ float sums[4][DP];
+  __shared__ float part_l[4];
   const JoinHead hd = fp.heads[blockIdx.x];
-  const int r = blockIdx.y * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
-  if (hd.pieces == 0 || r >= hd.rows) return;
+  const int r = blockIdx.y, lane = threadIdx.x % 64, w = threadIdx.x / 64;
+  if (r >= hd.rows || hd.pieces == 0) return;
   const int unit_rows = fp.decode ? kDecodeRows : kChunkRows;
   const size_t size = piece_floats(unit_rows, DP);
-  constexpr int PER = DP / 64;
-  float m2 = -INFINITY, l = 0.f, o[PER];
+  // decode: piece 0 is slot 1 of its workgroup, the others slot 0 of the next ones
+  auto piece = [&](int p) __attribute__((always_inline)) {
+    const size_t at = fp.decode ? (p == 0 ? hd.first : hd.first - 1 + 2 * static_cast<size_t>(p)) : hd.first + p;
+    return fp.pieces + at * size;
+  };
+  float m2 = -INFINITY;
+  for (int p = lane; p < hd.pieces; p += 64) m2 = fmaxf(m2, reinterpret_cast<const float2*>(piece(p))[r].x);
+#pragma unroll
+  for (int i = 32; i; i >>= 1) m2 = fmaxf(m2, __shfl_xor(m2, i));
+  float l = 0.f, o[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[i] = 0.f;
-  for (int p = 0; p < hd.pieces; ++p) {
-    // decode: piece 0 is slot 1 of its workgroup, the others slot 0 of the next ones
-    const size_t at = fp.decode ? (p == 0 ? hd.first : hd.first - 1 + 2 * static_cast<size_t>(p)) : hd.first + p;
-    const float* part = fp.pieces + at * size;
+#pragma unroll 8
+  for (int p = w; p < hd.pieces; p += 4) {
+    const float* part = piece(p);
     const float2 ml = reinterpret_cast<const float2*>(part)[r];
     const float* x = part + 2 * unit_rows + static_cast<size_t>(r) * DP + lane * PER;
-    const float m = fmaxf(m2, ml.x);
-    const float f0 = m2 == m ? 1.f : __builtin_amdgcn_exp2f(m2 - m);
-    const float f1 = ml.x == m ? 1.f : __builtin_amdgcn_exp2f(ml.x - m);
-    m2 = m;
-    l = l * f0 + ml.y * f1;
+    const float f = ml.x == m2 ? 1.f : __builtin_amdgcn_exp2f(ml.x - m2);
+    l += f * ml.y;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) o[i] = o[i] * f0 + x[i] * f1;
+    for (int i = 0; i < PER; ++i) o[i] += f * x[i];
   }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) sums[w][lane * PER + i] = o[i];
+  if (lane == 0) part_l[w] = l;
+  __syncthreads();
   const int rr = hd.g0 + r, tok = fdiv(a.by_group, rr), g = rr - tok * a.group;
   const int64_t row = hd.row0 + tok;
   const int head = hd.h * a.group + g;
   const bool sees = r >= hd.empty;
-  T* to = reinterpret_cast<T*>(a.out) + row * a.o_sr + head * a.o_sh + lane * PER;
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (lane * PER + i < a.d) to[i] = store_cvt<T>(sees ? o[i] / l : 0.f);
-  if (a.lse && lane == 0)
-    a.lse[row * a.hq + head] = sees ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  const float all = (part_l[0] + part_l[1]) + (part_l[2] + part_l[3]);
+  const int e = threadIdx.x;
+  if (e < a.d) {
+    const float x = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+    (reinterpret_cast<T*>(a.out) + row * a.o_sr + head * a.o_sh)[e] = store_cvt<T>(sees ? x / all : 0.f);
+  }
+  if (a.lse && e == 0) a.lse[row * a.hq + head] = sees ? (m2 + __builtin_amdgcn_logf(all)) * kLn2 : -INFINITY;
 }
 
 }  // namespace
@@ -500,7 +513,7 @@ hipError_t run_forward(const AttnArgs& a, const ForwardPlan& p, hipStream_t st) 
   }
   if (e != hipSuccess) return e;
   const int units = p.decode ? p.grid : p.strips * a.hkv;
-  return launch_on(forward_join<T, DP>, dim3(units, (p.join_rows + 3) / 4), dim3(256), st, a, p);
+  return launch_on(forward_join<T, DP>, dim3(units, p.join_rows), dim3(256), st, a, p);
 }
 
 template hipError_t run_forward<float, KVX_ATTN_DP>(const AttnArgs&, const ForwardPlan&, hipStream_t);
