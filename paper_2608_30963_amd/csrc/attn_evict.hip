@@ -41,6 +41,42 @@ __device__ __forceinline__ int block_scan(int x, int* sh, int& total) {
 }
 
 constexpr int kBins = 2048;
+constexpr int kHeld = 8;                           // weights of a thread in registers
+constexpr int kChunk = kHeld * kSelThreads;        // slots of the workgroup's
+constexpr int kWaves = kSelThreads / 64;
+
+// Positions in slot order of the slots that are on, where slot u * 1024 + t of
+// a chunk is thread t's bit u: counts of every wave and u, then their sums
+// before it; only the first `rounds` u have any.  `count` is the caller's for this use alone.  Returns the number
+// of slots on.
+__device__ __forceinline__ int chunk_scan(uint32_t on, int rounds, int* count, int (&at)[kHeld]) {
+  const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
+  if (lane >= rounds && lane < kHeld) count[lane * kWaves + w] = 0;
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    if (u >= rounds) continue;
+    const uint64_t m = __ballot(on >> u & 1);
+    at[u] = __popcll(m & ((1ull << lane) - 1));
+    if (lane == 0) count[u * kWaves + w] = __popcll(m);
+  }
+  __syncthreads();
+  static_assert(kHeld * kWaves == 128, "two counts a lane");
+  const int c0 = count[2 * lane], c1 = count[2 * lane + 1];
+  int s = c0 + c1;
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) {
+    const int y = __shfl_up(s, i);
+    if (lane >= i) s += y;
+  }
+  const int before = s - c0 - c1;
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    if (u >= rounds) continue;
+    const int i = u * kWaves + w;
+    at[u] += __shfl(before, i / 2) + (i % 2 ? __shfl(c0, i / 2) : 0);
+  }
+  return __shfl(s, 63);
+}
 
 // One workgroup per (layer, context, KV head).  The key of the last kept slot
 // is found by a radix search over the keys' bits, 11, 11 and 10 at a time from
@@ -48,10 +84,12 @@ constexpr int kBins = 2048;
 // it are kept, of those equal to it the first ones, and a scan in slot order
 // writes the kept slots in rising order.  11 bits: the first hold sign,
 // exponent and two bits of the number, so that counts of like weights fall on
-// more than a few counters.
-__global__ void __launch_bounds__(kSelThreads) evict_select(EvictArgs a) {
+// more than a few counters.  Up to 8192 slots the weights are read once and
+// stay in registers; longer contexts are read again for each of the steps.
+__global__ void __launch_bounds__(kSelThreads, 8) evict_select(EvictArgs a) {
   __shared__ int count[kBins];
-  __shared__ int scan[kSelThreads / 64];
+  __shared__ int counts[2][128];
+  __shared__ int scan[kWaves];
   __shared__ int found[3];  // digit, rank left within it, its count
   const int set = blockIdx.x, tid = threadIdx.x;
   const int b = set / a.heads % a.batch;
@@ -64,11 +102,22 @@ __global__ void __launch_bounds__(kSelThreads) evict_select(EvictArgs a) {
   int32_t* kept = a.kept + static_cast<int64_t>(set) * a.keep;
   const int first = min(a.sink, n), last = max(first, n - a.recent);
   const int middle = keep - first - (n - last);  // slots to pick from [first, last)
-  const bool all = keep == n;
+  const bool all = keep == n, search = !all && middle > 0;
+  const int chunks = (n + kChunk - 1) / kChunk;
+  const int rounds = min(kHeld, (n + kSelThreads - 1) / kSelThreads);  // of a chunk
+  float x[kHeld];
+  auto load = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+      const int j = c * kChunk + u * kSelThreads + tid;
+      x[u] = j < n ? w[j] : 0.f;
+    }
+  };
+  if (chunks == 1) load(0);
   uint32_t key = 0;
   int equal = 0;      // of the keys equal to `key`, how many are kept
   bool some = false;  // and whether not all are
-  if (!all && middle > 0) {
+  if (search) {
     uint32_t mask = 0;
     int rank = middle;  // looking for the rank-th largest
 #pragma unroll 1
@@ -76,12 +125,19 @@ __global__ void __launch_bounds__(kSelThreads) evict_select(EvictArgs a) {
       const int bits = pass < 2 ? 11 : 10, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       for (int i = tid; i < kBins; i += kSelThreads) count[i] = 0;
       __syncthreads();
-      for (int j = first + tid; j < last; j += kSelThreads) {
-        const uint32_t k = order_key(w[j]);
-        if ((k & mask) == key) atomicAdd(&count[k >> shift & ((1u << bits) - 1)], 1);
+      for (int c = 0; c < chunks; ++c) {
+        if (chunks > 1) load(c);
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+          if (u >= rounds) continue;
+          const int j = c * kChunk + u * kSelThreads + tid;
+          const uint32_t k = order_key(x[u]);
+          if (j >= first && j < last && (k & mask) == key)
+            atomicAdd(&count[k >> shift & ((1u << bits) - 1)], 1);
+        }
       }
       __syncthreads();
-      // thread t: counters 2t' and 2t' + 1 from the top, t' = kSelThreads - 1 - t
+      // thread t: two counters from the top
       const int d = kBins - 2 - 2 * tid;
       const int hi = count[d + 1], lo = count[d];
       int total;
@@ -97,39 +153,45 @@ __global__ void __launch_bounds__(kSelThreads) evict_select(EvictArgs a) {
       rank = found[1];
       some = rank < found[2];
       mask |= ((1u << bits) - 1) << shift;
-      __syncthreads();
     }
     equal = rank;
   }
   int done = 0, ties = 0;
-  for (int j0 = 0; j0 < n; j0 += kSelThreads) {
-    const int j = j0 + tid;
-    const float x = j < n ? w[j] : 0.f;
-    int total;
-    bool keep_j = j < n, tie = false;
-    if (!all && j >= first && j < last) {
-      const uint32_t k = order_key(x);
-      tie = some && k == key;
-      keep_j = middle > 0 && (k > key || (k == key && !some));
+  for (int c = 0; c < chunks; ++c) {
+    if (chunks > 1) load(c);
+    uint32_t on = 0, tie = 0;
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+      if (u >= rounds) continue;
+      const int j = c * kChunk + u * kSelThreads + tid;
+      const uint32_t k = order_key(x[u]);
+      const bool picked = j >= first && j < last && !all;
+      const bool same = k == key;
+      if (picked ? search && (k > key || (same && !some)) : j < n) on |= 1u << u;
+      if (picked && some && same) tie |= 1u << u;
     }
+    int at[kHeld];
     if (some) {
-      const int before = block_scan(tie, scan, total);
-      if (tie) keep_j = ties + before < equal;
+      const int total = chunk_scan(tie, rounds, counts[0], at);
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u)
+        if ((tie >> u & 1) && ties + at[u] < equal) on |= 1u << u;
       ties += total;
     }
-    const int at = done + block_scan(keep_j, scan, total);
-    if (keep_j) {
-      kept[at] = j;
-      // in place: slots up to j have all been read, a barrier ago
-      if (wo) wo[at] = x;
-    }
+    const int total = chunk_scan(on, rounds, counts[1], at);
+    // in place: this chunk's weights have all been read, a barrier ago
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u)
+      if (on >> u & 1) {
+        kept[done + at[u]] = c * kChunk + u * kSelThreads + tid;
+        if (wo) wo[done + at[u]] = x[u];
+      }
     done += total;
+    __syncthreads();  // the counts' next use
   }
   for (int i = keep + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
-  if (wo) {
-    __syncthreads();
+  if (wo)
     for (int i = keep + tid; i < min(a.mass_capacity, max(a.keep, n)); i += kSelThreads) wo[i] = 0.f;
-  }
 }
 
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
