@@ -142,36 +142,65 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     copy_tile<T, DP, TK, 4>(a.c, kb, vb, b, t0 * TK, lo, hi, blocks, a.d, w, l3);
     fetch_blocks(a.c, b, t0 * TK + TK, hi, w, blocks);
   }
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    // the tile has landed, and every wave is done with the other buffer
+  // Three loops, so that the one that matters has few registers to keep: tiles
+  // before the first that all of the wave's queries see (windows), tiles that
+  // all see, and the rest.  In the middle one the reference stays what the
+  // first of its tiles gives; should a score ever pass it by 2^kRoom, the last
+  // loop goes on, which moves it.
+  const float c2 = CAP ? 1.f : a.scale2;
+  auto arrive = [&](int t) __attribute__((always_inline)) {
+    // tile t has landed, and every wave is done with the other buffer
     vm_wait<0>();
     tile_barrier();
-    const int j0 = t * TK;
     if (t + 1 < t1) {
-      copy_tile<T, DP, TK, 4>(a.c, kb, vb, b, j0 + TK, lo, hi, blocks, a.d, w, l3 + (buf ^ 1) * 2 * kBytes);
-      fetch_blocks(a.c, b, j0 + 2 * TK, hi, w, blocks);
+      copy_tile<T, DP, TK, 4>(a.c, kb, vb, b, t * TK + TK, lo, hi, blocks, a.d, w,
+                              l3 + ((t + 1 - t0) & 1) * 2 * kBytes);
+      fetch_blocks(a.c, b, t * TK + 2 * TK, hi, w, blocks);
     }
-    if (j0 >= whi || j0 + TK <= wlo) continue;
-    const char* k = lds + buf * 2 * kBytes;
-    const char* v = k + kBytes;
-    if (j0 >= alo && j0 + TK <= ahi) {
-      f32x16 s[NS];
+  };
+  auto edges = [&](int t) __attribute__((always_inline)) {
+    if (t * TK >= whi || t * TK + TK <= wlo) return;
+    const char* k = lds + ((t - t0) & 1) * 2 * kBytes;
+    // 32 slots at a time: the masks and checks want registers too
+#pragma unroll 1
+    for (int u = 0; u < NS; ++u)
+      odd |= edge_step<T, DP, CAP>(a, k + u * 32 * L::kRowBytes, k + kBytes + u * 32 * L::kRowBytes, at,
+                                   q, t * TK + 32 * u, qr.lo, qr.hi, st, acc);
+  };
+  int t = t0;
+  for (; t < t1 && t * TK < alo; ++t) {
+    arrive(t);
+    edges(t);
+  }
+  const int tm = min(t1, ahi / TK);
+  bool here = false;  // tile t has landed
+  if (t < tm) {
+    arrive(t);
+    here = true;
+    f32x16 s[NS];
+    auto score = [&]() __attribute__((always_inline)) {
+      const char* k = lds + ((t - t0) & 1) * 2 * kBytes;
 #pragma unroll
       for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, at, q);
       if constexpr (CAP) cap_scores(a, s);
-      softmax_step(CAP ? 1.f : a.scale2, s, st, acc);
+      return top_score(c2, s);
+    };
+    rescale(st, score(), acc);
+    while (!exceeds(st, score(), kRoom)) {
+      weights(c2, s, st);
+      const char* v = lds + ((t - t0) & 1) * 2 * kBytes + kBytes;
 #pragma unroll
       for (int u = 0; u < NS; ++u) L::template add_values<false>(v + u * 32 * L::kRowBytes, at, s[u], acc);
-    } else {
-      // 32 slots at a time: the masks' and checks' registers are not the
-      // loop's above
-#pragma unroll 1
-      for (int u = 0; u < NS; ++u) {
-        odd |= edge_step<T, DP, CAP>(a, k + u * 32 * L::kRowBytes, v + u * 32 * L::kRowBytes, at, q,
-                                     j0 + 32 * u, qr.lo, qr.hi, st, acc);
-      }
+      here = false;
+      if (++t == tm) break;
+      arrive(t);
+      here = true;
     }
+  }
+  for (; t < t1; ++t) {
+    if (!here) arrive(t);
+    here = false;
+    edges(t);
   }
 
   const int unit = h * fp.strips + strip;

@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
     for (int i = 0; i < kCopies; ++i) {
       const int row = (i * 8 + w) * R + lane / L::kChunks;
       const int r = min(r_first + s * kRows + row, c.m * a.group - 1);
-      const int chunk = (lane % L::kChunks) ^ (row & L::kSwz);
+      const int chunk = (lane % L::kChunks) ^ L::key_swz(row);
       const int tok = fdiv(a.by_group, r), g = r - tok * a.group;
       const char* from = a.q + ((c.q0 + tok) * a.q_sr + (h * a.group + g) * a.q_sh) * static_cast<int64_t>(sizeof(T)) + chunk * 16;
       if (chunk * 16 < a.d * static_cast<int>(sizeof(T)))

@@ -54,35 +54,44 @@ __device__ __forceinline__ bool finite(float x) {
   return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
 }
 
-// Rows of head_dim DP (padded with zeros past a.d) in LDS: 16-byte chunk c of
-// row r lies at chunk c ^ (r % 8) of its row, which spreads the rows that one
-// read instruction touches over the banks.  A lane's address is one of a few
-// that are formed once (LaneAt) and a constant: the swizzle is within 128 bytes.
+// Rows of head_dim DP (padded with zeros past a.d) in LDS.  16-byte chunk c of
+// row r lies at chunk c ^ swz(r) of its row, so that the 16 rows (keys), or the
+// 4 rows of 64 bytes (values), that a read instruction takes at a time cover
+// all of the LDS's 64 banks: with one swizzle by r % 8 for both, reads took 1.6
+// (keys) and 1.8 (values) times as long.  A lane's address is one of a few that
+// are formed once (LaneAt) and a constant, since the swizzle is within 256
+// (keys) or 128 bytes (values).
 template <typename T, int DP>
 struct Tile {
   static constexpr int kChunks = DP * sizeof(T) / 16;
-  static constexpr int kSwz = 7;
+  static constexpr int kKeyAt = kChunks < 16 ? 4 : 8;   // addresses of a lane's key pieces
   static constexpr int kRowBytes = DP * sizeof(T);
   static constexpr int kRowsPerCopy = 64 / kChunks;  // rows of one wave's copy instruction
   static constexpr bool kBf16 = sizeof(T) == 2;
   static constexpr int kQ = kBf16 ? DP / 16 : DP / 8;  // 16-byte query pieces of a lane
 
+  static __device__ __forceinline__ int key_swz(int r) {
+    return kChunks < 16 ? (r >> 1) & 7 : r & 15;
+  }
+  static __device__ __forceinline__ int value_swz(int r) { return (r & 1) << 2 | ((r >> 1) & 3); }
+
   struct LaneAt {
-    int k[4];  // keys: row n, chunk 2 i + h is at k[i % 4] + i / 4 * 128
+    int k[kKeyAt];  // keys: row n, chunk 2 i + h is at k[i % kKeyAt] + i / kKeyAt * kKeyAt * 32
     int v[4];  // values: see value_frag (bf16: two) and add_values
   };
   static __device__ __forceinline__ LaneAt lane_at() {
     const int lane = threadIdx.x % 64, n = lane % 32, h = lane / 32, i = lane % 16;
     LaneAt at;
 #pragma unroll
+    for (int x = 0; x < kKeyAt; ++x) at.k[x] = n * kRowBytes + ((2 * x + h) ^ key_swz(n)) * 16;
+#pragma unroll
     for (int x = 0; x < 4; ++x) {
-      at.k[x] = n * kRowBytes + ((2 * x + h) ^ (n & 7)) * 16;
       if constexpr (kBf16) {
         const int row = 4 * h + i / 4, c = 4 * (x & 1) + 2 * (lane / 16 % 2) + i % 4 / 2;
-        at.v[x] = row * kRowBytes + (c ^ row) * 16 + i % 2 * 8;
+        at.v[x] = row * kRowBytes + (c ^ value_swz(row)) * 16 + i % 2 * 8;
       } else {
         const int row = 4 * h + x;
-        at.v[x] = row * kRowBytes + (n / 4 ^ row) * 16 + n % 4 * 4;
+        at.v[x] = row * kRowBytes + (n / 4 ^ value_swz(row)) * 16 + n % 4 * 4;
       }
     }
     return at;
@@ -110,11 +119,11 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
       if constexpr (kBf16) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + at.k[i % 4] + i / 4 * 128);
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + at.k[i % kKeyAt] + i / kKeyAt * kKeyAt * 32);
         const bf16x8 b = __builtin_bit_cast(bf16x8, q[i]);
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(SWAP ? b : a, SWAP ? a : b, s, 0, 0, 0);
       } else {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(k + at.k[i % 4] + i / 4 * 128);
+        const f32x4 a = *reinterpret_cast<const f32x4*>(k + at.k[i % kKeyAt] + i / kKeyAt * kKeyAt * 32);
         const f32x4 b = __builtin_bit_cast(f32x4, q[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -274,50 +283,52 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
   constexpr int kCopies = Copies<T, DP, TK, WAVES>::kN, R = L::kRowsPerCopy;
   const int lane = threadIdx.x % 64, sub = lane / L::kChunks;
   const uint32_t st = static_cast<uint32_t>(c.st) * sizeof(T);
-  const bool full = d == DP;
-  auto copies = [&](int i, uint32_t rows, const char* k, const char* v) __attribute__((always_inline)) {
-    // rows: of the tile, by which k and v are short of the instruction's first
-    const int row = (i * WAVES + w) * R + sub;
-    const int chunk = (lane % L::kChunks) ^ (row & L::kSwz);
-    const uint32_t off = (rows + sub) * st + chunk * 16;
-    const uint32_t to = lds + (i * WAVES + w) * 1024;
-    if (full || chunk * 16 < d * static_cast<int>(sizeof(T))) {
-      copy16(k, off, to);
-      if constexpr (VALUES) copy16(v, off, to + TK * L::kRowBytes);
-    }
-  };
-  const int64_t sb = c.sb * static_cast<int64_t>(sizeof(T));
-  if (j0 >= lo && j0 + TK <= hi && c.run >= TK) {
-    // the whole tile lies in one block
-    const int32_t id = c.table ? blocks.id[0] : b;
-    const uint32_t slot = c.table ? j0 - fdiv(c.bs, j0) * c.bs.d : j0;
-    const int64_t at = id * sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
+  // copy i moves rows (i WAVES + w) R + sub: the swizzle of its low bits is
+  // the lane's, that of the high ones a constant
+  const int low = w * R + sub, bytes = d * static_cast<int>(sizeof(T));
+  const int ck = ((lane % L::kChunks) ^ L::key_swz(low)) * 16;
+  const int cv = ((lane % L::kChunks) ^ L::value_swz(low)) * 16;
+  if (j0 >= lo && j0 + TK <= hi && c.run >= 8) {
+    const int64_t sb = c.sb * static_cast<int64_t>(sizeof(T));
+    int64_t at[kCopies];
+    if (c.run >= TK) {
+      // the whole tile lies in one block
+      const int32_t id = c.table ? blocks.id[0] : b;
+      const uint32_t slot = c.table ? j0 - fdiv(c.bs, j0) * c.bs.d : j0;
+      const int64_t first = id * sb + static_cast<int64_t>(static_cast<uint64_t>(slot + w * R) * st);
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i) copies(i, (i * WAVES + w) * R, kb + at, vb + at);
-  } else if (j0 >= lo && j0 + TK <= hi && c.run >= 8) {
+      for (int i = 0; i < kCopies; ++i) at[i] = first + static_cast<int64_t>(i * WAVES * R) * st;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        const int j = j0 + (i * WAVES + w) * R;
+        const uint32_t slot = j - fdiv(c.bs, j) * c.bs.d;
+        at[i] = blocks.id[i] * sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-      const int j = j0 + (i * WAVES + w) * R;
-      const uint32_t slot = j - fdiv(c.bs, j) * c.bs.d;
-      const int64_t at = blocks.id[i] * sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
-      copies(i, 0, kb + at, vb + at);
+      const int k = ck ^ (L::key_swz(i * WAVES * R) * 16), v = cv ^ (L::value_swz(i * WAVES * R) * 16);
+      const uint32_t to = lds + (i * WAVES + w) * 1024;
+      if (k < bytes) copy16(kb + at[i], sub * st + k, to);
+      if constexpr (VALUES)
+        if (v < bytes) copy16(vb + at[i], sub * st + v, to + TK * L::kRowBytes);
     }
   } else {
     // lane i finds row i's place
     const int j = min(max(j0 + lane % TK, lo), hi - 1);
     const int64_t at = cache_offset(c, cache_block(c, b, j), j) * static_cast<int64_t>(sizeof(T));
     const uint32_t at_lo = static_cast<uint32_t>(at), at_hi = static_cast<uint32_t>(at >> 32);
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < kCopies; ++i) {
-      const int row = (i * WAVES + w) * R + sub;
-      const int chunk = (lane % L::kChunks) ^ (row & L::kSwz);
+      const int row = i * WAVES * R + low;
+      const int k = ck ^ (L::key_swz(i * WAVES * R) * 16), v = cv ^ (L::value_swz(i * WAVES * R) * 16);
       const int64_t o = static_cast<int64_t>(static_cast<uint64_t>(__shfl(at_hi, row)) << 32 |
-                                             __shfl(at_lo, row)) + chunk * 16;
+                                             __shfl(at_lo, row));
       const uint32_t to = lds + (i * WAVES + w) * 1024;
-      if (full || chunk * 16 < d * static_cast<int>(sizeof(T))) {
-        copy16(kb + o, to);
-        if constexpr (VALUES) copy16(vb + o, to + TK * L::kRowBytes);
-      }
+      if (k < bytes) copy16(kb + o + k, to);
+      if constexpr (VALUES)
+        if (v < bytes) copy16(vb + o + v, to + TK * L::kRowBytes);
     }
   }
 }
@@ -436,28 +447,43 @@ struct Softmax {
   float m2 = -INFINITY, l = 0.f;
 };
 
-// One step over NS groups of 32 slots' scores, which become weights; c brings
-// them to log2 units.  The reference moves only when a score exceeds it by
-// more than 2^8, so the products are rescaled rarely; weights stay below 2^8.
-template <int NS, int NB>
-__device__ __forceinline__ void softmax_step(float c, f32x16 (&s)[NS], Softmax& st,
-                                             f32x16 (&acc)[NB]) {
+// The largest of a query's scores of NS groups of 32 slots, in log2 units (c
+// brings them there).
+template <int NS>
+__device__ __forceinline__ float top_score(float c, const f32x16 (&s)[NS]) {
   float top = s[0][0];
 #pragma unroll
   for (int t = 0; t < NS; ++t)
 #pragma unroll
     for (int v = t ? 0 : 1; v < 16; ++v) top = fmaxf(top, s[t][v]);
-  top = half_max(top) * c;
-  if (__any(top - st.m2 > 8.f)) {
-    const float m = fmaxf(st.m2, top);
-    const float alpha = m == st.m2 ? 1.f : __builtin_amdgcn_exp2f(st.m2 - m);
-    st.m2 = m;
-    st.l *= alpha;
+  return half_max(top) * c;
+}
+
+// Whether a score exceeds its query's reference by more than 2^by.
+__device__ __forceinline__ bool exceeds(const Softmax& st, float top, float by) {
+  return __any(top - st.m2 > by);
+}
+
+// How far scores may pass their reference without a rescaling (log2 units).
+// Weights and sums are floating-point numbers, as exact at 2^80 as at 1, and
+// 2^80 times a sum over 2^31 slots is far from fp32's largest, 2^128.
+constexpr float kRoom = 80.f;
+
+template <int NB>
+__device__ __forceinline__ void rescale(Softmax& st, float top, f32x16 (&acc)[NB]) {
+  const float m = fmaxf(st.m2, top);
+  const float alpha = m == st.m2 ? 1.f : __builtin_amdgcn_exp2f(st.m2 - m);
+  st.m2 = m;
+  st.l *= alpha;
 #pragma unroll
-    for (int db = 0; db < NB; ++db)
+  for (int db = 0; db < NB; ++db)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
-  }
+    for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
+}
+
+// Scores become weights.
+template <int NS>
+__device__ __forceinline__ void weights(float c, f32x16 (&s)[NS], Softmax& st) {
   const float ref = st.m2 == -INFINITY ? 0.f : -st.m2;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -468,6 +494,14 @@ __device__ __forceinline__ void softmax_step(float c, f32x16 (&s)[NS], Softmax& 
       sum[v % 4] += s[t][v];
     }
   st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+template <int NS, int NB>
+__device__ __forceinline__ void softmax_step(float c, f32x16 (&s)[NS], Softmax& st,
+                                             f32x16 (&acc)[NB]) {
+  const float top = top_score(c, s);
+  if (exceeds(st, top, 8.f)) rescale(st, top, acc);
+  weights(c, s, st);
 }
 
 // Capped scores, in log2 units.
