@@ -9,8 +9,8 @@ namespace {
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// Units of the chunk kernel that are split, at most: with fewer workgroups
-// than compute units some of those would idle.
+// Pieces that the units of the chunk kernel are split into, at most: with fewer
+// workgroups than the compute units take some of those would idle.
 int64_t most_pieces(const kvx_attn* at) { return 2 * int64_t(at->n_cu); }
 
 size_t head_bytes(const kvx_attn* at) { return (most_pieces(at) * sizeof(JoinHead) + 255) / 256 * 256; }
@@ -37,11 +37,11 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
     const int64_t strips = (int64_t(a.rows) * at->group + kChunkRows - 1) / kChunkRows +
                            std::min(a.batch, a.rows);
     const int64_t units = strips * a.hkv;
+    p.join_rows = kChunkRows;
     p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(16, most_pieces(at) / units)));
     if (units * p.splits > INT32_MAX) return hipErrorInvalidValue;
     p.strips = static_cast<int>(strips);
     p.grid = static_cast<int>(units * p.splits);
-    p.join_rows = kChunkRows;
   }
   const bool f32 = at->dtype == KVX_F32;
   switch (padded_dim(at->model.head_dim)) {

@@ -40,13 +40,93 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const QueryRow& q, 
 }
 
 // ---------------------------------------------------------------------------
-// Chunks: 4 waves of 32 query rows share tiles of kTile slots, copied straight
-// into one of two LDS buffers while the other is computed on; one barrier per
-// tile.
+// Chunks: 4 waves of 32 query rows share tiles of 64 slots (32 where rows
+// are of 1024 bytes), copied straight into LDS ahead of their use: keys two
+// tiles, into one of three buffers, values one, into one of two.  One barrier
+// per tile.  The scores of tile t + 1 are formed beside the weights of tile t,
+// which need other units of the compute unit.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP>
 constexpr int chunk_tile() { return DP * sizeof(T) <= 512 ? 64 : 32; }
+
+// One turn of the chunk kernel's middle loop: the scores `next` of the tile
+// whose keys are at k, the weights of the scores s, their products with the
+// values at v, and next's largest scores.  A step is one LDS piece's matrix
+// instructions and a share of the vector work, which the units do side by
+// side; steps are kept apart, since the compiler left to itself read LDS just
+// before each use and did the vector work in one go.  Pieces are read kAhead
+// steps before their use.  Of the NS * 16 weights of a lane, three quarters
+// come beside the scores, the last quarter beside the first half of the
+// products (which do not need them), the largest scores beside the products.
+template <typename T, int DP, bool CAP, int NS>
+__device__ __forceinline__ void middle_turn(const AttnArgs& a, const char* k, const char* v,
+                                            const typename Tile<T, DP>::LaneAt& at,
+                                            const uint4 (&q)[Tile<T, DP>::kQ], float c2,
+                                            f32x16 (&s)[NS], f32x16 (&next)[NS], Softmax& st,
+                                            f32x16 (&acc)[DP / 32], float& top) {
+  using L = Tile<T, DP>;
+  static_assert(L::kBf16 && NS == 2, "two groups of slots, bf16");
+  constexpr int KQ = L::kQ, kSteps = NS * KQ, kAheadK = 6, kAheadV = 4, NB = DP / 32;
+  constexpr int kWeights = 16 * NS, kBeside = kWeights * 3 / 4, kLater = kWeights - kBeside;
+  static_assert(2 * NS * NB == kSteps, "");
+  uint4 kf[kAheadK + 1];
+  bf16x8 vf[kAheadV + 1], b;
+  const float ref = st.m2 == -INFINITY ? 0.f : -st.m2;
+  float sum[2] = {0.f, 0.f};
+  auto read_key = [&](int i) __attribute__((always_inline)) {
+    kf[i % (kAheadK + 1)] = *reinterpret_cast<const uint4*>(
+        k + i / KQ * 32 * L::kRowBytes + at.k[i % KQ % L::kKeyAt] + i % KQ / L::kKeyAt * L::kKeyAt * 32);
+  };
+  auto read_value = [&](int j) __attribute__((always_inline)) {
+    vf[j % (kAheadV + 1)] = L::value_frag(v + j / (2 * NB) * 32 * L::kRowBytes, at, j / NB % 2, j % NB);
+  };
+  auto weigh = [&](int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = from; e < to; ++e) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 16][e % 16], c2, ref));
+      s[e / 16][e % 16] = p;
+      sum[e % 2] += p;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kAheadK; ++i) read_key(i);
+#pragma unroll
+  for (int u = 0; u < NS; ++u)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) next[u][x] = 0.f;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    if (i + kAheadK < kSteps) read_key(i + kAheadK);
+    if (i + kAheadV >= kSteps) read_value(i + kAheadV - kSteps);
+    next[i / KQ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+        __builtin_bit_cast(bf16x8, kf[i % (kAheadK + 1)]), __builtin_bit_cast(bf16x8, q[i % KQ]),
+        next[i / KQ], 0, 0, 0);
+    weigh(kBeside * i / kSteps, kBeside * (i + 1) / kSteps);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int j = 0; j < kSteps; ++j) {
+    if (j + kAheadV < kSteps) read_value(j + kAheadV);
+    if (j % NB == 0) {
+      // weights rounded once to bf16 for the matrix instruction; the sum that
+      // divides them keeps fp32
+#pragma unroll
+      for (int e = 0; e < 8; ++e) b[e] = static_cast<__bf16>(s[j / NB / 2][j / NB % 2 * 8 + e]);
+    }
+    acc[j % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % (kAheadV + 1)], b, acc[j % NB], 0, 0, 0);
+    if (j < kSteps / 2) weigh(kBeside + 2 * kLater * j / kSteps, kBeside + 2 * kLater * (j + 1) / kSteps);
+#pragma unroll
+    for (int e = kWeights * j / kSteps; e < kWeights * (j + 1) / kSteps; ++e) {
+      float x = next[e / 16][e % 16];
+      if constexpr (CAP) next[e / 16][e % 16] = x = score2(a, x);
+      top = e == 0 ? x : fmaxf(top, x);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  top = half_max(top) * c2;
+  st.l += sum[0] + sum[1];
+}
 
 template <typename T, int DP, bool CAP>
 __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
@@ -54,7 +134,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   using L = Tile<T, DP>;
   constexpr int TK = chunk_tile<T, DP>(), NS = TK / 32, NB = DP / 32;
   constexpr int kBytes = TK * L::kRowBytes;  // keys or values of a tile
-  __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];  // [buffer][K, V]
+  __shared__ __attribute__((aligned(16))) char lds[5 * kBytes];  // 3 of keys, 2 of values
   const int lane = threadIdx.x % 64, n = lane % 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 
@@ -104,6 +184,9 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   const int t0 = lo / TK + split * per, t1 = min(t0 + per, lo / TK + tiles);
 
   const QueryRow qr = query_row(a, c, r0 + w * 32 + n);
+  uint4 q[L::kQ];
+  const T* qp = reinterpret_cast<const T*>(a.q) + qr.row * a.q_sr + (h * a.group + qr.g) * a.q_sh;
+  L::load_q(q, w * 32 + n < valid ? qp : nullptr, a.d);
   // what the wave's rows see: together, and all of them
   const int rows_w = min(32, valid - w * 32);
   int wlo = 0, whi = 0, alo = 0, ahi = 0;
@@ -113,34 +196,42 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     seen_by(a, c, rw, rw, alo, ahi);
     seen_by(a, c, rw + rows_w - 1, rw + rows_w - 1, alo, whi);
   }
-  uint4 q[L::kQ];
-  const T* qp = reinterpret_cast<const T*>(a.q) + qr.row * a.q_sr + (h * a.group + qr.g) * a.q_sh;
-  L::load_q(q, r0 + w * 32 + n < c.m * a.group ? qp : nullptr, a.d);
 
   f32x16 acc[NB];
+  Softmax st;
 #pragma unroll
   for (int db = 0; db < NB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
-  Softmax st;
 
   if (a.d < DP) {
-    for (int i = threadIdx.x; i < 4 * kBytes / 16; i += 256)
+    for (int i = threadIdx.x; i < 5 * kBytes / 16; i += 256)
       reinterpret_cast<uint4*>(lds)[i] = uint4{0, 0, 0, 0};
     __syncthreads();
   }
   const uint32_t l3 = lds_address(lds);
   const char* kb = a.c.k + h * a.c.sh * static_cast<int64_t>(sizeof(T));
   const char* vb = a.c.v + h * a.c.sh * static_cast<int64_t>(sizeof(T));
-  Copies<T, DP, TK, 4> blocks;
+  Copies<T, DP, TK, 4> kblocks, vblocks;
   bool odd = false;
   const typename L::LaneAt at = L::lane_at();
   // the queries are here: the compiler must not wait for them in the loop
   __builtin_amdgcn_s_waitcnt(0);
+  auto copy_keys = [&](int t, int slot) __attribute__((always_inline)) {
+    copy_tile<T, DP, TK, 4, true, false>(a.c, kb, vb, b, t * TK, lo, hi, kblocks, a.d, w,
+                                         l3 + slot * kBytes, 0);
+    vblocks = kblocks;
+    fetch_blocks(a.c, b, t * TK + TK, hi, w, kblocks);
+  };
+  auto copy_values = [&](int t) __attribute__((always_inline)) {
+    copy_tile<T, DP, TK, 4, false, true>(a.c, kb, vb, b, t * TK, lo, hi, vblocks, a.d, w, 0,
+                                         l3 + (3 + ((t - t0) & 1)) * kBytes);
+  };
   if (t0 < t1) {
-    fetch_blocks(a.c, b, t0 * TK, hi, w, blocks);
-    copy_tile<T, DP, TK, 4>(a.c, kb, vb, b, t0 * TK, lo, hi, blocks, a.d, w, l3);
-    fetch_blocks(a.c, b, t0 * TK + TK, hi, w, blocks);
+    fetch_blocks(a.c, b, t0 * TK, hi, w, kblocks);
+    copy_keys(t0, 0);
+    copy_values(t0);
+    if (t0 + 1 < t1) copy_keys(t0 + 1, 1);
   }
   // Three loops, so that the one that matters has few registers to keep: tiles
   // before the first that all of the wave's queries see (windows), tiles that
@@ -148,72 +239,91 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   // first of its tiles gives; should a score ever pass it by 2^kRoom, the last
   // loop goes on, which moves it.
   const float c2 = CAP ? 1.f : a.scale2;
+  int slot = 0;  // of tile t's keys
+  auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
   auto arrive = [&](int t) __attribute__((always_inline)) {
-    // tile t has landed, and every wave is done with the other buffer
+    // tile t's values and tile t + 1's keys have landed, and every wave is done
+    // with tile t - 1
     vm_wait<0>();
     tile_barrier();
-    if (t + 1 < t1) {
-      copy_tile<T, DP, TK, 4>(a.c, kb, vb, b, t * TK + TK, lo, hi, blocks, a.d, w,
-                              l3 + ((t + 1 - t0) & 1) * 2 * kBytes);
-      fetch_blocks(a.c, b, t * TK + 2 * TK, hi, w, blocks);
-    }
+    if (t + 1 < t1) copy_values(t + 1);
+    if (t + 2 < t1) copy_keys(t + 2, after(after(slot)));
+    __builtin_amdgcn_sched_barrier(0);
   };
+  auto values_of = [&](int t) { return lds + (3 + ((t - t0) & 1)) * kBytes; };
   auto edges = [&](int t) __attribute__((always_inline)) {
     if (t * TK >= whi || t * TK + TK <= wlo) return;
-    const char* k = lds + ((t - t0) & 1) * 2 * kBytes;
+    const char *k = lds + slot * kBytes, *v = values_of(t);
     // 32 slots at a time: the masks and checks want registers too
 #pragma unroll 1
     for (int u = 0; u < NS; ++u)
-      odd |= edge_step<T, DP, CAP>(a, k + u * 32 * L::kRowBytes, k + kBytes + u * 32 * L::kRowBytes, at,
-                                   q, t * TK + 32 * u, qr.lo, qr.hi, st, acc);
+      odd |= edge_step<T, DP, CAP>(a, k + u * 32 * L::kRowBytes, v + u * 32 * L::kRowBytes, at, q,
+                                   t * TK + 32 * u, qr.lo, qr.hi, st, acc);
   };
   int t = t0;
   for (; t < t1 && t * TK < alo; ++t) {
     arrive(t);
     edges(t);
+    slot = after(slot);
   }
   const int tm = min(t1, ahi / TK);
   bool here = false;  // tile t has landed
   if (t < tm) {
-    arrive(t);
-    here = true;
     f32x16 s[NS];
-    auto score = [&]() __attribute__((always_inline)) {
-      const char* k = lds + ((t - t0) & 1) * 2 * kBytes;
+    float top;
+    auto score = [&](int slot, f32x16 (&s)[NS]) __attribute__((always_inline)) {
+      const char* k = lds + slot * kBytes;
 #pragma unroll
       for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, at, q);
       if constexpr (CAP) cap_scores(a, s);
-      return top_score(c2, s);
+      top = top_score(c2, s);
     };
-    rescale(st, score(), acc);
-    while (!exceeds(st, score(), kRoom)) {
-      weights(c2, s, st);
-      const char* v = lds + ((t - t0) & 1) * 2 * kBytes + kBytes;
+    arrive(t);
+    score(slot, s);
+    rescale(st, top, acc);
+    while (true) {
+      // the scores of tile t are within reach of the reference.  (After the
+      // last tile the next one's are formed of what LDS holds, and not used.)
+      f32x16 next[NS];
+      const char *k = lds + after(slot) * kBytes, *v = values_of(t);
+      if constexpr (L::kBf16) {
+        middle_turn<T, DP, CAP, NS>(a, k, v, at, q, c2, s, next, st, acc, top);
+      } else {
+        score(after(slot), next);
 #pragma unroll
-      for (int u = 0; u < NS; ++u) L::template add_values<false>(v + u * 32 * L::kRowBytes, at, s[u], acc);
-      here = false;
+        for (int u = 0; u < NS; ++u) {
+          weights(c2, s[u], st);
+          L::template add_values<false>(v + u * 32 * L::kRowBytes, at, s[u], acc);
+        }
+      }
+      slot = after(slot);
       if (++t == tm) break;
       arrive(t);
-      here = true;
+      here = exceeds(st, top, kRoom);
+      if (here) break;
+#pragma unroll
+      for (int u = 0; u < NS; ++u) s[u] = next[u];
     }
   }
   for (; t < t1; ++t) {
     if (!here) arrive(t);
     here = false;
     edges(t);
+    slot = after(slot);
   }
 
   const int unit = h * fp.strips + strip;
   float* part = fp.pieces + (static_cast<size_t>(unit) * fp.splits + split) * piece_floats(kChunkRows, DP);
   if (fp.splits > 1 && split == 0 && threadIdx.x == 0)
     *head = JoinHead{fp.splits, valid, c.q0, r0, h, unit * fp.splits, unseeing(a, c, r0)};
+  const int r = w * 32 + n;
   if (fp.splits == 1) {
-    if (w * 32 + n < valid) store_out<T, NB>(a, qr, h, acc, st);
+    if (r < valid) store_out<T, NB>(a, qr, h, acc, st);
   } else {
     const float l = half_sum(st.l);
-    if (w * 32 + n < valid) {
-      if (lane < 32) reinterpret_cast<float2*>(part)[w * 32 + n] = float2{st.m2, l};
-      float* o = part + 2 * kChunkRows + static_cast<size_t>(w * 32 + n) * DP;
+    if (r < valid) {
+      if (lane < 32) reinterpret_cast<float2*>(part)[r] = float2{st.m2, l};
+      float* o = part + 2 * kChunkRows + static_cast<size_t>(r) * DP;
 #pragma unroll
       for (int db = 0; db < NB; ++db)
 #pragma unroll
@@ -342,7 +452,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
     Copies<T, DP, 32, 1> blocks;
     auto copy = [&](int t) __attribute__((always_inline)) {
       copy_tile<T, DP, 32, 1>(a.c, kb, vb, b, slot_of(t), lo, hi, blocks, a.d, 0,
-                              ring3 + t % NST * D::kStage);
+                              ring3 + t % NST * D::kStage, ring3 + t % NST * D::kStage + kBytes);
       fetch_blocks(a.c, b, slot_of(t + 1), hi, 0, blocks);
     };
     bool odd = false;

@@ -122,8 +122,8 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
         if (from && lane < 32)
           copy4(reinterpret_cast<const char*>(from + mrow + min(slot_of(t) + n, end - 1)),
                 earlier3 + t % NST * 128);
-        copy_tile<T, DP, 32, 1, false>(a.c, kb, nullptr, b, slot_of(t), lo, hi, blocks, a.d, 0,
-                                       ring3 + t % NST * kStage);
+        copy_tile<T, DP, 32, 1, true, false>(a.c, kb, nullptr, b, slot_of(t), lo, hi, blocks, a.d, 0,
+                                             ring3 + t % NST * kStage, 0);
         fetch_blocks(a.c, b, slot_of(t + 1), hi, 0, blocks);
       };
       auto put = [&](int t, float sum) __attribute__((always_inline)) {

@@ -70,10 +70,10 @@ struct Tile {
   static constexpr bool kBf16 = sizeof(T) == 2;
   static constexpr int kQ = kBf16 ? DP / 16 : DP / 8;  // 16-byte query pieces of a lane
 
-  static __device__ __forceinline__ int key_swz(int r) {
+  static __device__ __forceinline__ constexpr int key_swz(int r) {
     return kChunks < 16 ? (r >> 1) & 7 : r & 15;
   }
-  static __device__ __forceinline__ int value_swz(int r) { return (r & 1) << 2 | ((r >> 1) & 3); }
+  static __device__ __forceinline__ constexpr int value_swz(int r) { return (r & 1) << 2 | ((r >> 1) & 3); }
 
   struct LaneAt {
     int k[kKeyAt];  // keys: row n, chunk 2 i + h is at k[i % kKeyAt] + i / kKeyAt * kKeyAt * 32
@@ -236,6 +236,32 @@ __device__ __forceinline__ void copy16(const char* from, uint32_t lds) {
                : "memory");
 }
 
+// N such copies of one base, to lds + i * STEP: the wait states are spent once.
+template <int N, int STEP>
+__device__ __forceinline__ void copy16_run(const char* from, const uint32_t* off, uint32_t lds) {
+  static_assert(N == 2 || N % 4 == 0, "");
+  const uint64_t p = reinterpret_cast<uint64_t>(from);
+  const uint64_t base = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p >> 32))) << 32 |
+                        static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p)));
+  lds = __builtin_amdgcn_readfirstlane(lds);
+  if constexpr (N == 2) {
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
+        "s_add_u32 m0, m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(lds),
+        "v"(off[0]), "v"(off[1]), "s"(base), "n"(STEP)
+        : "memory", "scc");
+  } else {
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5" ::"s"(lds),
+        "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "n"(STEP)
+        : "memory", "scc");
+    if constexpr (N > 4) copy16_run<N - 4, STEP>(from, off + 4, lds + 4 * STEP);
+  }
+}
+
 // 4 bytes per lane, lane i's to lds + 4 i.
 __device__ __forceinline__ void copy4(const char* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from)
@@ -271,14 +297,14 @@ __device__ __forceinline__ void fetch_blocks(const CacheArgs& c, int b, int j0, 
 }
 
 // Copies rows j0 .. j0 + TK - 1 of a cache (keys at kb, values at vb of one
-// head, unless VALUES is false) into LDS at `lds` and `lds + TK rows`, each wave w of WAVES its share,
-// each lane the chunk that belongs at its place.  Slots outside [lo, hi) are
-// replaced by the nearest inside.
-template <typename T, int DP, int TK, int WAVES, bool VALUES = true>
+// head) into LDS at lk and lv, each wave w of WAVES its share, each lane the
+// chunk that belongs at its place.  Slots outside [lo, hi) are replaced by the
+// nearest inside.
+template <typename T, int DP, int TK, int WAVES, bool KEYS = true, bool VALUES = true>
 __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, const char* vb, int b,
                                           int j0, int lo, int hi,
                                           const Copies<T, DP, TK, WAVES>& blocks, int d, int w,
-                                          uint32_t lds) {
+                                          uint32_t lk, uint32_t lv) {
   using L = Tile<T, DP>;
   constexpr int kCopies = Copies<T, DP, TK, WAVES>::kN, R = L::kRowsPerCopy;
   const int lane = threadIdx.x % 64, sub = lane / L::kChunks;
@@ -288,11 +314,30 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
   const int low = w * R + sub, bytes = d * static_cast<int>(sizeof(T));
   const int ck = ((lane % L::kChunks) ^ L::key_swz(low)) * 16;
   const int cv = ((lane % L::kChunks) ^ L::value_swz(low)) * 16;
-  if (j0 >= lo && j0 + TK <= hi && c.run >= 8) {
+  if (kCopies <= 8 && j0 >= lo && j0 + TK <= hi && c.run >= TK && d == DP) {
+    // the whole tile lies in one block, rows have all of DP: one base (not for
+    // more copies, whose offsets would fill the registers)
+    const int32_t id = c.table ? blocks.id[0] : b;
+    const uint32_t slot = c.table ? j0 - fdiv(c.bs, j0) * c.bs.d : j0;
+    const int64_t at = id * (c.sb * static_cast<int64_t>(sizeof(T))) +
+                       static_cast<int64_t>(static_cast<uint64_t>(slot + w * R) * st);
+    uint32_t off[kCopies];
+    if constexpr (KEYS) {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i)
+        off[i] = (i * WAVES * R + sub) * st + (ck ^ (L::key_swz(i * WAVES * R) * 16));
+      copy16_run<kCopies, WAVES * 1024>(kb + at, off, lk + w * 1024);
+    }
+    if constexpr (VALUES) {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i)
+        off[i] = (i * WAVES * R + sub) * st + (cv ^ (L::value_swz(i * WAVES * R) * 16));
+      copy16_run<kCopies, WAVES * 1024>(vb + at, off, lv + w * 1024);
+    }
+  } else if (j0 >= lo && j0 + TK <= hi && c.run >= 8) {
     const int64_t sb = c.sb * static_cast<int64_t>(sizeof(T));
     int64_t at[kCopies];
     if (c.run >= TK) {
-      // the whole tile lies in one block
       const int32_t id = c.table ? blocks.id[0] : b;
       const uint32_t slot = c.table ? j0 - fdiv(c.bs, j0) * c.bs.d : j0;
       const int64_t first = id * sb + static_cast<int64_t>(static_cast<uint64_t>(slot + w * R) * st);
@@ -309,10 +354,11 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
       const int k = ck ^ (L::key_swz(i * WAVES * R) * 16), v = cv ^ (L::value_swz(i * WAVES * R) * 16);
-      const uint32_t to = lds + (i * WAVES + w) * 1024;
-      if (k < bytes) copy16(kb + at[i], sub * st + k, to);
+      const uint32_t to = (i * WAVES + w) * 1024;
+      if constexpr (KEYS)
+        if (k < bytes) copy16(kb + at[i], sub * st + k, lk + to);
       if constexpr (VALUES)
-        if (v < bytes) copy16(vb + at[i], sub * st + v, to + TK * L::kRowBytes);
+        if (v < bytes) copy16(vb + at[i], sub * st + v, lv + to);
     }
   } else {
     // lane i finds row i's place
@@ -325,10 +371,11 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
       const int k = ck ^ (L::key_swz(i * WAVES * R) * 16), v = cv ^ (L::value_swz(i * WAVES * R) * 16);
       const int64_t o = static_cast<int64_t>(static_cast<uint64_t>(__shfl(at_hi, row)) << 32 |
                                              __shfl(at_lo, row));
-      const uint32_t to = lds + (i * WAVES + w) * 1024;
-      if (k < bytes) copy16(kb + o + k, to);
+      const uint32_t to = (i * WAVES + w) * 1024;
+      if constexpr (KEYS)
+        if (k < bytes) copy16(kb + o + k, lk + to);
       if constexpr (VALUES)
-        if (v < bytes) copy16(vb + o + v, to + TK * L::kRowBytes);
+        if (v < bytes) copy16(vb + o + v, lv + to);
     }
   }
 }
@@ -481,19 +528,16 @@ __device__ __forceinline__ void rescale(Softmax& st, float top, f32x16 (&acc)[NB
     for (int v = 0; v < 16; ++v) acc[db][v] *= alpha;
 }
 
-// Scores become weights.
-template <int NS>
-__device__ __forceinline__ void weights(float c, f32x16 (&s)[NS], Softmax& st) {
+// 32 slots' scores become weights.
+__device__ __forceinline__ void weights(float c, f32x16& s, Softmax& st) {
   const float ref = st.m2 == -INFINITY ? 0.f : -st.m2;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  float sum[2] = {0.f, 0.f};
 #pragma unroll
-  for (int t = 0; t < NS; ++t)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      s[t][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][v], c, ref));
-      sum[v % 4] += s[t][v];
-    }
-  st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  for (int v = 0; v < 16; ++v) {
+    s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, ref));
+    sum[v % 2] += s[v];
+  }
+  st.l += sum[0] + sum[1];
 }
 
 template <int NS, int NB>
@@ -501,7 +545,8 @@ __device__ __forceinline__ void softmax_step(float c, f32x16 (&s)[NS], Softmax& 
                                              f32x16 (&acc)[NB]) {
   const float top = top_score(c, s);
   if (exceeds(st, top, 8.f)) rescale(st, top, acc);
-  weights(c, s, st);
+#pragma unroll
+  for (int t = 0; t < NS; ++t) weights(c, s[t], st);
 }
 
 // Capped scores, in log2 units.

@@ -300,6 +300,40 @@ def test_masked_values_may_be_anything():
         att.close()
 
 
+@pytest.mark.parametrize("dtype,m,d", [("bf16", 1, 128), ("bf16", 140, 128), ("bf16", 140, 256),
+                                       ("f32", 70, 64)])
+def test_scores_that_rise_along_the_cache(dtype, m, d):
+    """Scores from -200 to 200 along the slots (and the other way round): the
+    sums' reference has to move by far more than fp32's exponents span."""
+    T = U.torch()
+    n, hq = 900, 4
+    for rising in (1.0, -1.0):
+        cache = Cache([n], 2, d, dtype, 64)
+        g = T.Generator().manual_seed(8)
+        rows = T.randn(n, 2, d, generator=g) * 0.1
+        rows[..., 0] += T.linspace(-200.0, 200.0, n)[:, None] * rising
+        rows = rows.to(_dt(dtype))
+        blk, slot = cache.place(0, np.arange(n))
+        cache.dev[0][1, blk, :, slot] = rows.cuda()
+        q = _rows(m, hq, d, dtype, 3, 0.1)
+        q[..., 0] = d ** 0.5
+        att = kvx.Attention(kvx.ModelShape(2, 2, d, 1e4), hq,
+                            kvx.KVX_BF16 if dtype == "bf16" else kvx.KVX_F32)
+        out = T.zeros_like(q)
+        lse = T.zeros(m, hq, device="cuda")
+        io = kvx.make_attn_io(cache.struct, _int([n]), q, out=out, lse=lse, layer=1, max_new=m,
+                              q_start=_int([0, m]))
+        att.forward(io, att.workspace())
+        T.cuda.synchronize()
+        ro, rl, mag, size = R.attend(_f64(q), _f64(rows), cache.f64(1, 1, 0), d ** -0.5)
+        delta = _delta(size, d, 0.0)
+        rel = 2 * delta + (n + 64) * EPS + (2.0 ** -8 if dtype == "bf16" else 0.0)
+        tol = mag * rel[..., None] + (2.0 ** -8 * np.abs(ro) if dtype == "bf16" else 0.0)
+        assert (np.abs(_f64(out) - ro) <= tol).all(), (dtype, m, rising)
+        assert (np.abs(_f64(lse) - rl) <= delta + (n + 64) * EPS + 2.0 ** -22 * (1 + np.abs(rl))).all()
+        att.close()
+
+
 APPEND = [
     # name, dtype, hq, hkv, d, page, (new, cached), axes, options
     ("one", "bf16", 12, 2, 128, 16, [(1, 300)], 1, {}),
