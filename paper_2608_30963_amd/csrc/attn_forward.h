@@ -29,7 +29,7 @@ constexpr int kDecodeRows = 32;
 struct ForwardPlan {
   bool decode;
   int grid;       // workgroups
-  int splits;     // chunk: pieces of a unit
+  int splits;     // pieces of a unit; 1: none is split; decode: 0, as the work divides
   int strips;     // chunk: q tiles of all contexts, at most
   int join_rows;  // query rows that a unit may have
   JoinHead* heads;

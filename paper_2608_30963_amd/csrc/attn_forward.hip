@@ -30,8 +30,12 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
   p.decode = int64_t(max_new) * at->group <= kDecodeRows;
   if (p.decode) {
     p.grid = at->n_cu;
-    p.splits = 1;
-    // a context with more new tokens than it was said to have fills its units
+    p.splits = 0;  // as many as the lengths give
+    // short contexts: a workgroup a unit, no join.  Measured (us, captured;
+    // split, whole), heads 12 / 2: 128 slots 10.5, 7.5; 512 10.9, 11.4; 1024 11.5,
+    // 16.8; 64 contexts of 300 slots, heads 64 / 8: 29.0, 25.8; 32 of 1024, heads
+    // 28 / 4: 21.2, 21.6
+    if (a.c.capacity <= 512) p.splits = 1;
     p.join_rows = kDecodeRows;
   } else {
     const int64_t strips = (int64_t(a.rows) * at->group + kChunkRows - 1) / kChunkRows +

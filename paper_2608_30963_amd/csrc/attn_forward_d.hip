@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   const uint32_t l3 = lds_address(lds);
   const char* kb = a.c.k + h * a.c.sh * static_cast<int64_t>(sizeof(T));
   const char* vb = a.c.v + h * a.c.sh * static_cast<int64_t>(sizeof(T));
-  Copies<T, DP, TK, 4> kblocks, vblocks;
+  Blocks<TK> kblocks, vblocks;
   bool odd = false;
   const typename L::LaneAt at = L::lane_at();
   // the queries are here: the compiler must not wait for them in the loop
@@ -221,14 +221,14 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     copy_tile<T, DP, TK, 4, true, false>(a.c, kb, vb, b, t * TK, lo, hi, kblocks, a.d, w,
                                          l3 + slot * kBytes, 0);
     vblocks = kblocks;
-    fetch_blocks(a.c, b, t * TK + TK, hi, w, kblocks);
+    fetch_blocks(a.c, b, t * TK + TK, hi, kblocks);
   };
   auto copy_values = [&](int t) __attribute__((always_inline)) {
     copy_tile<T, DP, TK, 4, false, true>(a.c, kb, vb, b, t * TK, lo, hi, vblocks, a.d, w, 0,
                                          l3 + (3 + ((t - t0) & 1)) * kBytes);
   };
   if (t0 < t1) {
-    fetch_blocks(a.c, b, t0 * TK, hi, w, kblocks);
+    fetch_blocks(a.c, b, t0 * TK, hi, kblocks);
     copy_keys(t0, 0);
     copy_values(t0);
     if (t0 + 1 < t1) copy_keys(t0 + 1, 1);
@@ -397,19 +397,23 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
   const int w = __builtin_amdgcn_readfirstlane(tid / 64);
   JoinHead* head = fp.heads + blockIdx.x;
 
-  const Share share = line_share<NW>(a, [&](int b) {
+  // a unit is one step of the line where units are not split
+  const bool whole = fp.splits == 1;
+  const Share share = line_share(a, [&](int b) {
     const Context c = context(a, b);
     const int qts = (c.m * a.group + kDecodeRows - 1) / kDecodeRows;
+    if (whole) return static_cast<int64_t>(qts);
     int64_t s = 0;
     for (int qt = 0; qt < qts; ++qt) s += decode_steps<D::kStep>(a, c, qt);
     return s;
   });
-  if (tid == 0) head->pieces = 0;
+  if (tid == 0 && !whole) head->pieces = 0;
   const int64_t s0 = share.s0, s1 = share.s1, per = share.per;
   if (s0 >= s1) return;
   int h = share.h, b = share.b, step = share.step;
   Context c = context(a, b);
-  int qt = 0;
+  int qt = whole ? step : 0;
+  if (whole) step = 0;
   for (int x; step >= (x = decode_steps<D::kStep>(a, c, qt)); ++qt) step -= x;
 
   const typename L::LaneAt at = L::lane_at();
@@ -419,7 +423,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
   for (int64_t s = s0; s < s1;) {
     // one unit: steps [step, step + cnt) of its `all`
     const int all = decode_steps<D::kStep>(a, c, qt);
-    const int cnt = static_cast<int>(min<int64_t>(all - step, s1 - s));
+    const int cnt = whole ? all : static_cast<int>(min<int64_t>(all - step, s1 - s));
     const int r0 = qt * kDecodeRows, valid = min(kDecodeRows, c.m * a.group - r0);
     int lo, hi, alo, ahi, xlo, xhi;
     seen_by(a, c, r0, r0 + valid - 1, lo, hi);
@@ -449,17 +453,17 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
     }
 
     auto slot_of = [&](int t) __attribute__((always_inline)) { return j_first + t * NW * 32; };
-    Copies<T, DP, 32, 1> blocks;
+    Blocks<32> blocks;
     auto copy = [&](int t) __attribute__((always_inline)) {
       copy_tile<T, DP, 32, 1>(a.c, kb, vb, b, slot_of(t), lo, hi, blocks, a.d, 0,
                               ring3 + t % NST * D::kStage, ring3 + t % NST * D::kStage + kBytes);
-      fetch_blocks(a.c, b, slot_of(t + 1), hi, 0, blocks);
+      fetch_blocks(a.c, b, slot_of(t + 1), hi, blocks);
     };
     bool odd = false;
+    if (tiles > 0) fetch_blocks(a.c, b, slot_of(0), hi, blocks);
+    for (int t = 0; t < NST - 1 && t < tiles; ++t) copy(t);
     // the queries are here: the compiler must not wait for them in the loop
     __builtin_amdgcn_s_waitcnt(0);
-    if (tiles > 0) fetch_blocks(a.c, b, slot_of(0), hi, 0, blocks);
-    for (int t = 0; t < NST - 1 && t < tiles; ++t) copy(t);
     for (int t = 0; t < tiles; ++t) {
       // the stage that tile t + NST - 1 takes was read a tile ago
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -476,8 +480,26 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
       if (j0 >= alo && j0 + 32 <= ahi) {
         f32x16 sc[1] = {L::scores(k, at, q)};
         if constexpr (CAP) cap_scores(a, sc);
-        softmax_step(CAP ? 1.f : a.scale2, sc, st, acc);
-        L::template add_values<false>(v, at, sc[0], acc);
+        if constexpr (L::kBf16) {
+          // the first pieces of the values come beside the softmax
+          constexpr int kAhead = 2 * NB < 8 ? 2 * NB : 8;
+          bf16x8 vf[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) vf[i] = L::value_frag(v, at, i / NB, i % NB);
+          __builtin_amdgcn_sched_barrier(0);
+          softmax_step(CAP ? 1.f : a.scale2, sc, st, acc);
+          bf16x8 p[2];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e / 8][e % 8] = static_cast<__bf16>(sc[0][e]);
+#pragma unroll
+          for (int i = 0; i < 2 * NB; ++i) {
+            acc[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kAhead], p[i / NB], acc[i % NB], 0, 0, 0);
+            if (i + kAhead < 2 * NB) vf[i % kAhead] = L::value_frag(v, at, (i + kAhead) / NB, (i + kAhead) % NB);
+          }
+        } else {
+          softmax_step(CAP ? 1.f : a.scale2, sc, st, acc);
+          L::template add_values<false>(v, at, sc[0], acc);
+        }
       } else {
         odd |= edge_step<T, DP, CAP>(a, k, v, at, q, j0, qr.lo, qr.hi, st, acc);
       }
@@ -567,7 +589,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
       *head = JoinHead{static_cast<int32_t>((end - 1) / per - blockIdx.x + 1), valid, c.q0, r0, h,
                        static_cast<int32_t>(2 * blockIdx.x + 1), unseeing(a, c, r0)};
     }
-    s += cnt;
+    s += whole ? 1 : cnt;
     step = 0;
     if (s < s1) {
       // the next q tile, of this context or one with new tokens after it
@@ -645,6 +667,7 @@ hipError_t run_forward(const AttnArgs& a, const ForwardPlan& p, hipStream_t st) 
     const dim3 block(64 * Decode<T, DP>::kWaves);
     e = cap ? launch_on(forward_decode<T, DP, true>, dim3(p.grid), block, st, a, p)
             : launch_on(forward_decode<T, DP, false>, dim3(p.grid), block, st, a, p);
+    if (p.splits == 1) return e;
   } else {
     e = cap ? launch_on(forward_chunk<T, DP, true>, dim3(p.grid), dim3(256), st, a, p)
             : launch_on(forward_chunk<T, DP, false>, dim3(p.grid), dim3(256), st, a, p);

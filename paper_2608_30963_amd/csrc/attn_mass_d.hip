@@ -66,7 +66,7 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
   const int lane = threadIdx.x % 64, n = lane % 32, half = lane / 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   copy_rest(a);
-  const Share share = line_share<NW>(a, [&](int b) {
+  const Share share = line_share(a, [&](int b) {
     const int n = min(max(a.tokens[b], 0), min(a.c.capacity, a.mass_capacity));
     return static_cast<int64_t>((n + kStep - 1) / kStep);
   });
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
       // tiles that the rows see: from t0 to t1; the others keep their sums
       const int t0 = hi > lo && lo > j_first + 31 ? (lo - j_first - 32) / kStep + 1 : 0;
       const int t1 = hi > lo ? min(tiles, hi > j_first ? (hi - j_first + kStep - 1) / kStep : 0) : 0;
-      Copies<T, DP, 32, 1> blocks;
+      Blocks<32> blocks;
       const float* from = r0 > 0 ? a.mass : a.mass_in;
       const uint32_t earlier3 = lds_address(reinterpret_cast<const char*>(earlier[w]));
       auto copy = [&](int t) __attribute__((always_inline)) {
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
                 earlier3 + t % NST * 128);
         copy_tile<T, DP, 32, 1, true, false>(a.c, kb, nullptr, b, slot_of(t), lo, hi, blocks, a.d, 0,
                                              ring3 + t % NST * kStage, 0);
-        fetch_blocks(a.c, b, slot_of(t + 1), hi, 0, blocks);
+        fetch_blocks(a.c, b, slot_of(t + 1), hi, blocks);
       };
       auto put = [&](int t, float sum) __attribute__((always_inline)) {
         const int j = slot_of(t) + n;
@@ -134,10 +134,10 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
         for (int t = 0; t < tiles; ++t)
           if (t < t0 || t >= t1)
             put(t, a.mass_in ? a.mass_in[mrow + min(slot_of(t) + n, end - 1)] : 0.f);
+      if (t0 < t1) fetch_blocks(a.c, b, slot_of(t0), hi, blocks);
+      for (int t = t0; t < t0 + NST - 1 && t < t1; ++t) copy(t);
       // the queries are here: the compiler must not wait for them in the loop
       __builtin_amdgcn_s_waitcnt(0);
-      if (t0 < t1) fetch_blocks(a.c, b, slot_of(t0), hi, 0, blocks);
-      for (int t = t0; t < t0 + NST - 1 && t < t1; ++t) copy(t);
       for (int t = t0; t < t1; ++t) {
         // the stage that tile t + NST - 1 takes was read a tile ago
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

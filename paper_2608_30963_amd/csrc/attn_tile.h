@@ -113,22 +113,33 @@ struct Tile {
   // LDS row n's with the pieces' rows.
   template <bool SWAP = false>
   static __device__ __forceinline__ f32x16 scores(const char* k, const LaneAt& at, const uint4 (&q)[kQ]) {
+    // pieces are read kAhead matrix instructions before their use: the
+    // compiler alone reads them just before it and waits
+    constexpr int kAhead = kQ < 8 ? kQ : 8;
+    uint4 piece[kAhead];
+    auto read = [&](int i) __attribute__((always_inline)) {
+      piece[i % kAhead] =
+          *reinterpret_cast<const uint4*>(k + at.k[i % kKeyAt] + i / kKeyAt * kKeyAt * 32);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) read(i);
     f32x16 s;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
+      const uint4 x = piece[i % kAhead];
       if constexpr (kBf16) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + at.k[i % kKeyAt] + i / kKeyAt * kKeyAt * 32);
-        const bf16x8 b = __builtin_bit_cast(bf16x8, q[i]);
+        const bf16x8 a = __builtin_bit_cast(bf16x8, x), b = __builtin_bit_cast(bf16x8, q[i]);
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(SWAP ? b : a, SWAP ? a : b, s, 0, 0, 0);
       } else {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(k + at.k[i % kKeyAt] + i / kKeyAt * kKeyAt * 32);
-        const f32x4 b = __builtin_bit_cast(f32x4, q[i]);
+        const f32x4 a = __builtin_bit_cast(f32x4, x), b = __builtin_bit_cast(f32x4, q[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           s = __builtin_amdgcn_mfma_f32_32x32x2f32(SWAP ? b[e] : a[e], SWAP ? a[e] : b[e], s, 0, 0, 0);
       }
+      if (i + kAhead < kQ) read(i + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
     }
     return s;
   }
@@ -268,32 +279,22 @@ __device__ __forceinline__ void copy4(const char* from, uint32_t lds) {
                : "memory");
 }
 
-// Where the rows of a wave's copies start, of a tile of TK slots that WAVES
-// waves copy: the blocks, read by the scalar unit a tile ahead of their use.
-// One copy instruction moves kRowsPerCopy rows, which lie in one block where
-// runs of 8 slots do.
-template <typename T, int DP, int TK, int WAVES>
-struct Copies {
-  static constexpr int kN = TK * Tile<T, DP>::kRowBytes / 1024 / WAVES;  // keys or values
-  static constexpr int kRows = Tile<T, DP>::kRowsPerCopy;
-  int32_t id[kN];
+// The blocks of a tile's slots, one per 16: read by the scalar unit a tile
+// ahead of their use, where 16 slots, from a multiple of 16 on, lie in one
+// block.
+template <int TK>
+struct Blocks {
+  int32_t id[TK / 16];
 };
 
-template <typename T, int DP, int TK, int WAVES>
-__device__ __forceinline__ void fetch_blocks(const CacheArgs& c, int b, int j0, int hi, int w,
-                                             Copies<T, DP, TK, WAVES>& out) {
-  using C = Copies<T, DP, TK, WAVES>;
-  if (!c.table || c.run < 8) return;
+template <int TK>
+__device__ __forceinline__ void fetch_blocks(const CacheArgs& c, int b, int j0, int hi, Blocks<TK>& out) {
+  if (!c.table || c.run < 16) return;
   const __attribute__((address_space(4))) int32_t* t =
       (const __attribute__((address_space(4))) int32_t*)(c.table) +
       static_cast<int64_t>(b) * c.max_blocks;
-  if (c.run >= TK) {
-    out.id[0] = t[fdiv(c.bs, min(j0, hi - 1))];
-  } else {
 #pragma unroll
-    for (int i = 0; i < C::kN; ++i)
-      out.id[i] = t[fdiv(c.bs, min(j0 + (i * WAVES + w) * C::kRows, hi - 1))];
-  }
+  for (int k = 0; k < TK / 16; ++k) out.id[k] = t[fdiv(c.bs, min(j0 + 16 * k, hi - 1))];
 }
 
 // Copies rows j0 .. j0 + TK - 1 of a cache (keys at kb, values at vb of one
@@ -302,63 +303,78 @@ __device__ __forceinline__ void fetch_blocks(const CacheArgs& c, int b, int j0, 
 // nearest inside.
 template <typename T, int DP, int TK, int WAVES, bool KEYS = true, bool VALUES = true>
 __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, const char* vb, int b,
-                                          int j0, int lo, int hi,
-                                          const Copies<T, DP, TK, WAVES>& blocks, int d, int w,
+                                          int j0, int lo, int hi, const Blocks<TK>& blocks, int d, int w,
                                           uint32_t lk, uint32_t lv) {
   using L = Tile<T, DP>;
-  constexpr int kCopies = Copies<T, DP, TK, WAVES>::kN, R = L::kRowsPerCopy;
+  constexpr int R = L::kRowsPerCopy;                          // rows of a copy instruction
+  constexpr int kCopies = TK * L::kRowBytes / 1024 / WAVES;   // of a wave, keys or values
+  constexpr int kStep = WAVES * R;                            // rows from one to the wave's next
+  constexpr int kRun = kStep < 16 ? 16 / kStep : 1;           // of them in 16 slots
   const int lane = threadIdx.x % 64, sub = lane / L::kChunks;
   const uint32_t st = static_cast<uint32_t>(c.st) * sizeof(T);
-  // copy i moves rows (i WAVES + w) R + sub: the swizzle of its low bits is
-  // the lane's, that of the high ones a constant
+  // copy i moves rows i kStep + w R + sub: the swizzle of its low bits is the
+  // lane's, that of the high ones a constant
   const int low = w * R + sub, bytes = d * static_cast<int>(sizeof(T));
   const int ck = ((lane % L::kChunks) ^ L::key_swz(low)) * 16;
   const int cv = ((lane % L::kChunks) ^ L::value_swz(low)) * 16;
+  const int64_t sb = c.sb * static_cast<int64_t>(sizeof(T));
   if (kCopies <= 8 && j0 >= lo && j0 + TK <= hi && c.run >= TK && d == DP) {
     // the whole tile lies in one block, rows have all of DP: one base (not for
     // more copies, whose offsets would fill the registers)
     const int32_t id = c.table ? blocks.id[0] : b;
     const uint32_t slot = c.table ? j0 - fdiv(c.bs, j0) * c.bs.d : j0;
-    const int64_t at = id * (c.sb * static_cast<int64_t>(sizeof(T))) +
-                       static_cast<int64_t>(static_cast<uint64_t>(slot + w * R) * st);
+    const int64_t at = id * sb + static_cast<int64_t>(static_cast<uint64_t>(slot + w * R) * st);
     uint32_t off[kCopies];
     if constexpr (KEYS) {
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i)
-        off[i] = (i * WAVES * R + sub) * st + (ck ^ (L::key_swz(i * WAVES * R) * 16));
+      for (int i = 0; i < kCopies; ++i) off[i] = (i * kStep + sub) * st + (ck ^ (L::key_swz(i * kStep) * 16));
       copy16_run<kCopies, WAVES * 1024>(kb + at, off, lk + w * 1024);
     }
     if constexpr (VALUES) {
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i)
-        off[i] = (i * WAVES * R + sub) * st + (cv ^ (L::value_swz(i * WAVES * R) * 16));
+      for (int i = 0; i < kCopies; ++i) off[i] = (i * kStep + sub) * st + (cv ^ (L::value_swz(i * kStep) * 16));
       copy16_run<kCopies, WAVES * 1024>(vb + at, off, lv + w * 1024);
     }
-  } else if (j0 >= lo && j0 + TK <= hi && c.run >= 8) {
-    const int64_t sb = c.sb * static_cast<int64_t>(sizeof(T));
-    int64_t at[kCopies];
-    if (c.run >= TK) {
-      const int32_t id = c.table ? blocks.id[0] : b;
-      const uint32_t slot = c.table ? j0 - fdiv(c.bs, j0) * c.bs.d : j0;
-      const int64_t first = id * sb + static_cast<int64_t>(static_cast<uint64_t>(slot + w * R) * st);
+  } else if (j0 >= lo && j0 + TK <= hi && c.run >= 16) {
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i) at[i] = first + static_cast<int64_t>(i * WAVES * R) * st;
-    } else {
-#pragma unroll
-      for (int i = 0; i < kCopies; ++i) {
-        const int j = j0 + (i * WAVES + w) * R;
-        const uint32_t slot = j - fdiv(c.bs, j) * c.bs.d;
-        at[i] = blocks.id[i] * sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
+    for (int i = 0; i < kCopies; i += kRun) {
+      const int row = i * kStep + w * R, j = j0 + row;  // the first of kRun copies in one block
+      int32_t id = b;
+      uint32_t slot = j;
+      if (c.table) {
+        id = blocks.id[i * kStep / 16];
+        if constexpr (kStep > 16)
+          if (w * R >= 16) id = blocks.id[i * kStep / 16 + 1];
+        slot = j - fdiv(c.bs, j) * c.bs.d;
       }
-    }
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-      const int k = ck ^ (L::key_swz(i * WAVES * R) * 16), v = cv ^ (L::value_swz(i * WAVES * R) * 16);
+      const int64_t at = id * sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
       const uint32_t to = (i * WAVES + w) * 1024;
-      if constexpr (KEYS)
-        if (k < bytes) copy16(kb + at[i], sub * st + k, lk + to);
-      if constexpr (VALUES)
-        if (v < bytes) copy16(vb + at[i], sub * st + v, lv + to);
+      if constexpr (kRun > 1) {
+        if (d == DP) {
+          uint32_t off[kRun];
+          if constexpr (KEYS) {
+#pragma unroll
+            for (int x = 0; x < kRun; ++x)
+              off[x] = (x * kStep + sub) * st + (ck ^ (L::key_swz(x * kStep) * 16));
+            copy16_run<kRun, WAVES * 1024>(kb + at, off, lk + to);
+          }
+          if constexpr (VALUES) {
+#pragma unroll
+            for (int x = 0; x < kRun; ++x)
+              off[x] = (x * kStep + sub) * st + (cv ^ (L::value_swz(x * kStep) * 16));
+            copy16_run<kRun, WAVES * 1024>(vb + at, off, lv + to);
+          }
+          continue;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < kRun; ++x) {
+        const int k = ck ^ (L::key_swz((i + x) * kStep) * 16), v = cv ^ (L::value_swz((i + x) * kStep) * 16);
+        if constexpr (KEYS)
+          if (k < bytes) copy16(kb + at, (x * kStep + sub) * st + k, lk + to + x * WAVES * 1024);
+        if constexpr (VALUES)
+          if (v < bytes) copy16(vb + at, (x * kStep + sub) * st + v, lv + to + x * WAVES * 1024);
+      }
     }
   } else {
     // lane i finds row i's place
@@ -367,8 +383,8 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
     const uint32_t at_lo = static_cast<uint32_t>(at), at_hi = static_cast<uint32_t>(at >> 32);
 #pragma unroll 1
     for (int i = 0; i < kCopies; ++i) {
-      const int row = i * WAVES * R + low;
-      const int k = ck ^ (L::key_swz(i * WAVES * R) * 16), v = cv ^ (L::value_swz(i * WAVES * R) * 16);
+      const int row = i * kStep + low;
+      const int k = ck ^ (L::key_swz(i * kStep) * 16), v = cv ^ (L::value_swz(i * kStep) * 16);
       const int64_t o = static_cast<int64_t>(static_cast<uint64_t>(__shfl(at_hi, row)) << 32 |
                                              __shfl(at_lo, row));
       const uint32_t to = (i * WAVES + w) * 1024;
@@ -414,38 +430,27 @@ struct Share {
   int h, b, step;  // where s0 lies
 };
 
-// Found by all NW waves together; every thread of the workgroup calls it.
-template <int NW, typename Steps>
+// Inclusive sum over a wave's lanes.
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+  const int lane = threadIdx.x % 64;
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) {
+    const int64_t y = __shfl_up(x, i);
+    if (lane >= i) x += y;
+  }
+  return x;
+}
+
+// Found by every wave for itself, 64 contexts at a time (a launch of few
+// contexts waits for no barrier); the waves' results are the same.
+template <typename Steps>
 __device__ __forceinline__ Share line_share(const AttnArgs& a, Steps steps_of) {
-  constexpr int NT = 64 * NW;
-  __shared__ int64_t scan[NW];
-  __shared__ int found[2];
-  const int tid = threadIdx.x, lane = tid % 64, w = tid / 64;
-  auto before_of = [&](int64_t x, int64_t& total) __attribute__((always_inline)) {
-    int64_t s = x;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const int64_t y = __shfl_up(s, i);
-      if (lane >= i) s += y;
-    }
-    __syncthreads();
-    if (lane == 63) scan[w] = s;
-    __syncthreads();
-    int64_t base = 0;
-    total = 0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      if (i < w) base += scan[i];
-      total += scan[i];
-    }
-    return base + s - x;
-  };
-  int64_t line = 0, mine = 0, before = 0;  // line: of one head
-  for (int b0 = 0; b0 < a.batch; b0 += NT) {
-    int64_t total;
-    mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
-    before = before_of(mine, total);
-    line += total;
+  const int lane = threadIdx.x % 64;
+  int64_t line = 0, mine = 0, upto = 0;  // line: of one head
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    mine = b0 + lane < a.batch ? steps_of(b0 + lane) : 0;
+    upto = wave_sum(mine);
+    line += __shfl(upto, 63);
   }
   Share sh{};
   const int64_t whole = line * a.hkv;
@@ -453,31 +458,22 @@ __device__ __forceinline__ Share line_share(const AttnArgs& a, Steps steps_of) {
   sh.s0 = min<int64_t>(whole, blockIdx.x * sh.per);
   sh.s1 = min(whole, sh.s0 + sh.per);
   if (sh.s0 >= sh.s1) return sh;
-  sh.h = static_cast<int>(sh.s0 / line);
-  const int64_t into = sh.s0 - sh.h * line;
-  if (a.batch <= NT) {
-    if (before <= into && into < before + mine) {
-      found[0] = tid;
-      found[1] = static_cast<int>(into - before);
+  sh.h = __builtin_amdgcn_readfirstlane(static_cast<int>(sh.s0 / line));
+  int64_t into = sh.s0 - sh.h * line;
+  for (int b0 = 0;; b0 += 64) {
+    if (a.batch > 64) {
+      mine = b0 + lane < a.batch ? steps_of(b0 + lane) : 0;
+      upto = wave_sum(mine);
     }
-  } else {
-    int64_t past = 0;
-    for (int b0 = 0; b0 < a.batch && past <= into; b0 += NT) {
-      int64_t total;
-      mine = b0 + tid < a.batch ? steps_of(b0 + tid) : 0;
-      before = past + before_of(mine, total);
-      if (before <= into && into < before + mine) {
-        found[0] = b0 + tid;
-        found[1] = static_cast<int>(into - before);
-      }
-      past += total;
+    const uint64_t past = __ballot(upto > into);
+    if (past) {
+      const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      sh.b = __builtin_amdgcn_readfirstlane(b0 + f);
+      sh.step = __builtin_amdgcn_readfirstlane(static_cast<int>(into - (__shfl(upto, f) - __shfl(mine, f))));
+      return sh;
     }
+    into -= __shfl(upto, 63);
   }
-  __syncthreads();
-  sh.b = __builtin_amdgcn_readfirstlane(found[0]);
-  sh.step = __builtin_amdgcn_readfirstlane(found[1]);
-  sh.h = __builtin_amdgcn_readfirstlane(sh.h);
-  return sh;
 }
 
 // Waves and stages of the rings of 32-slot tiles that a workgroup holds in LDS
