@@ -74,8 +74,9 @@ struct AttnArgs {
   int32_t batch, rows, hq, hkv, group, d;
   FastDiv by_group;        // division by group
   int32_t window;          // 0: none
-  float scale2;            // score scale * log2(e); with a cap scale / cap
+  float scale2;            // score scale * log2(e)
   float cap2;              // cap * log2(e), 0: none
+  float tanh2;             // 2 scale / cap * log2(e)
   const char* q;           // forward, mass
   int64_t q_sr, q_sh;      // elements
   char* out;
@@ -110,12 +111,15 @@ __device__ __forceinline__ int end_seen(const Context& c, int p) {
   return p < 0 ? 0 : max(p + 1, c.prefix);
 }
 
-// Score in units of log2: x is the dot product q.k.  tanh(y) = 1 - 2 / (1 +
-// exp(2y)); its absolute error is that of 1, 2^-24, times the cap.
+// The r of a capped score: tanh(y) = 1 - 2 r, r = 1 / (1 + exp(2 y)).  Its
+// absolute error, as that of 1 - 2 r, is 2^-24 or so, times the cap.
+__device__ __forceinline__ float cap_part(const AttnArgs& a, float x) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * a.tanh2));
+}
+
+// Score in units of log2: x is the dot product q.k.
 __device__ __forceinline__ float score2(const AttnArgs& a, float x) {
-  if (a.cap2 == 0.f) return x * a.scale2;
-  const float e = __builtin_amdgcn_exp2f(x * a.scale2 * 2.885390081777927f);
-  return a.cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + e));
+  return a.cap2 == 0.f ? x * a.scale2 : __builtin_fmaf(-2.f * a.cap2, cap_part(a, x), a.cap2);
 }
 
 // Launchers; each returns the launch's own status.

@@ -111,8 +111,9 @@ kvx_status prepare(const kvx_attn* at, const kvx_attn_io* io, AttnArgs& a) {
   a.d = at->model.head_dim;
   a.window = io->window;
   const double log2e = 1.4426950408889634;
-  a.scale2 = static_cast<float>(at->softcap > 0.0 ? at->scale / at->softcap : at->scale * log2e);
+  a.scale2 = static_cast<float>(at->scale * log2e);
   a.cap2 = static_cast<float>(at->softcap * log2e);
+  a.tanh2 = at->softcap > 0.0 ? static_cast<float>(2.0 * at->scale / at->softcap * log2e) : 0.f;
   a.q = static_cast<const char*>(io->q);
   a.q_sr = io->q_stride[0];
   a.q_sh = io->q_stride[1];

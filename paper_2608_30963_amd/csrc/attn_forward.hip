@@ -13,6 +13,27 @@ int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // workgroups than the compute units take some of those would idle.
 int64_t most_pieces(const kvx_attn* at) { return 2 * int64_t(at->n_cu); }
 
+// Workgroups of the chunk kernel that a compute unit takes at once.
+int resident(const kvx_attn* at) {
+  return padded_dim(at->model.head_dim) * (at->dtype == KVX_F32 ? 4 : 2) <= 256 ? 2 : 1;
+}
+
+// Pieces of a unit: each costs a share of the unit and some 3% of it to start
+// and to join, and the card takes so many workgroups at a time.
+int splits_of(const kvx_attn* at, int64_t units) {
+  const int64_t slots = int64_t(at->n_cu) * resident(at);
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= 16 && (s == 1 || units * s <= most_pieces(at)); ++s) {
+    const double cost = double((units * s + slots - 1) / slots) * (1.0 / s + 0.03);
+    if (cost < least) {
+      least = cost;
+      best = s;
+    }
+  }
+  return best;
+}
+
 size_t head_bytes(const kvx_attn* at) { return (most_pieces(at) * sizeof(JoinHead) + 255) / 256 * 256; }
 
 }  // namespace
@@ -42,7 +63,7 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
                            std::min(a.batch, a.rows);
     const int64_t units = strips * a.hkv;
     p.join_rows = kChunkRows;
-    p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(16, most_pieces(at) / units)));
+    p.splits = splits_of(at, units);
     if (units * p.splits > INT32_MAX) return hipErrorInvalidValue;
     p.strips = static_cast<int>(strips);
     p.grid = static_cast<int>(units * p.splits);

@@ -40,15 +40,16 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const QueryRow& q, 
 }
 
 // ---------------------------------------------------------------------------
-// Chunks: 4 waves of 32 query rows share tiles of 64 slots (32 where rows
-// are of 1024 bytes), copied straight into LDS ahead of their use: keys two
-// tiles, into one of three buffers, values one, into one of two.  One barrier
-// per tile.  The scores of tile t + 1 are formed beside the weights of tile t,
+// Chunks: 4 waves of 32 query rows share tiles of 64 slots (32 where rows have
+// over 256 bytes), copied straight into LDS ahead of their use: values DEPTH
+// tiles, keys one more.  One barrier per tile.  Depth 2 where one workgroup
+// fills a compute unit, so that no other one hides the copies' latency, and
+// LDS has room.  The scores of tile t + 1 are formed beside the weights of tile t,
 // which need other units of the compute unit.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP>
-constexpr int chunk_tile() { return DP * sizeof(T) <= 512 ? 64 : 32; }
+constexpr int chunk_tile() { return DP * sizeof(T) <= 256 ? 64 : 32; }
 
 // One turn of the chunk kernel's middle loop: the scores `next` of the tile
 // whose keys are at k, the weights of the scores s, their products with the
@@ -66,13 +67,16 @@ __device__ __forceinline__ void middle_turn(const AttnArgs& a, const char* k, co
                                             f32x16 (&s)[NS], f32x16 (&next)[NS], Softmax& st,
                                             f32x16 (&acc)[DP / 32], float& top) {
   using L = Tile<T, DP>;
-  static_assert(L::kBf16 && NS == 2, "two groups of slots, bf16");
+  static_assert(L::kBf16, "");
   constexpr int KQ = L::kQ, kSteps = NS * KQ, kAheadK = 6, kAheadV = 4, NB = DP / 32;
   constexpr int kWeights = 16 * NS, kBeside = kWeights * 3 / 4, kLater = kWeights - kBeside;
   static_assert(2 * NS * NB == kSteps, "");
   uint4 kf[kAheadK + 1];
   bf16x8 vf[kAheadV + 1], b;
-  const float ref = st.m2 == -INFINITY ? 0.f : -st.m2;
+  // scores in log2 units less the reference: scale * s + shift.  Capped ones
+  // are kept as the r of cap_part, which the line cap2 (1 - 2 r) brings there
+  const float scale = CAP ? -2.f * a.cap2 : c2;
+  const float shift = (CAP ? a.cap2 : 0.f) + (st.m2 == -INFINITY ? 0.f : -st.m2);
   float sum[2] = {0.f, 0.f};
   auto read_key = [&](int i) __attribute__((always_inline)) {
     kf[i % (kAheadK + 1)] = *reinterpret_cast<const uint4*>(
@@ -84,7 +88,7 @@ __device__ __forceinline__ void middle_turn(const AttnArgs& a, const char* k, co
   auto weigh = [&](int from, int to) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = from; e < to; ++e) {
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 16][e % 16], c2, ref));
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 16][e % 16], scale, shift));
       s[e / 16][e % 16] = p;
       sum[e % 2] += p;
     }
@@ -119,14 +123,17 @@ __device__ __forceinline__ void middle_turn(const AttnArgs& a, const char* k, co
 #pragma unroll
     for (int e = kWeights * j / kSteps; e < kWeights * (j + 1) / kSteps; ++e) {
       float x = next[e / 16][e % 16];
-      if constexpr (CAP) next[e / 16][e % 16] = x = score2(a, x);
-      top = e == 0 ? x : fmaxf(top, x);
+      if constexpr (CAP) next[e / 16][e % 16] = x = cap_part(a, x);
+      top = e == 0 ? x : CAP ? fminf(top, x) : fmaxf(top, x);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  top = half_max(top) * c2;
+  top = CAP ? a.cap2 - 2.f * a.cap2 * -half_max(-top) : half_max(top) * c2;
   st.l += sum[0] + sum[1];
 }
+
+template <typename T, int DP>
+constexpr int chunk_depth() { return DP * sizeof(T) == 512 ? 2 : 1; }
 
 template <typename T, int DP, bool CAP>
 __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
@@ -134,7 +141,9 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   using L = Tile<T, DP>;
   constexpr int TK = chunk_tile<T, DP>(), NS = TK / 32, NB = DP / 32;
   constexpr int kBytes = TK * L::kRowBytes;  // keys or values of a tile
-  __shared__ __attribute__((aligned(16))) char lds[5 * kBytes];  // 3 of keys, 2 of values
+  constexpr int kDepth = chunk_depth<T, DP>(), kKeys = kDepth + 2, kValues = kDepth + 1;
+  constexpr int kCopies = kBytes / 1024 / 4;  // of a wave, keys or values
+  __shared__ __attribute__((aligned(16))) char lds[(kKeys + kValues) * kBytes];
   const int lane = threadIdx.x % 64, n = lane % 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 
@@ -205,7 +214,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.f;
 
   if (a.d < DP) {
-    for (int i = threadIdx.x; i < 5 * kBytes / 16; i += 256)
+    for (int i = threadIdx.x; i < (kKeys + kValues) * kBytes / 16; i += 256)
       reinterpret_cast<uint4*>(lds)[i] = uint4{0, 0, 0, 0};
     __syncthreads();
   }
@@ -223,15 +232,18 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     vblocks = kblocks;
     fetch_blocks(a.c, b, t * TK + TK, hi, kblocks);
   };
-  auto copy_values = [&](int t) __attribute__((always_inline)) {
+  auto copy_values = [&](int t, int slot) __attribute__((always_inline)) {
     copy_tile<T, DP, TK, 4, false, true>(a.c, kb, vb, b, t * TK, lo, hi, vblocks, a.d, w, 0,
-                                         l3 + (3 + ((t - t0) & 1)) * kBytes);
+                                         l3 + (kKeys + slot) * kBytes);
   };
   if (t0 < t1) {
     fetch_blocks(a.c, b, t0 * TK, hi, kblocks);
     copy_keys(t0, 0);
-    copy_values(t0);
-    if (t0 + 1 < t1) copy_keys(t0 + 1, 1);
+#pragma unroll
+    for (int i = 0; i < kDepth; ++i) {
+      if (t0 + i < t1) copy_values(t0 + i, i);
+      if (t0 + i + 1 < t1) copy_keys(t0 + i + 1, i + 1);
+    }
   }
   // Three loops, so that the one that matters has few registers to keep: tiles
   // before the first that all of the wave's queries see (windows), tiles that
@@ -239,21 +251,27 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   // first of its tiles gives; should a score ever pass it by 2^kRoom, the last
   // loop goes on, which moves it.
   const float c2 = CAP ? 1.f : a.scale2;
-  int slot = 0;  // of tile t's keys
-  auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
+  int kslot = 0, vslot = 0;  // of tile t
+  auto after = [](int slot, int n, int by) { return slot + by >= n ? slot + by - n : slot + by; };
   auto arrive = [&](int t) __attribute__((always_inline)) {
-    // tile t's values and tile t + 1's keys have landed, and every wave is done
-    // with tile t - 1
-    vm_wait<0>();
+    // tile t's values and tile t + 1's keys have landed, those of kDepth - 1
+    // more tiles may be in flight, and every wave is done with tile t - 1
+    if (t + kDepth < t1)
+      vm_wait<(kDepth - 1) * 2 * kCopies>();
+    else
+      vm_wait<0>();
     tile_barrier();
-    if (t + 1 < t1) copy_values(t + 1);
-    if (t + 2 < t1) copy_keys(t + 2, after(after(slot)));
+    if (t + kDepth < t1) copy_values(t + kDepth, after(vslot, kValues, kDepth));
+    if (t + kDepth + 1 < t1) copy_keys(t + kDepth + 1, after(kslot, kKeys, kDepth + 1));
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto values_of = [&](int t) { return lds + (3 + ((t - t0) & 1)) * kBytes; };
+  auto next_slots = [&]() __attribute__((always_inline)) {
+    kslot = after(kslot, kKeys, 1);
+    vslot = after(vslot, kValues, 1);
+  };
   auto edges = [&](int t) __attribute__((always_inline)) {
     if (t * TK >= whi || t * TK + TK <= wlo) return;
-    const char *k = lds + slot * kBytes, *v = values_of(t);
+    const char *k = lds + kslot * kBytes, *v = lds + (kKeys + vslot) * kBytes;
     // 32 slots at a time: the masks and checks want registers too
 #pragma unroll 1
     for (int u = 0; u < NS; ++u)
@@ -264,7 +282,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   for (; t < t1 && t * TK < alo; ++t) {
     arrive(t);
     edges(t);
-    slot = after(slot);
+    next_slots();
   }
   const int tm = min(t1, ahi / TK);
   bool here = false;  // tile t has landed
@@ -275,28 +293,42 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
       const char* k = lds + slot * kBytes;
 #pragma unroll
       for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, at, q);
-      if constexpr (CAP) cap_scores(a, s);
-      top = top_score(c2, s);
+      if constexpr (!CAP) {
+        top = top_score(c2, s);
+      } else {
+        f32x16 x[NS];
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            s[u][v] = cap_part(a, s[u][v]);
+            x[u][v] = -s[u][v];
+          }
+        top = a.cap2 + top_score(2.f * a.cap2, x);
+      }
     };
     arrive(t);
-    score(slot, s);
+    score(kslot, s);
     rescale(st, top, acc);
     while (true) {
       // the scores of tile t are within reach of the reference.  (After the
       // last tile the next one's are formed of what LDS holds, and not used.)
       f32x16 next[NS];
-      const char *k = lds + after(slot) * kBytes, *v = values_of(t);
+      const char *k = lds + after(kslot, kKeys, 1) * kBytes, *v = lds + (kKeys + vslot) * kBytes;
       if constexpr (L::kBf16) {
         middle_turn<T, DP, CAP, NS>(a, k, v, at, q, c2, s, next, st, acc, top);
       } else {
-        score(after(slot), next);
+        score(after(kslot, kKeys, 1), next);
 #pragma unroll
         for (int u = 0; u < NS; ++u) {
+          if constexpr (CAP)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) s[u][x] = a.cap2 - 2.f * a.cap2 * s[u][x];
           weights(c2, s[u], st);
           L::template add_values<false>(v + u * 32 * L::kRowBytes, at, s[u], acc);
         }
       }
-      slot = after(slot);
+      next_slots();
       if (++t == tm) break;
       arrive(t);
       here = exceeds(st, top, kRoom);
@@ -309,7 +341,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     if (!here) arrive(t);
     here = false;
     edges(t);
-    slot = after(slot);
+    next_slots();
   }
 
   const int unit = h * fp.strips + strip;
@@ -606,16 +638,18 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
   }
 }
 
-// Joins the pieces of units: a workgroup per query row, wave w the pieces w,
-// w + 4, .., whose sums are then added in the waves' order.
-template <typename T, int DP>
+// Joins the pieces of units: W waves a query row, wave w the pieces w, w + W,
+// .., whose sums are then added in the waves' order.  Four for single tokens,
+// whose few rows have many pieces; one for chunks.
+template <typename T, int DP, int W>
 __global__ void __launch_bounds__(256) forward_join(AttnArgs a, ForwardPlan fp) {
   constexpr int PER = DP / 64;
   __shared__ float sums[4][DP];
   __shared__ float part_l[4];
   const JoinHead hd = fp.heads[blockIdx.x];
-  const int r = blockIdx.y, lane = threadIdx.x % 64, w = threadIdx.x / 64;
-  if (r >= hd.rows || hd.pieces == 0) return;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, w = wave % W;
+  const int r = blockIdx.y * (4 / W) + wave / W;
+  if (hd.pieces == 0 || blockIdx.y * (4 / W) >= hd.rows) return;
   const int unit_rows = fp.decode ? kDecodeRows : kChunkRows;
   const size_t size = piece_floats(unit_rows, DP);
   // decode: piece 0 is slot 1 of its workgroup, the others slot 0 of the next ones
@@ -623,38 +657,48 @@ __global__ void __launch_bounds__(256) forward_join(AttnArgs a, ForwardPlan fp) 
     const size_t at = fp.decode ? (p == 0 ? hd.first : hd.first - 1 + 2 * static_cast<size_t>(p)) : hd.first + p;
     return fp.pieces + at * size;
   };
+  const int rc = min(r, hd.rows - 1);  // rows past the last one are not stored
   float m2 = -INFINITY;
-  for (int p = lane; p < hd.pieces; p += 64) m2 = fmaxf(m2, reinterpret_cast<const float2*>(piece(p))[r].x);
+  for (int p = lane; p < hd.pieces; p += 64) m2 = fmaxf(m2, reinterpret_cast<const float2*>(piece(p))[rc].x);
 #pragma unroll
   for (int i = 32; i; i >>= 1) m2 = fmaxf(m2, __shfl_xor(m2, i));
   float l = 0.f, o[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[i] = 0.f;
 #pragma unroll 8
-  for (int p = w; p < hd.pieces; p += 4) {
+  for (int p = w; p < hd.pieces; p += W) {
     const float* part = piece(p);
-    const float2 ml = reinterpret_cast<const float2*>(part)[r];
-    const float* x = part + 2 * unit_rows + static_cast<size_t>(r) * DP + lane * PER;
+    const float2 ml = reinterpret_cast<const float2*>(part)[rc];
+    const float* x = part + 2 * unit_rows + static_cast<size_t>(rc) * DP + lane * PER;
     const float f = ml.x == m2 ? 1.f : __builtin_amdgcn_exp2f(ml.x - m2);
     l += f * ml.y;
 #pragma unroll
     for (int i = 0; i < PER; ++i) o[i] += f * x[i];
   }
+  if constexpr (W > 1) {
+    static_assert(W == 4, "the waves of a workgroup");
 #pragma unroll
-  for (int i = 0; i < PER; ++i) sums[w][lane * PER + i] = o[i];
-  if (lane == 0) part_l[w] = l;
-  __syncthreads();
+    for (int i = 0; i < PER; ++i) sums[w][lane * PER + i] = o[i];
+    if (lane == 0) part_l[w] = l;
+    __syncthreads();
+    if (w > 0) return;
+    l = (part_l[0] + part_l[1]) + (part_l[2] + part_l[3]);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = lane * PER + i;
+      o[i] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+    }
+  }
+  if (r >= hd.rows) return;
   const int rr = hd.g0 + r, tok = fdiv(a.by_group, rr), g = rr - tok * a.group;
   const int64_t row = hd.row0 + tok;
   const int head = hd.h * a.group + g;
   const bool sees = r >= hd.empty;
-  const float all = (part_l[0] + part_l[1]) + (part_l[2] + part_l[3]);
-  const int e = threadIdx.x;
-  if (e < a.d) {
-    const float x = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
-    (reinterpret_cast<T*>(a.out) + row * a.o_sr + head * a.o_sh)[e] = store_cvt<T>(sees ? x / all : 0.f);
-  }
-  if (a.lse && e == 0) a.lse[row * a.hq + head] = sees ? (m2 + __builtin_amdgcn_logf(all)) * kLn2 : -INFINITY;
+  T* to = reinterpret_cast<T*>(a.out) + row * a.o_sr + head * a.o_sh;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (lane * PER + i < a.d) to[lane * PER + i] = store_cvt<T>(sees ? o[i] / l : 0.f);
+  if (a.lse && lane == 0) a.lse[row * a.hq + head] = sees ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 }  // namespace
@@ -674,8 +718,8 @@ hipError_t run_forward(const AttnArgs& a, const ForwardPlan& p, hipStream_t st) 
     if (p.splits == 1) return e;
   }
   if (e != hipSuccess) return e;
-  const int units = p.decode ? p.grid : p.strips * a.hkv;
-  return launch_on(forward_join<T, DP>, dim3(units, p.join_rows), dim3(256), st, a, p);
+  return p.decode ? launch_on(forward_join<T, DP, 4>, dim3(p.grid, p.join_rows), dim3(256), st, a, p)
+                  : launch_on(forward_join<T, DP, 1>, dim3(p.strips * a.hkv, p.join_rows / 4), dim3(256), st, a, p);
 }
 
 template hipError_t run_forward<float, KVX_ATTN_DP>(const AttnArgs&, const ForwardPlan&, hipStream_t);
