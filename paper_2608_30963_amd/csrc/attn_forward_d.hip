@@ -486,19 +486,24 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
 
     auto slot_of = [&](int t) __attribute__((always_inline)) { return j_first + t * NW * 32; };
     Blocks<32> blocks;
+    // block numbers are asked for where no wait for LDS follows soon: such a
+    // wait covers scalar loads too
     auto copy = [&](int t) __attribute__((always_inline)) {
       copy_tile<T, DP, 32, 1>(a.c, kb, vb, b, slot_of(t), lo, hi, blocks, a.d, 0,
                               ring3 + t % NST * D::kStage, ring3 + t % NST * D::kStage + kBytes);
-      fetch_blocks(a.c, b, slot_of(t + 1), hi, blocks);
     };
     bool odd = false;
     if (tiles > 0) fetch_blocks(a.c, b, slot_of(0), hi, blocks);
-    for (int t = 0; t < NST - 1 && t < tiles; ++t) copy(t);
+    for (int t = 0; t < NST - 1 && t < tiles; ++t) {
+      copy(t);
+      fetch_blocks(a.c, b, slot_of(t + 1), hi, blocks);
+    }
     // the queries are here: the compiler must not wait for them in the loop
     __builtin_amdgcn_s_waitcnt(0);
     for (int t = 0; t < tiles; ++t) {
-      // the stage that tile t + NST - 1 takes was read a tile ago
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      // the stage that tile t + NST - 1 takes was read a tile ago, its values
+      // used before this line
+      __builtin_amdgcn_sched_barrier(0);
       if (t + NST - 1 < tiles) {
         copy(t + NST - 1);
         // all but the last NST - 1 tiles' copies have landed
@@ -535,6 +540,8 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
       } else {
         odd |= edge_step<T, DP, CAP>(a, k, v, at, q, j0, qr.lo, qr.hi, st, acc);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      fetch_blocks(a.c, b, slot_of(t + NST), hi, blocks);
     }
 
     // the waves' results through LDS: each in its own ring, rows of DP floats,

@@ -22,30 +22,34 @@ __device__ __forceinline__ void copy_rest(const AttnArgs& a) {
   }
 }
 
-// Sum of the weights of the lane's slot over its 16 rows; lse2 holds the rows'
-// log-sum-exp in log2 units, +inf for rows that are not there.
+// exp2(score - lse) of one score: `less` is -lse in log2 units, with a cap plus
+// the cap (the score is cap2 - 2 cap2 r then); -inf for rows that are not there.
 template <bool CAP>
-__device__ __forceinline__ float weigh(const AttnArgs& a, const f32x16& s, const float (&lse2)[16]) {
+__device__ __forceinline__ float weight_of(const AttnArgs& a, float x, float less) {
+  return __builtin_amdgcn_exp2f(CAP ? __builtin_fmaf(-2.f * a.cap2, cap_part(a, x), less)
+                                    : __builtin_fmaf(x, a.scale2, less));
+}
+
+// Sum of the weights of the lane's slot over its 16 rows.
+template <bool CAP>
+__device__ __forceinline__ float weigh(const AttnArgs& a, const f32x16& s, const float (&less)[16]) {
   float sum[2] = {0.f, 0.f};
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const float x = CAP ? score2(a, s[v]) - lse2[v] : __builtin_fmaf(s[v], a.scale2, -lse2[v]);
-    sum[v % 2] += __builtin_amdgcn_exp2f(x);
-  }
+  for (int v = 0; v < 16; ++v) sum[v % 2] += weight_of<CAP>(a, s[v], less[v]);
   return sum[0] + sum[1];
 }
 
 // The same where rows may not see the lane's slot j; r0 is the first row.
 template <bool CAP>
 __device__ __forceinline__ float weigh_seen(const AttnArgs& a, const Context& c, const f32x16& s,
-                                            const float (&lse2)[16], int r0, int j) {
+                                            const float (&less)[16], int r0, int j) {
   const int h = threadIdx.x % 64 / 32;
   float sum = 0.f;
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
     const QueryRow q = query_row(a, c, r0 + 8 * (v / 4) + 4 * h + v % 4);
-    const float x = CAP ? score2(a, s[v]) - lse2[v] : __builtin_fmaf(s[v], a.scale2, -lse2[v]);
-    if (j >= q.lo && j < q.hi) sum += __builtin_amdgcn_exp2f(x);
+    const float p = weight_of<CAP>(a, s[v], less[v]);
+    if (j >= q.lo && j < q.hi) sum += p;
   }
   return sum;
 }
@@ -104,13 +108,13 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
       uint4 q[L::kQ];
       const T* qp = reinterpret_cast<const T*>(a.q) + qr.row * a.q_sr + (h * a.group + qr.g) * a.q_sh;
       L::load_q(q, n < valid ? qp : nullptr, a.d);
-      float lse2[16];
+      float less[16];
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const QueryRow u = query_row(a, c, r0 + 8 * (v / 4) + 4 * half + v % 4);
-        lse2[v] = u.lo < u.hi
-                      ? a.lse[static_cast<int64_t>(u.row) * a.hq + h * a.group + u.g] * kLog2e
-                      : INFINITY;
+        less[v] = u.lo < u.hi
+                      ? a.cap2 - a.lse[static_cast<int64_t>(u.row) * a.hq + h * a.group + u.g] * kLog2e
+                      : -INFINITY;
       }
       // tiles that the rows see: from t0 to t1; the others keep their sums
       const int t0 = hi > lo && lo > j_first + 31 ? (lo - j_first - 32) / kStep + 1 : 0;
@@ -124,7 +128,6 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
                 earlier3 + t % NST * 128);
         copy_tile<T, DP, 32, 1, true, false>(a.c, kb, nullptr, b, slot_of(t), lo, hi, blocks, a.d, 0,
                                              ring3 + t % NST * kStage, 0);
-        fetch_blocks(a.c, b, slot_of(t + 1), hi, blocks);
       };
       auto put = [&](int t, float sum) __attribute__((always_inline)) {
         const int j = slot_of(t) + n;
@@ -135,12 +138,16 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
           if (t < t0 || t >= t1)
             put(t, a.mass_in ? a.mass_in[mrow + min(slot_of(t) + n, end - 1)] : 0.f);
       if (t0 < t1) fetch_blocks(a.c, b, slot_of(t0), hi, blocks);
-      for (int t = t0; t < t0 + NST - 1 && t < t1; ++t) copy(t);
+      for (int t = t0; t < t0 + NST - 1 && t < t1; ++t) {
+        copy(t);
+        fetch_blocks(a.c, b, slot_of(t + 1), hi, blocks);
+      }
       // the queries are here: the compiler must not wait for them in the loop
       __builtin_amdgcn_s_waitcnt(0);
       for (int t = t0; t < t1; ++t) {
-        // the stage that tile t + NST - 1 takes was read a tile ago
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        // the stage that tile t + NST - 1 takes was read a tile ago, its values
+        // used before this line
+        __builtin_amdgcn_sched_barrier(0);
         if (t + NST - 1 < t1) {
           copy(t + NST - 1);
           vm_wait<(NST - 1) * kCopies>();
@@ -150,9 +157,11 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
         const int j0 = slot_of(t);
         const f32x16 sc = L::template scores<true>(ring + t % NST * kStage, at, q);
         const float sum = half_sum(j0 >= alo && j0 + 32 <= ahi
-                                       ? weigh<CAP>(a, sc, lse2)
-                                       : weigh_seen<CAP>(a, c, sc, lse2, r0, j0 + n));
+                                       ? weigh<CAP>(a, sc, less)
+                                       : weigh_seen<CAP>(a, c, sc, less, r0, j0 + n));
         put(t, (from ? earlier[w][t % NST][n] : 0.f) + sum);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_blocks(a.c, b, slot_of(t + NST), hi, blocks);
       }
       vm_wait<0>();  // the next pass reads these sums
     }
@@ -174,8 +183,8 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
 // ---------------------------------------------------------------------------
 // Chunks: 8 waves, QW of them over the query rows and 8 / QW over the slots,
 // 32 each.  The slots' keys stay in registers; stages of 32 QW query rows and
-// their log-sum-exps are copied into one of two LDS buffers while the other is
-// computed on.
+// their log-sum-exps are copied into LDS as many stages ahead of their use as
+// 128 KB hold: a stage is less work than a copy's latency.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP, bool CAP, int QW>
@@ -183,9 +192,10 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
   using L = Tile<T, DP>;
   constexpr int KW = 8 / QW, kRows = 32 * QW, kBytes = kRows * L::kRowBytes;
   constexpr int kCopies = kBytes / 1024 / 8;  // of a wave
+  constexpr int kBuffers = 131072 / kBytes < 4 ? 131072 / kBytes : 4;
   constexpr int R = L::kRowsPerCopy;
-  __shared__ __attribute__((aligned(16))) char lds[2 * kBytes];
-  __shared__ __attribute__((aligned(16))) float lse[2][kRows];
+  __shared__ __attribute__((aligned(16))) char lds[kBuffers * kBytes];
+  __shared__ __attribute__((aligned(16))) float lse[kBuffers][kRows];
   const int lane = threadIdx.x % 64, n = lane % 32, half = lane / 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int qw = w % QW, kw = w / QW;
@@ -217,7 +227,7 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
   }
   const typename L::LaneAt at = L::lane_at();
   if (a.d < DP) {
-    for (int i = threadIdx.x; i < 2 * kBytes / 16; i += 512)
+    for (int i = threadIdx.x; i < kBuffers * kBytes / 16; i += 512)
       reinterpret_cast<uint4*>(lds)[i] = uint4{0, 0, 0, 0};
   }
   __builtin_amdgcn_s_waitcnt(0);
@@ -243,31 +253,36 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
     }
   };
   float sum = 0.f;
-  if (stages > 0) copy_stage(0, 0);
+  for (int s = 0; s < kBuffers - 1 && s < stages; ++s) copy_stage(s, s);
   for (int s = 0; s < stages; ++s) {
-    const int buf = s & 1;
-    vm_wait<0>();
+    const int buf = s % kBuffers;
+    // this stage has landed, kBuffers - 2 more may be in flight, and every wave
+    // is done with the one before
+    if (s + kBuffers - 2 < stages)
+      vm_wait<(kBuffers - 2) * kCopies>();
+    else
+      vm_wait<0>();
     tile_barrier();
-    if (s + 1 < stages) copy_stage(s + 1, buf ^ 1);
+    if (s + kBuffers - 1 < stages) copy_stage(s + kBuffers - 1, (s + kBuffers - 1) % kBuffers);
     const int r0 = r_first + s * kRows + qw * 32;
     if (r0 >= r_end) continue;
-    float lse2[16];
+    float less[16];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const f32x4 y = *reinterpret_cast<const f32x4*>(&lse[buf][qw * 32 + 8 * x + 4 * half]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) lse2[4 * x + e] = y[e] * kLog2e;
+      for (int e = 0; e < 4; ++e) less[4 * x + e] = a.cap2 - y[e] * kLog2e;
     }
-    const f32x16 sc = L::scores(lds + buf * kBytes + qw * 32 * L::kRowBytes, at, key);
+    const f32x16 sc = L::template scores<false, 4>(lds + buf * kBytes + qw * 32 * L::kRowBytes, at, key);
     // whether all 32 rows see all of the wave's slots
     const int ja = j_first + kw * 32;
     int alo, ahi, x;
     seen_by(a, c, r0, r0, x, ahi);
     seen_by(a, c, min(r0 + 31, c.m * a.group - 1), min(r0 + 31, c.m * a.group - 1), alo, x);
     if (ja >= alo && ja + 32 <= ahi && r0 + 32 <= c.m * a.group)
-      sum += weigh<CAP>(a, sc, lse2);
+      sum += weigh<CAP>(a, sc, less);
     else
-      sum += weigh_seen<CAP>(a, c, sc, lse2, r0, j);
+      sum += weigh_seen<CAP>(a, c, sc, less, r0, j);
   }
   sum = half_sum(sum);
   // the row waves' sums, in their order

@@ -111,11 +111,11 @@ struct Tile {
   // Products of the 32 rows at LDS address k with the lanes' row pieces q:
   // lane (n, h) gets its row n's with rows 8 (v / 4) + 4 h + v % 4.  SWAP: its
   // LDS row n's with the pieces' rows.
-  template <bool SWAP = false>
+  template <bool SWAP = false, int AHEAD = 8>
   static __device__ __forceinline__ f32x16 scores(const char* k, const LaneAt& at, const uint4 (&q)[kQ]) {
-    // pieces are read kAhead matrix instructions before their use: the
-    // compiler alone reads them just before it and waits
-    constexpr int kAhead = kQ < 8 ? kQ : 8;
+    // pieces are read AHEAD matrix instructions before their use: the compiler
+    // alone reads them just before it and waits
+    constexpr int kAhead = kQ < AHEAD ? kQ : AHEAD;
     uint4 piece[kAhead];
     auto read = [&](int i) __attribute__((always_inline)) {
       piece[i % kAhead] =
