@@ -17,8 +17,20 @@ __device__ __forceinline__ void copy_rest(const AttnArgs& a) {
   for (int i = blockIdx.x; i < a.batch * a.hkv; i += gridDim.x) {
     const int n = min(max(a.tokens[i / a.hkv], 0), a.c.capacity);
     const int64_t at = static_cast<int64_t>(i) * a.mass_capacity;
-    for (int j = n + threadIdx.x; j < a.mass_capacity; j += blockDim.x)
-      a.mass[at + j] = a.mass_in ? a.mass_in[at + j] : 0.f;
+    // eight values a thread at a time, for the latency of reading them
+    for (int j0 = n + threadIdx.x; j0 < a.mass_capacity; j0 += 8 * blockDim.x) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int j = j0 + u * blockDim.x;
+        x[u] = a.mass_in && j < a.mass_capacity ? a.mass_in[at + j] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int j = j0 + u * blockDim.x;
+        if (j < a.mass_capacity) a.mass[at + j] = x[u];
+      }
+    }
   }
 }
 
