@@ -31,7 +31,7 @@ struct ForwardPlan {
   int grid;       // workgroups
   int splits;     // pieces of a unit; 1: none is split; decode: 0, as the work divides
   int strips;     // chunk: q tiles of all contexts, at most
-  int join_rows;  // query rows that a unit may have
+  int join_rows;  // query rows that a unit has by the caller's bound
   JoinHead* heads;
   float* pieces;
 };

@@ -57,7 +57,7 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
     // 16.8; 64 contexts of 300 slots, heads 64 / 8: 29.0, 25.8; 32 of 1024, heads
     // 28 / 4: 21.2, 21.6
     if (a.c.capacity <= 512) p.splits = 1;
-    p.join_rows = kDecodeRows;
+    p.join_rows = max_new * at->group;  // at most kDecodeRows
   } else {
     const int64_t strips = (int64_t(a.rows) * at->group + kChunkRows - 1) / kChunkRows +
                            std::min(a.batch, a.rows);

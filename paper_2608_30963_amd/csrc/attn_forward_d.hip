@@ -655,8 +655,7 @@ __global__ void __launch_bounds__(256) forward_join(AttnArgs a, ForwardPlan fp) 
   __shared__ float part_l[4];
   const JoinHead hd = fp.heads[blockIdx.x];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, w = wave % W;
-  const int r = blockIdx.y * (4 / W) + wave / W;
-  if (hd.pieces == 0 || blockIdx.y * (4 / W) >= hd.rows) return;
+  if (hd.pieces == 0) return;
   const int unit_rows = fp.decode ? kDecodeRows : kChunkRows;
   const size_t size = piece_floats(unit_rows, DP);
   // decode: piece 0 is slot 1 of its workgroup, the others slot 0 of the next ones
@@ -664,48 +663,52 @@ __global__ void __launch_bounds__(256) forward_join(AttnArgs a, ForwardPlan fp) 
     const size_t at = fp.decode ? (p == 0 ? hd.first : hd.first - 1 + 2 * static_cast<size_t>(p)) : hd.first + p;
     return fp.pieces + at * size;
   };
-  const int rc = min(r, hd.rows - 1);  // rows past the last one are not stored
-  float m2 = -INFINITY;
-  for (int p = lane; p < hd.pieces; p += 64) m2 = fmaxf(m2, reinterpret_cast<const float2*>(piece(p))[rc].x);
+  // the grid has the rows that the caller's bound on new tokens gives
+  for (int r0 = blockIdx.y * (4 / W); r0 < hd.rows; r0 += gridDim.y * (4 / W)) {
+    const int r = r0 + wave / W;
+    const int rc = min(r, hd.rows - 1);  // rows past the last one are not stored
+    float m2 = -INFINITY;
+    for (int p = lane; p < hd.pieces; p += 64) m2 = fmaxf(m2, reinterpret_cast<const float2*>(piece(p))[rc].x);
 #pragma unroll
-  for (int i = 32; i; i >>= 1) m2 = fmaxf(m2, __shfl_xor(m2, i));
-  float l = 0.f, o[PER];
+    for (int i = 32; i; i >>= 1) m2 = fmaxf(m2, __shfl_xor(m2, i));
+    float l = 0.f, o[PER];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) o[i] = 0.f;
+    for (int i = 0; i < PER; ++i) o[i] = 0.f;
 #pragma unroll 8
-  for (int p = w; p < hd.pieces; p += W) {
-    const float* part = piece(p);
-    const float2 ml = reinterpret_cast<const float2*>(part)[rc];
-    const float* x = part + 2 * unit_rows + static_cast<size_t>(rc) * DP + lane * PER;
-    const float f = ml.x == m2 ? 1.f : __builtin_amdgcn_exp2f(ml.x - m2);
-    l += f * ml.y;
+    for (int p = w; p < hd.pieces; p += W) {
+      const float* part = piece(p);
+      const float2 ml = reinterpret_cast<const float2*>(part)[rc];
+      const float* x = part + 2 * unit_rows + static_cast<size_t>(rc) * DP + lane * PER;
+      const float f = ml.x == m2 ? 1.f : __builtin_amdgcn_exp2f(ml.x - m2);
+      l += f * ml.y;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) o[i] += f * x[i];
-  }
-  if constexpr (W > 1) {
-    static_assert(W == 4, "the waves of a workgroup");
-#pragma unroll
-    for (int i = 0; i < PER; ++i) sums[w][lane * PER + i] = o[i];
-    if (lane == 0) part_l[w] = l;
-    __syncthreads();
-    if (w > 0) return;
-    l = (part_l[0] + part_l[1]) + (part_l[2] + part_l[3]);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = lane * PER + i;
-      o[i] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+      for (int i = 0; i < PER; ++i) o[i] += f * x[i];
     }
-  }
-  if (r >= hd.rows) return;
-  const int rr = hd.g0 + r, tok = fdiv(a.by_group, rr), g = rr - tok * a.group;
-  const int64_t row = hd.row0 + tok;
-  const int head = hd.h * a.group + g;
-  const bool sees = r >= hd.empty;
-  T* to = reinterpret_cast<T*>(a.out) + row * a.o_sr + head * a.o_sh;
+    if constexpr (W > 1) {
+      static_assert(W == 4, "the waves of a workgroup");
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (lane * PER + i < a.d) to[lane * PER + i] = store_cvt<T>(sees ? o[i] / l : 0.f);
-  if (a.lse && lane == 0) a.lse[row * a.hq + head] = sees ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+      for (int i = 0; i < PER; ++i) sums[w][lane * PER + i] = o[i];
+      if (lane == 0) part_l[w] = l;
+      __syncthreads();
+      l = (part_l[0] + part_l[1]) + (part_l[2] + part_l[3]);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int e = lane * PER + i;
+        o[i] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+      }
+      __syncthreads();
+    }
+    if (r >= hd.rows || w > 0) continue;
+    const int rr = hd.g0 + r, tok = fdiv(a.by_group, rr), g = rr - tok * a.group;
+    const int64_t row = hd.row0 + tok;
+    const int head = hd.h * a.group + g;
+    const bool sees = r >= hd.empty;
+    T* to = reinterpret_cast<T*>(a.out) + row * a.o_sr + head * a.o_sh;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (lane * PER + i < a.d) to[lane * PER + i] = store_cvt<T>(sees ? o[i] / l : 0.f);
+    if (a.lse && lane == 0) a.lse[row * a.hq + head] = sees ? (m2 + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  }
 }
 
 }  // namespace
