@@ -4,7 +4,8 @@ The package is deliberately small:
 
 * ``kvx``    -- Python binding of the C-ABI library ``libkvx.so`` (argument
                marshalling only; every step of the translation runs in HIP
-               kernels behind ``kvx_translate``).
+               kernels behind ``kvx_translate``), and of decoding on the
+               translated cache (``kvx_attn_*``).
 * ``synth``  -- seeded synthetic inputs shaped like the paper's model pairs.
 * ``build``  -- compiles ``csrc/`` into ``libkvx.so`` with hipcc for gfx950.
 
