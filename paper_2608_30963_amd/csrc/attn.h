@@ -111,15 +111,32 @@ __device__ __forceinline__ int end_seen(const Context& c, int p) {
   return p < 0 ? 0 : max(p + 1, c.prefix);
 }
 
-// The r of a capped score: tanh(y) = 1 - 2 r, r = 1 / (1 + exp(2 y)).  Its
-// absolute error, as that of 1 - 2 r, is 2^-24 or so, times the cap.
+// A capped score is cap tanh(y), y = dot scale / cap, x the dot product q.k.
+//
+// cap_part: the r of tanh(y) = 1 - 2 r, r = 1 / (1 + exp(2 y)).  Its absolute
+// error is 2^-24 or so, and the score's that times the cap: far below what
+// bf16 weights are rounded by, for which it serves.
 __device__ __forceinline__ float cap_part(const AttnArgs& a, float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * a.tanh2));
 }
 
-// Score in units of log2: x is the dot product q.k.
+// tanh(y) with a relative error of 2^-22: below 0.6, where 1 - 2 r loses digits,
+// y + y^3 P(y^2), P the polynomial of least relative error there (3e-9).
+__device__ __forceinline__ float cap_tanh(const AttnArgs& a, float x) {
+  constexpr float kHalfLn2 = 0.34657359f;
+  const float y = x * (a.tanh2 * kHalfLn2), z = y * y;
+  float p = __builtin_fmaf(z, -0.005895158275961876f, 0.020795971155166626f);
+  p = __builtin_fmaf(z, p, -0.053783830255270004f);
+  p = __builtin_fmaf(z, p, 0.13331924378871918f);
+  p = __builtin_fmaf(z, p, -0.33333298563957214f);
+  return z < 0.36f ? __builtin_fmaf(y * z, p, y) : __builtin_fmaf(-2.f, cap_part(a, x), 1.f);
+}
+
+// Score in units of log2.
+template <bool EXACT>
 __device__ __forceinline__ float score2(const AttnArgs& a, float x) {
-  return a.cap2 == 0.f ? x * a.scale2 : __builtin_fmaf(-2.f * a.cap2, cap_part(a, x), a.cap2);
+  if (a.cap2 == 0.f) return x * a.scale2;
+  return EXACT ? a.cap2 * cap_tanh(a, x) : __builtin_fmaf(-2.f * a.cap2, cap_part(a, x), a.cap2);
 }
 
 // Launchers; each returns the launch's own status.

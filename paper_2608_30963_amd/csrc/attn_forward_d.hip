@@ -295,6 +295,9 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
       for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, at, q);
       if constexpr (!CAP) {
         top = top_score(c2, s);
+      } else if constexpr (!L::kBf16) {
+        cap_scores<T>(a, s);
+        top = top_score(c2, s);
       } else {
         f32x16 x[NS];
 #pragma unroll
@@ -321,9 +324,6 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
         score(after(kslot, kKeys, 1), next);
 #pragma unroll
         for (int u = 0; u < NS; ++u) {
-          if constexpr (CAP)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) s[u][x] = a.cap2 - 2.f * a.cap2 * s[u][x];
           weights(c2, s[u], st);
           L::template add_values<false>(v + u * 32 * L::kRowBytes, at, s[u], acc);
         }
@@ -516,7 +516,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
       const int j0 = slot_of(t);
       if (j0 >= alo && j0 + 32 <= ahi) {
         f32x16 sc[1] = {L::scores(k, at, q)};
-        if constexpr (CAP) cap_scores(a, sc);
+        if constexpr (CAP) cap_scores<T>(a, sc);
         if constexpr (L::kBf16) {
           // the first pieces of the values come beside the softmax
           constexpr int kAhead = 2 * NB < 8 ? 2 * NB : 8;

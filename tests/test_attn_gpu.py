@@ -300,6 +300,38 @@ def test_masked_values_may_be_anything():
         att.close()
 
 
+@pytest.mark.parametrize("m,d", [(1, 128), (3, 256), (75, 128), (70, 256)])
+def test_small_scores_under_a_large_cap(m, d):
+    """fp32 scores far below their cap keep a relative precision: tanh's 2^-22
+    and two roundings beside it are within 2^-21 of the terms' magnitudes."""
+    T = U.torch()
+    print(f"[attn] cap {m} x {d}", flush=True)
+    n, hq, cap = 400, 4, 1000.0
+    cache = Cache([n], 2, d, "f32", 16)
+    q = _rows(m, hq, d, "f32", 3)
+    att = kvx.Attention(kvx.ModelShape(2, 2, d, 1e4), hq, kvx.KVX_F32, softcap=cap)
+    out = T.zeros_like(q)
+    lse = T.zeros(m, hq, device="cuda")
+    mass = T.zeros(1, 2, n, device="cuda")
+    kw = dict(layer=1, max_new=m, q_start=_int([0, m]), lse=lse)
+    att.forward(kvx.make_attn_io(cache.struct, _int([n]), q, out=out, **kw), att.workspace())
+    att.mass(kvx.make_attn_io(cache.struct, _int([n]), q, mass=mass, **kw))
+    T.cuda.synchronize()
+    k, v = cache.f64(0, 1, 0), cache.f64(1, 1, 0)
+    ro, rl, mag, size = R.attend(_f64(q), k, v, d ** -0.5, cap)
+    delta = ((d + 8) * EPS + 2.0 ** -21) * size
+    tol = mag * (2 * delta + (n + 64) * EPS)[..., None]
+    assert (np.abs(_f64(out) - ro) <= tol).all(), (np.abs(_f64(out) - ro) / tol).max()
+    ltol = delta + (n + 64) * EPS + 2.0 ** -22 * (1 + np.abs(rl))
+    assert (np.abs(_f64(lse) - rl) <= ltol).all()
+    got = _f64(lse)
+    ref, size = R.mass(_f64(q), k, got, d ** -0.5, cap)
+    delta = ((d + 8) * EPS + 2.0 ** -21) * size
+    tol = ref * (2 * delta + (m * hq + 64) * EPS + 4 * EPS * (np.abs(got).max() + 1)) + 2.0 ** -126
+    assert (np.abs(_f64(mass)[0] - ref) <= tol).all()
+    att.close()
+
+
 @pytest.mark.parametrize("dtype,m,d", [("bf16", 1, 128), ("bf16", 140, 128), ("bf16", 140, 256),
                                        ("f32", 70, 64)])
 def test_scores_that_rise_along_the_cache(dtype, m, d):
