@@ -48,6 +48,11 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
   ForwardPlan p{};
   p.heads = static_cast<JoinHead*>(workspace);
   p.pieces = reinterpret_cast<float*>(static_cast<char*>(workspace) + head_bytes(at));
+  // up to 32 query rows per context: the ring of single tokens, which splits the
+  // cache evenly over the card; more: the chunk kernel.  Measured (us; ring,
+  // chunk), heads 28 / 4 x 128, 16 contexts of 4096 slots: 28 rows 36.6, 36.1; 56
+  // rows 54.4, 44.0; 112 rows 83.0, 56.6; one of 128k: 7 rows 53, 239; 28 rows 62,
+  // 241.  A few contexts of 1024 slots lose by it: 28 rows 18.7, 15.0.
   p.decode = int64_t(max_new) * at->group <= kDecodeRows;
   if (p.decode) {
     p.grid = at->n_cu;
