@@ -1,4 +1,6 @@
 """The decoding example on the GPU: translated cache, question, answer, budget."""
+import gc
+
 import numpy as np
 import pytest
 
@@ -6,6 +8,19 @@ from oracle import attn as R
 from tests import gpu_util as U
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _memory_as_before():
+    """The stand-in layers' products leave torch's matrix library a workspace,
+    cut out of whatever block was cached; other tests rely on blocks that are
+    wholly free going back to the driver."""
+    yield
+    T = U.torch()
+    T.cuda.synchronize()
+    gc.collect()
+    T._C._cuda_clearCublasWorkspaces()
+    T.cuda.empty_cache()
 
 
 def _decoder(config, batch, budget, slack):
