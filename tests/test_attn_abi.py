@@ -93,3 +93,21 @@ def test_struct_layouts_match_header(tmp_path):
     got = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True,
                                           text=True).stdout.split()]
     assert got == expect
+
+
+def test_recorded_traffic_goes_by_the_fused_kernel_alone(tmp_path, monkeypatch):
+    """Sources of decoding are no part of the fused launch: the benchmark's
+    recorded traffic holds whatever they are."""
+    import shutil
+
+    import bench
+    src = tmp_path / "csrc"
+    shutil.copytree(bench.KERNEL_SOURCES, src)
+    monkeypatch.setattr(bench, "KERNEL_SOURCES", str(src))
+    h0 = bench.kernel_source_hash()
+    for f in sorted(src.glob("attn*")):
+        with open(f, "a") as fh:
+            fh.write("\n// edit\n")
+    assert bench.kernel_source_hash() == h0
+    assert bench.recorded("qwen2.5-7b->qwen2.5-1.5b", "bf16x2", 4096, 1, "contiguous",
+                          "traffic_bytes_per_launch") is not None
