@@ -98,8 +98,6 @@ def test_struct_layouts_match_header(tmp_path):
 def test_recorded_traffic_goes_by_the_fused_kernel_alone(tmp_path, monkeypatch):
     """Sources of decoding are no part of the fused launch: the benchmark's
     recorded traffic holds whatever they are."""
-    import shutil
-
     import bench
     src = tmp_path / "csrc"
     shutil.copytree(bench.KERNEL_SOURCES, src)
