@@ -16,7 +16,9 @@
  * in slots 0 .. n-1; its m new tokens are the last ones, so that new token i
  * has slot p = n - m + i.  Query head h reads KV head h / (Hq / Hkv).  New
  * tokens of all contexts stand one after another in rows, context b's from
- * row q_start[b] on.
+ * row q_start[b] on.  A context may outgrow its cache (a replayed step counts
+ * on without the host): slots keep their numbers, those past the capacity are
+ * not stored, seen or kept, and all others stay as they are.
  *
  * Status codes and dtypes are those of kvx.h.  No function throws.  Every
  * host-visible argument is checked before anything is enqueued.  Device

@@ -87,9 +87,12 @@ struct AttnArgs {
   int32_t mass_capacity;
 };
 
-// A context's rows and slots, clamped to what the caller's buffers hold.
+// A context's rows and slots, clamped to what the caller's buffers hold.  New
+// token i has slot p0 + i by the length that the caller gave, also where that
+// is past the cache's capacity: then the first n = capacity slots are there.
 struct Context {
-  int q0, m, n;  // first row, new tokens, cached tokens
+  int q0, m, n;  // first row, new tokens, slots that the cache holds
+  int p0;        // slot of the first new token, n - m or more
   int prefix;    // slots that every new token sees
 };
 
@@ -98,17 +101,21 @@ __device__ __forceinline__ Context context(const AttnArgs& a, int b) {
   c.q0 = a.q_start ? min(max(a.q_start[b], 0), a.rows) : b;
   const int q1 = a.q_start ? min(max(a.q_start[b + 1], c.q0), a.rows) : b + 1;
   c.m = q1 - c.q0;
-  c.n = min(max(a.tokens[b], 0), a.c.capacity);
+  // room above for the rows that pad a tile past the last new token
+  const int all = min(max(a.tokens[b], 0), INT32_MAX - 1024);
+  c.n = min(all, a.c.capacity);
+  c.p0 = all - c.m;
   c.prefix = a.prefix ? min(max(a.prefix[b], 0), c.n) : 0;
   return c;
 }
 
-// Slots [lo, hi) that the new token of slot p sees; empty for p < 0.
+// Slots [lo, hi) that the new token of slot p sees; empty for p < 0, and where
+// a window starts past the cache's last slot.
 __device__ __forceinline__ int first_seen(const AttnArgs& a, int p) {
   return a.window && p >= a.window ? p - a.window + 1 : 0;
 }
 __device__ __forceinline__ int end_seen(const Context& c, int p) {
-  return p < 0 ? 0 : max(p + 1, c.prefix);
+  return p < 0 ? 0 : min(max(p + 1, c.prefix), c.n);
 }
 
 // A capped score is cap tanh(y), y = dot scale / cap, x the dot product q.k.

@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs g, int pieces, i
   if (row >= a.rows) return;
   const int b = context_of(a, static_cast<int>(row));
   const Context c = context(a, b);
-  const int slot = c.n - c.m + static_cast<int>(row) - c.q0;
+  const int slot = c.p0 + static_cast<int>(row) - c.q0;
   const int half = a.d / 2;
   float cs[N], sn[N];
 #pragma unroll

@@ -20,7 +20,7 @@ struct JoinHead {
   int32_t g0;      // its head within the group
   int32_t h;       // KV head
   int32_t first;   // index of the unit's first piece
-  int32_t empty;   // query rows before this one see nothing
+  int32_t from, to;  // query rows that see anything
 };
 
 constexpr int kChunkRows = 128;  // query rows of a workgroup of the chunk kernel

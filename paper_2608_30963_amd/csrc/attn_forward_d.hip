@@ -6,9 +6,12 @@
 namespace kvx {
 namespace {
 
-// Query rows from r0 on that see nothing: their slots are negative.
-__device__ __forceinline__ int unseeing(const AttnArgs& a, const Context& c, int r0) {
-  return max(0, (c.m - c.n) * a.group - r0);
+// Query rows [from, to) of those from r0 on that see anything: slots before them
+// are negative, windows after them start past the cache's last slot.
+__device__ __forceinline__ void seeing(const AttnArgs& a, const Context& c, int r0, int& from, int& to) {
+  from = -c.p0 * a.group - r0;
+  const int64_t last = a.window ? min<int64_t>(c.m, int64_t(c.n) + a.window - 1 - c.p0) : c.m;
+  to = static_cast<int>(max<int64_t>(last, 0)) * a.group - r0;
 }
 
 // out row of query (row, head) from O^T registers and its sum; lane (n, h) has
@@ -199,7 +202,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   const int r0 = qt * kChunkRows, valid = min(kChunkRows, c.m * a.group - r0);
   int lo, hi;
   seen_by(a, c, r0, r0 + valid - 1, lo, hi);
-  const int tiles = (hi + TK - 1) / TK - lo / TK;
+  const int tiles = lo < hi ? (hi + TK - 1) / TK - lo / TK : 0;
   const int per = (tiles + fp.splits - 1) / fp.splits;
   const int t0 = lo / TK + split * per, t1 = min(t0 + per, lo / TK + tiles);
 
@@ -357,8 +360,11 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
 
   const int unit = h * fp.strips + strip;
   float* part = fp.pieces + (static_cast<size_t>(unit) * fp.splits + split) * piece_floats(kChunkRows, DP);
-  if (fp.splits > 1 && split == 0 && threadIdx.x == 0)
-    *head = JoinHead{fp.splits, valid, c.q0, r0, h, unit * fp.splits, unseeing(a, c, r0)};
+  if (fp.splits > 1 && split == 0 && threadIdx.x == 0) {
+    int from, to;
+    seeing(a, c, r0, from, to);
+    *head = JoinHead{fp.splits, valid, c.q0, r0, h, unit * fp.splits, from, to};
+  }
   const int r = w * 32 + n;
   if (fp.splits == 1) {
     if (r < valid) store_out<T, NB>(a, qr, h, acc, st);
@@ -430,8 +436,9 @@ __device__ __forceinline__ int decode_steps(const AttnArgs& a, const Context& c,
   int lo, hi;
   const int r0 = qt * kDecodeRows;
   seen_by(a, c, r0, min(r0 + kDecodeRows, c.m * a.group) - 1, lo, hi);
+  if (lo >= hi) return 1;
   lo &= ~31;
-  return max(1, (hi - lo + STEP - 1) / STEP);
+  return (hi - lo + STEP - 1) / STEP;
 }
 
 template <typename T, int DP, bool CAP>
@@ -481,7 +488,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
     seen_by(a, c, r0 + valid - 1, r0 + valid - 1, alo, xhi);  // the most that any row's start is
     const int j_first = (lo & ~31) + (step * NW + w) * 32;
     // tiles of this wave: every NW-th of the range, as far as slots are seen
-    const int tiles = min(cnt, hi > j_first ? (hi - j_first + NW * 32 - 1) / (NW * 32) : 0);
+    const int tiles = min(cnt, lo < hi && hi > j_first ? (hi - j_first + NW * 32 - 1) / (NW * 32) : 0);
     const QueryRow qr = query_row(a, c, r0 + n);
     uint4 q[L::kQ];
     const T* qp = reinterpret_cast<const T*>(a.q) + qr.row * a.q_sr + (h * a.group + qr.g) * a.q_sh;
@@ -643,8 +650,10 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
     if (begins && !ends && tid == 0) {
       // the unit's other pieces are the first ones of the next workgroups
       const int64_t end = s - step + all;
+      int from, to;
+      seeing(a, c, r0, from, to);
       *head = JoinHead{static_cast<int32_t>((end - 1) / per - blockIdx.x + 1), valid, c.q0, r0, h,
-                       static_cast<int32_t>(2 * blockIdx.x + 1), unseeing(a, c, r0)};
+                       static_cast<int32_t>(2 * blockIdx.x + 1), from, to};
     }
     s += whole ? 1 : cnt;
     step = 0;
@@ -722,7 +731,7 @@ __global__ void __launch_bounds__(256) forward_join(AttnArgs a, ForwardPlan fp) 
     const int rr = hd.g0 + r, tok = fdiv(a.by_group, rr), g = rr - tok * a.group;
     const int64_t row = hd.row0 + tok;
     const int head = hd.h * a.group + g;
-    const bool sees = r >= hd.empty;
+    const bool sees = r >= hd.from && r < hd.to;
     T* to = reinterpret_cast<T*>(a.out) + row * a.o_sr + head * a.o_sh;
 #pragma unroll
     for (int i = 0; i < PER; ++i)

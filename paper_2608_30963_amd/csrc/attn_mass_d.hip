@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
   if (j_first >= end) return;
   const int j_last = min(end, j_first + KW * 32) - 1;
   // rows of the tokens that see any of the workgroup's slots
-  const int p0 = c.n - c.m;
+  const int p0 = c.p0;
   const int i0 = max(max(0, -p0), j_first < c.prefix ? 0 : j_first - p0);
   const int i1 = a.window ? static_cast<int>(min<int64_t>(c.m, int64_t(j_last) + a.window - p0)) : c.m;
   const int r_first = i0 * a.group, r_end = i1 * a.group;

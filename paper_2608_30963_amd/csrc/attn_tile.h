@@ -408,16 +408,16 @@ __device__ __forceinline__ QueryRow query_row(const AttnArgs& a, const Context& 
   const int i = fdiv(a.by_group, r);
   q.row = c.q0 + i;
   q.g = r - i * a.group;
-  const int p = c.n - c.m + i;
+  const int p = c.p0 + i;
   q.lo = first_seen(a, p);
   q.hi = r < c.m * a.group ? end_seen(c, p) : 0;
   return q;
 }
 
-// Slots that query rows r0 .. r1 of a context see together.
+// Slots that query rows r0 .. r1 of a context see together; lo == hi: none does.
 __device__ __forceinline__ void seen_by(const AttnArgs& a, const Context& c, int r0, int r1,
                                         int& lo, int& hi) {
-  const int p0 = c.n - c.m + fdiv(a.by_group, r0), p1 = c.n - c.m + fdiv(a.by_group, r1);
+  const int p0 = c.p0 + fdiv(a.by_group, r0), p1 = c.p0 + fdiv(a.by_group, r1);
   hi = end_seen(c, p1);
   lo = min(first_seen(a, max(p0, 0)), hi);
 }
