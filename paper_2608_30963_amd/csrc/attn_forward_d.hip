@@ -9,7 +9,7 @@ namespace {
 // Query rows [from, to) of those from r0 on that see anything: slots before them
 // are negative, windows after them start past the cache's last slot.
 __device__ __forceinline__ void seeing(const AttnArgs& a, const Context& c, int r0, int& from, int& to) {
-  from = -c.p0 * a.group - r0;
+  from = max(0, -c.p0) * a.group - r0;  // slots times heads may pass 32 bits, rows do not
   const int64_t last = a.window ? min<int64_t>(c.m, int64_t(c.n) + a.window - 1 - c.p0) : c.m;
   to = static_cast<int>(max<int64_t>(last, 0)) * a.group - r0;
 }

@@ -147,3 +147,43 @@ def test_attention_past_the_capacity(case, window):
 
 def _top(x):
     return x.max(initial=0.0)
+
+
+def _repeated(n, page, blocks, d, dtype, seed=0):
+    """One context of n slots of one KV head, whose table names `blocks` blocks
+    over and over: (cache, rows(kv, slots))."""
+    T = U.torch()
+    g = T.Generator().manual_seed(seed)
+    dev = [T.randn(1, blocks, 1, page, d, generator=g).to(A._dt(dtype)) for _ in range(2)]
+    table = (T.arange(-(-n // page), dtype=T.int32) * 5 % blocks).view(1, -1).cuda()
+    host = [A._f64(t) for t in dev]
+    gpu = [t.cuda() for t in dev]
+
+    def rows(kv, j):
+        return host[kv][0, j // page * 5 % blocks, :, j % page]
+
+    return kvx.make_cache(gpu[0], gpu[1], table), rows
+
+
+@pytest.mark.parametrize("hq,n,m", [(128, 17_000_011, 1), (32, 67_200_003, 1), (128, 17_000_011, 2)])
+def test_attention_of_slots_times_heads_past_32_bits(hq, n, m):
+    """A cache so long that its slots times the heads of a group pass 2^31;
+    blocks repeat, so that it takes little memory, and a window bounds the work."""
+    T = U.torch()
+    print(f"[long attention] {hq} heads, {n} slots", flush=True)
+    assert n * hq > 2 ** 31
+    d, window = 64, 3000
+    cache, rows = _repeated(n, 64, 7, d, "bf16")
+    q = A._rows(m, hq, d, "bf16", 3)
+    att = kvx.Attention(kvx.ModelShape(1, 1, d, 1e4), hq, kvx.KVX_BF16)
+    out, lse = T.zeros_like(q), T.zeros(m, hq, device="cuda")
+    att.forward(kvx.make_attn_io(cache, A._int([n]), q, out=out, lse=lse, window=window, max_new=m,
+                                 q_start=A._int([0, m])), att.workspace())
+    T.cuda.synchronize()
+    j = np.arange(n - window - m, n)
+    ro, rl, mag, size = R.attend(A._f64(q), rows(0, j), rows(1, j), d ** -0.5, 0.0, window)
+    delta = A._delta(size, d, 0.0)
+    tol = mag * (2 * delta + (window + 64) * EPS + 2.0 ** -8)[..., None] + 2.0 ** -8 * np.abs(ro)
+    assert (np.abs(A._f64(out) - ro) <= tol).all()
+    assert (np.abs(A._f64(lse) - rl) <= delta + (window + 64) * EPS + 2.0 ** -22 * (1 + np.abs(rl))).all()
+    att.close()
