@@ -239,7 +239,9 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
   // rows of the tokens that see any of the workgroup's slots
   const int p0 = c.p0;
   const int i0 = max(max(0, -p0), j_first < c.prefix ? 0 : j_first - p0);
-  const int i1 = a.window ? static_cast<int>(min<int64_t>(c.m, int64_t(j_last) + a.window - p0)) : c.m;
+  // (not below 0: a negative count times the heads may pass 32 bits)
+  const int i1 =
+      a.window ? static_cast<int>(max<int64_t>(0, min<int64_t>(c.m, int64_t(j_last) + a.window - p0))) : c.m;
   const int r_first = i0 * a.group, r_end = i1 * a.group;
   const int stages = r_end > r_first ? (r_end - r_first + kRows - 1) / kRows : 0;
 

@@ -187,3 +187,29 @@ def test_attention_of_slots_times_heads_past_32_bits(hq, n, m):
     assert (np.abs(A._f64(out) - ro) <= tol).all()
     assert (np.abs(A._f64(lse) - rl) <= delta + (window + 64) * EPS + 2.0 ** -22 * (1 + np.abs(rl))).all()
     att.close()
+
+
+@pytest.mark.parametrize("hq,n,m", [(128, 17_000_011, 1), (256, 9_000_011, 2)])
+def test_weights_of_slots_times_heads_past_32_bits(hq, n, m):
+    """The same of the cached tokens' weights: those that a window leaves out,
+    which are nearly all, stay as they were."""
+    T = U.torch()
+    print(f"[long weights] {hq} heads, {n} slots", flush=True)
+    assert n * hq > 2 ** 31
+    d, window = 64, 3000
+    cache, rows = _repeated(n, 64, 7, d, "bf16")
+    q = A._rows(m, hq, d, "bf16", 3)
+    att = kvx.Attention(kvx.ModelShape(1, 1, d, 1e4), hq, kvx.KVX_BF16)
+    j = np.arange(n - window - m, n)
+    _, rl, _, _ = R.attend(A._f64(q), rows(0, j), rows(1, j), d ** -0.5, 0.0, window)
+    lse = T.from_numpy(rl.astype(np.float32)).cuda()
+    mass = T.full((1, 1, n), 0.5, device="cuda")
+    att.mass(kvx.make_attn_io(cache, A._int([n]), q, lse=lse, window=window, max_new=m,
+                              q_start=A._int([0, m]), mass_in=mass, mass=mass))
+    T.cuda.synchronize()
+    assert (mass[0, 0, :int(j[0]) + 1] == 0.5).all()
+    ref, size = R.mass(A._f64(q), rows(0, j), A._f64(lse), d ** -0.5, 0.0, window)
+    rel = 2 * A._delta(size, d, 0.0) + (m * hq + 64) * EPS + 4 * EPS * (np.abs(rl).max() + 1)
+    got = A._f64(mass[0, 0, int(j[0]):])
+    assert (np.abs(got - 0.5 - ref[0]) <= ref[0] * rel + 2 * EPS * (0.5 + ref[0]) + 2.0 ** -126).all()
+    att.close()
