@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kSelThreads, 8) evict_select(EvictArgs a) {
     done += total;
     __syncthreads();  // the counts' next use
   }
-  for (int i = keep + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
+  for (int64_t i = keep + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
   if (wo)
     for (int i = keep + tid; i < min(a.mass_capacity, max(a.keep, n)); i += kSelThreads) wo[i] = 0.f;
 }
@@ -263,21 +263,23 @@ hipError_t launch_evict(const kvx_attn* at, const EvictArgs& args, hipStream_t s
   a.src = in_bytes(a.src, es);
   a.dst = in_bytes(a.dst, es);
   const int sets = a.layers * a.batch * a.heads;
-  const hipError_t e = launch_on(evict_select, dim3(sets), dim3(kSelThreads), st, a);
-  if (e != hipSuccess) return e;
   // pieces of a workgroup: a power of two that divides a row's, of at least 128
-  // bytes (a memory line)
+  // bytes (a memory line).  Elsewhere a step of rows a workgroup, more where a
+  // launch would have too many; rows past the cache's slots are never kept
   const int whole = a.row_bytes / 16;
-  int pieces = whole & -whole, rows = a.keep, parts;
+  int pieces = whole & -whole, rows = std::min(a.keep, a.src.capacity), parts;
   if (a.in_place) {
     pieces = std::min(pieces, 8);
     parts = whole / pieces;
   } else {
     pieces = std::min(pieces, 64);
+    const int most = rows, per = whole / pieces;
     rows = kMoveThreads * kMoveUnroll / pieces;
-    parts = whole / pieces * ((a.keep + rows - 1) / rows);
+    while (per * ((int64_t(most) + rows - 1) / rows) > 65535) rows *= 2;
+    parts = static_cast<int>(per * ((int64_t(most) + rows - 1) / rows));
   }
-  if (parts > 65535) return hipErrorInvalidValue;
+  const hipError_t e = launch_on(evict_select, dim3(sets), dim3(kSelThreads), st, a);
+  if (e != hipSuccess) return e;
   return launch_on(evict_move, dim3(sets, 2, parts), dim3(kMoveThreads), st, a, __builtin_ctz(pieces), rows);
 }
 

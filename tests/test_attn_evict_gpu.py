@@ -1,0 +1,69 @@
+"""Eviction (kvx_attn_evict) at sizes where its launches and buffers end: many
+kept tokens, and weights for fewer slots than are cached."""
+import numpy as np
+import pytest
+
+from oracle import attn as R
+from paper_2608_30963_amd import kvx
+from tests import gpu_util as U
+from tests import test_attn_gpu as A
+
+pytestmark = pytest.mark.gpu
+
+
+def test_keep_far_beyond_the_cache():
+    """A budget of more tokens than one launch has workgroups for, on a small
+    cache: everything is kept, whole."""
+    T = U.torch()
+    print("[evict] keep beyond the cache", flush=True)
+    lens, d, keep = [100, 7], 256, 2_200_000
+    cache, dst = (A.Cache(lens, 1, d, "f32", 16, layers=1, seed=s) for s in (0, 9))
+    w = T.rand(1, 2, 1, 128, device="cuda")
+    mass = w.clone()
+    kept = T.full((1, 2, 1, keep), -7, dtype=T.int32, device="cuda")
+    left = A._int([0, 0])
+    att = kvx.Attention(kvx.ModelShape(1, 1, d, 1e4), 1, kvx.KVX_F32)
+    att.evict(kvx.make_evict_io(cache.struct, A._int(lens), mass, kept, keep, sink=4, recent=8,
+                                mass_out=mass, tokens_out=left, dst=dst.struct))
+    T.cuda.synchronize()
+    assert left.tolist() == lens
+    for b, n in enumerate(lens):
+        assert (kept[0, b, 0, :n].cpu().numpy() == np.arange(n)).all()
+        assert (kept[0, b, 0, n:] == -1).all()
+        assert T.equal(mass[0, b, 0, :n], w[0, b, 0, :n])
+        for kv in range(2):
+            assert T.equal(dst.read(kv, 0, b, n), cache.rows[kv][0][b])
+    att.close()
+
+
+def test_millions_of_rows_to_other_memory():
+    """More rows than a launch has workgroups for at one step each.  The source
+    names 5 blocks over and over, so that it takes little memory."""
+    T = U.torch()
+    print("[evict] 2.2 million rows", flush=True)
+    d, page, keep, n = 256, 32, 2_200_000, 2_300_005
+    g = T.Generator().manual_seed(0)
+    src = [T.randn(1, 5, 1, page, d, generator=g).cuda() for _ in range(2)]
+    table = (T.arange(-(-n // page), dtype=T.int32) * 3 % 5).view(1, -1).cuda()
+    dst = [T.zeros(1, 1, 1, keep, d, device="cuda") for _ in range(2)]
+    w = T.rand(1, 1, 1, n, device="cuda", generator=T.Generator("cuda").manual_seed(1))
+    kept = T.full((1, 1, 1, keep), -7, dtype=T.int32, device="cuda")
+    left = A._int([0])
+    att = kvx.Attention(kvx.ModelShape(1, 1, d, 1e4), 1, kvx.KVX_F32)
+    att.evict(kvx.make_evict_io(kvx.make_cache(src[0], src[1], table), A._int([n]), w, kept, keep,
+                                sink=4, recent=100, tokens_out=left,
+                                dst=kvx.make_cache(dst[0], dst[1])))
+    T.cuda.synchronize()
+    assert left.tolist() == [keep]
+    weight = w[0, 0, 0].cpu().numpy().astype(np.float64)
+    always = np.zeros(n, bool)
+    always[:4] = always[-100:] = True
+    rest = np.flatnonzero(~always)
+    rest = rest[np.argsort(-weight[rest], kind="stable")[:keep - 104]]
+    want = T.from_numpy(np.sort(np.concatenate([np.flatnonzero(always), rest]))).cuda()
+    assert T.equal(kept[0, 0, 0].long(), want)
+    for s, t in zip(src, dst):
+        for i in range(0, keep, 200_000):
+            j = want[i:i + 200_000]
+            assert T.equal(t[0, 0, 0, i:i + 200_000], s[0, j // page * 3 % 5, 0, j % page])
+    att.close()
