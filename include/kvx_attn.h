@@ -102,7 +102,8 @@ typedef struct {
   float* lse;                /* [rows][n_heads] log-sum-exp of the visible scores;
                                 forward: written unless NULL; mass: read */
   /* mass: [batch][n_kv_heads][mass_capacity], slot-indexed; mass_in NULL is
-   * zero and may be mass itself.  Slots >= n are copied from mass_in (or 0). */
+   * zero and may be mass itself.  Slots >= n are copied from mass_in (or 0).
+   * tokens[b] <= mass_capacity is wanted: slots past it get no weight. */
   const float* mass_in;
   float* mass;
   int32_t mass_capacity;
@@ -118,7 +119,8 @@ typedef struct {
   kvx_cache src;
   kvx_cache dst;             /* where kept rows go, slots 0 .. ; k == NULL: in
                                 place.  Other memory than src's */
-  const float* mass;         /* [layers][batch][n_kv_heads][mass_capacity] */
+  const float* mass;         /* [layers][batch][n_kv_heads][mass_capacity]; cached
+                                tokens past it count as weight 0 */
   float* mass_out;           /* same shape, or NULL: the kept tokens' weights, then
                                 zeros up to min(mass_capacity, max(keep, n)); may be
                                 mass itself */

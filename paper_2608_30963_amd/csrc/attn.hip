@@ -426,8 +426,7 @@ kvx_status kvx_attn_evict(const kvx_attn* at, const kvx_evict_io* io, void* stre
     if (s != KVX_OK) return s;
     if (a.dst.capacity < io->keep && a.dst.capacity < a.src.capacity) return KVX_ESHAPE;
   }
-  // every cached token has a weight
-  if (io->mass_capacity < a.src.capacity && io->mass_capacity > INT32_MAX / 2) return KVX_ESHAPE;
+  if (io->mass_capacity > INT32_MAX / 2) return KVX_ESHAPE;
   a.tokens = io->tokens;
   a.layers = at->model.n_layers;
   a.batch = io->batch;

@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kSelThreads, 8) evict_select(EvictArgs a) {
   __shared__ int found[3];  // digit, rank left within it, its count
   const int set = blockIdx.x, tid = threadIdx.x;
   const int b = set / a.heads % a.batch;
-  const int n = min(min(max(a.tokens[b], 0), a.src.capacity), a.mass_capacity);
+  const int n = min(max(a.tokens[b], 0), a.src.capacity), weighed = min(n, a.mass_capacity);
   const int keep = min(n, a.keep);
   if (a.tokens_out && tid == 0 && set < a.heads * a.batch && set % a.heads == 0)
     a.tokens_out[b] = keep;
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kSelThreads, 8) evict_select(EvictArgs a) {
 #pragma unroll
     for (int u = 0; u < kHeld; ++u) {
       const int j = c * kChunk + u * kSelThreads + tid;
-      x[u] = j < n ? w[j] : 0.f;
+      x[u] = j < weighed ? w[j] : 0.f;
     }
   };
   if (chunks == 1) load(0);
@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(kSelThreads, 8) evict_select(EvictArgs a) {
     for (int u = 0; u < kHeld; ++u)
       if (on >> u & 1) {
         kept[done + at[u]] = c * kChunk + u * kSelThreads + tid;
-        if (wo) wo[done + at[u]] = x[u];
+        if (wo && done + at[u] < a.mass_capacity) wo[done + at[u]] = x[u];
       }
     done += total;
     __syncthreads();  // the counts' next use
@@ -212,7 +212,7 @@ constexpr int kMoveUnroll = 8;  // 16-byte pieces of a thread in flight
 __global__ void __launch_bounds__(kMoveThreads) evict_move(EvictArgs a, int log_pieces, int rows) {
   const int set = blockIdx.x, v = blockIdx.y, tid = threadIdx.x;
   const int h = set % a.heads, b = set / a.heads % a.batch, l = set / a.heads / a.batch;
-  const int n = min(min(max(a.tokens[b], 0), a.src.capacity), a.mass_capacity);
+  const int n = min(max(a.tokens[b], 0), a.src.capacity);
   const int keep = min(min(n, a.keep), a.dst.capacity);
   const int32_t* kept = a.kept + static_cast<int64_t>(set) * a.keep;
   const int pieces = 1 << log_pieces;

@@ -67,3 +67,61 @@ def test_millions_of_rows_to_other_memory():
             j = want[i:i + 200_000]
             assert T.equal(t[0, 0, 0, i:i + 200_000], s[0, j // page * 3 % 5, 0, j % page])
     att.close()
+
+
+@pytest.mark.parametrize("lens,room,keep,sink,recent", [
+    ([200, 61], 150, 100, 4, 16), ([200, 149], 150, 180, 4, 60), ([9000, 30], 8200, 900, 4, 850),
+    ([50], 1, 20, 2, 3)])
+@pytest.mark.parametrize("in_place", [False, True], ids=["out", "in_place"])
+def test_weights_of_fewer_slots_than_are_cached(lens, room, keep, sink, recent, in_place):
+    """Cached tokens past the weights' slots count as weight 0: the protected
+    ones stay, and lengths are those of the cache."""
+    T = U.torch()
+    print(f"[evict] {lens} tokens, weights of {room} slots", flush=True)
+    hkv, d = 2, 64
+    cache = A.Cache(lens, hkv, d, "bf16", 16)
+    rng = np.random.default_rng(4)
+    w = rng.exponential(size=(2, len(lens), hkv, room)).astype(np.float32)
+    w[..., ::7] = -1.0
+    mass = T.from_numpy(w.copy()).cuda()
+    guard = T.full((mass.numel() + 64,), 5.0, device="cuda")
+    out = mass if in_place else guard[:mass.numel()].view(mass.shape)
+    kept = T.full((2, len(lens), hkv, keep), -7, dtype=T.int32, device="cuda")
+    left = T.zeros(len(lens), dtype=T.int32, device="cuda")
+    att = kvx.Attention(kvx.ModelShape(2, hkv, d, 1e4), hkv, kvx.KVX_BF16)
+    att.evict(kvx.make_evict_io(cache.struct, A._int(lens), mass, kept, keep, sink=sink,
+                                recent=recent, mass_out=out, tokens_out=left))
+    T.cuda.synchronize()
+    assert left.tolist() == [min(n, keep) for n in lens]
+    assert (guard[mass.numel():] == 5.0).all()
+    got, wo = kept.cpu().numpy(), out.cpu().numpy()
+    for b, n in enumerate(lens):
+        for l in range(2):
+            for h in range(hkv):
+                full = np.zeros(max(n, room), np.float32)
+                full[:room] = w[l, b, h]
+                ref = R.keep(full[:n], keep, sink, recent)
+                assert (got[l, b, h, :len(ref)] == ref).all(), (l, b, h)
+                assert (got[l, b, h, len(ref):] == -1).all()
+                r = min(len(ref), room)
+                assert (wo[l, b, h, :r] == full[ref][:r]).all()
+                assert (wo[l, b, h, r:min(room, max(n, keep))] == 0).all()
+                for kv in range(2):
+                    rows = cache.read(kv, l, b, len(ref))[:, h]
+                    assert T.equal(rows, cache.rows[kv][l][b][ref, h]), (l, b, h, kv)
+    att.close()
+
+
+def test_more_weights_than_an_index_holds_are_refused():
+    T = U.torch()
+    cache = A.Cache([20], 1, 64, "bf16", 16, layers=1)
+    att = kvx.Attention(kvx.ModelShape(1, 1, 64, 1e4), 1, kvx.KVX_BF16)
+    mass = T.zeros(1, 1, 1, 32, device="cuda")
+    kept = T.full((1, 1, 1, 8), -7, dtype=T.int32, device="cuda")
+    io = kvx.make_evict_io(cache.struct, A._int([20]), mass, kept, 8, mass_out=mass)
+    io.mass_capacity = 2 ** 31 - 1
+    with pytest.raises(kvx.KvxError) as e:
+        att.evict(io)
+    T.cuda.synchronize()
+    assert e.value.status == kvx.KVX_ESHAPE and (kept == -7).all()
+    att.close()
