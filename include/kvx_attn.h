@@ -154,6 +154,8 @@ kvx_status kvx_attn_workspace_bytes(const kvx_attn* attn, size_t* bytes);
  * memory of the caller's, 16-byte aligned, not read before it is written;
  * calls that share one must not overlap.  Scores, softmax statistics and sums
  * are fp32; weights are rounded to bf16 for their product with bf16 values.
+ * Values whose magnitudes add up to less than 2^104 over a context's slots give
+ * finite outputs whatever the scores are.
  * Results depend on no order of execution: equal calls give equal bits. */
 kvx_status kvx_attn_forward(const kvx_attn* attn, const kvx_attn_io* io, void* workspace,
                             size_t workspace_bytes, void* stream);
