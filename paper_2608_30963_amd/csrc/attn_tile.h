@@ -510,8 +510,7 @@ __device__ __forceinline__ bool exceeds(const Softmax& st, float top, float by) 
 // How far scores may pass their reference without a rescaling (log2 units).
 // Weights and sums are floating-point numbers, as exact at 2^24 as at 1.  What
 // bounds it is the sums of values, which grow by the same: values of sum |v| up to
-// 2^104 over the slots stay below fp32's largest, 2^128.  Scores of 16 and more over
-// all of their first tile's are rare; tiles after one take the last loop.
+// 2^104 over the slots stay below fp32's largest, 2^128.
 constexpr float kRoom = 24.f;
 
 template <int NB>
