@@ -310,7 +310,14 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
   constexpr int kCopies = TK * L::kRowBytes / 1024 / WAVES;   // of a wave, keys or values
   constexpr int kStep = WAVES * R;                            // rows from one to the wave's next
   constexpr int kRun = kStep < 16 ? 16 / kStep : 1;           // of them in 16 slots
-  const int lane = threadIdx.x % 64, sub = lane / L::kChunks;
+  int lane = threadIdx.x % 64;
+  if constexpr (kCopies > 8) {
+    // what copies derive from the lane is formed anew for every tile: the
+    // compiler would take all of it out of the caller's loop, keep it in scratch
+    // memory and wait for every copy in flight where it reads it back
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(lane));
+  }
+  const int sub = lane / L::kChunks;
   const uint32_t st = static_cast<uint32_t>(c.st) * sizeof(T);
   // copy i moves rows i kStep + w R + sub: the swizzle of its low bits is the
   // lane's, that of the high ones a constant
