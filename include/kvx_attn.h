@@ -154,6 +154,8 @@ kvx_status kvx_attn_workspace_bytes(const kvx_attn* attn, size_t* bytes);
  * memory of the caller's, 16-byte aligned, not read before it is written;
  * calls that share one must not overlap.  Scores, softmax statistics and sums
  * are fp32; weights are rounded to bf16 for their product with bf16 values.
+ * Capped scores err by 2^-21 of the terms of their dot product, those of bf16
+ * calls with caps up to 128 by 2^-22 of the cap.
  * Values whose magnitudes add up to less than 2^104 over a context's slots give
  * finite outputs whatever the scores are.
  * Results depend on no order of execution: equal calls give equal bits. */

@@ -121,8 +121,10 @@ __device__ __forceinline__ int end_seen(const Context& c, int p) {
 // A capped score is cap tanh(y), y = dot scale / cap, x the dot product q.k.
 //
 // cap_part: the r of tanh(y) = 1 - 2 r, r = 1 / (1 + exp(2 y)).  Its absolute
-// error is 2^-24 or so, and the score's that times the cap: far below what
-// bf16 weights are rounded by, for which it serves.
+// error is 2^-24 or so, and the score's at most 2^-22 times the cap: up to
+// kPartCap below 2^-15, far less than bf16 weights are rounded by, for which
+// it serves there.
+constexpr double kPartCap = 128.0;
 __device__ __forceinline__ float cap_part(const AttnArgs& a, float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * a.tanh2));
 }
@@ -140,10 +142,8 @@ __device__ __forceinline__ float cap_tanh(const AttnArgs& a, float x) {
 }
 
 // Score in units of log2.
-template <bool EXACT>
 __device__ __forceinline__ float score2(const AttnArgs& a, float x) {
-  if (a.cap2 == 0.f) return x * a.scale2;
-  return EXACT ? a.cap2 * cap_tanh(a, x) : __builtin_fmaf(-2.f * a.cap2, cap_part(a, x), a.cap2);
+  return a.cap2 == 0.f ? x * a.scale2 : a.cap2 * cap_tanh(a, x);
 }
 
 // Launchers; each returns the launch's own status.

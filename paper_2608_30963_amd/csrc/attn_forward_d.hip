@@ -62,6 +62,13 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const QueryRow& q, 
 // which need other units of the compute unit.
 // ---------------------------------------------------------------------------
 
+// How the tiles that all queries see form capped scores: bf16 ones, under caps up to
+// kPartCap, by cap_part, all others by cap_tanh.  Measured (us; cap_part,
+// cap_tanh), cap 50: 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256: 124,
+// 153; 1024 in 8192, heads 28 / 4 x 128: 202, 279; 64 contexts of single tokens over up
+// to 8k slots, heads 28 / 4 x 128: 130, 134.
+enum class Cap { none, part, tanh };
+
 template <typename T, int DP>
 constexpr int chunk_tile() { return DP * sizeof(T) <= 256 ? 64 : 32; }
 
@@ -74,7 +81,7 @@ constexpr int chunk_tile() { return DP * sizeof(T) <= 256 ? 64 : 32; }
 // steps before their use.  Of the NS * 16 weights of a lane, three quarters
 // come beside the scores, the last quarter beside the first half of the
 // products (which do not need them), the largest scores beside the products.
-template <typename T, int DP, bool CAP, int NS>
+template <typename T, int DP, Cap CAP, int NS>
 __device__ __forceinline__ void middle_turn(const AttnArgs& a, const char* k, const char* v,
                                             const typename Tile<T, DP>::LaneAt& at,
                                             const uint4 (&q)[Tile<T, DP>::kQ], float c2,
@@ -87,10 +94,10 @@ __device__ __forceinline__ void middle_turn(const AttnArgs& a, const char* k, co
   static_assert(2 * NS * NB == kSteps, "");
   uint4 kf[kAheadK + 1];
   bf16x8 vf[kAheadV + 1], b;
-  // scores in log2 units less the reference: scale * s + shift.  Capped ones
+  // scores in log2 units less the reference: scale * s + shift.  Cap::part ones
   // are kept as the r of cap_part, which the line cap2 (1 - 2 r) brings there
-  const float scale = CAP ? -2.f * a.cap2 : c2;
-  const float shift = (CAP ? a.cap2 : 0.f) + (st.m2 == -INFINITY ? 0.f : -st.m2);
+  const float scale = CAP == Cap::part ? -2.f * a.cap2 : c2;
+  const float shift = (CAP == Cap::part ? a.cap2 : 0.f) + (st.m2 == -INFINITY ? 0.f : -st.m2);
   float sum[2] = {0.f, 0.f};
   auto read_key = [&](int i) __attribute__((always_inline)) {
     kf[i % (kAheadK + 1)] = *reinterpret_cast<const uint4*>(
@@ -137,19 +144,20 @@ __device__ __forceinline__ void middle_turn(const AttnArgs& a, const char* k, co
 #pragma unroll
     for (int e = kWeights * j / kSteps; e < kWeights * (j + 1) / kSteps; ++e) {
       float x = next[e / 16][e % 16];
-      if constexpr (CAP) next[e / 16][e % 16] = x = cap_part(a, x);
-      top = e == 0 ? x : CAP ? fminf(top, x) : fmaxf(top, x);
+      if constexpr (CAP == Cap::part) next[e / 16][e % 16] = x = cap_part(a, x);
+      if constexpr (CAP == Cap::tanh) next[e / 16][e % 16] = x = a.cap2 * cap_tanh(a, x);
+      top = e == 0 ? x : CAP == Cap::part ? fminf(top, x) : fmaxf(top, x);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  top = CAP ? a.cap2 - 2.f * a.cap2 * -half_max(-top) : half_max(top) * c2;
+  top = CAP == Cap::part ? a.cap2 - 2.f * a.cap2 * -half_max(-top) : half_max(top) * c2;
   st.l += sum[0] + sum[1];
 }
 
 template <typename T, int DP>
 constexpr int chunk_depth() { return DP * sizeof(T) == 512 ? 2 : 1; }
 
-template <typename T, int DP, bool CAP>
+template <typename T, int DP, Cap CAP>
 __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     forward_chunk(AttnArgs a, ForwardPlan fp) {
   using L = Tile<T, DP>;
@@ -268,7 +276,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   // 64 / 8 x 128: 1834, 1855 and 1872, 1929; fp32, 3 x 257 in 1024, heads 12 / 2 x
   // 128: 59, 58 and 60, 67; capped, 1531 in 5627, heads 8 / 4 x 256: 135, 127 and 138, 133.
   constexpr bool kInLoop = sizeof(T) == 4 || DP <= 128;
-  const float c2 = CAP ? 1.f : a.scale2;
+  const float c2 = CAP == Cap::none ? a.scale2 : 1.f;
   int kslot = 0, vslot = 0;  // of tile t
   auto after = [](int slot, int n, int by) { return slot + by >= n ? slot + by - n : slot + by; };
   auto arrive = [&](int t) __attribute__((always_inline)) {
@@ -293,7 +301,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     // 32 slots at a time: the masks and checks want registers too
 #pragma unroll 1
     for (int u = 0; u < NS; ++u)
-      odd |= edge_step<T, DP, CAP>(a, k + u * 32 * L::kRowBytes, v + u * 32 * L::kRowBytes, at, q,
+      odd |= edge_step<T, DP, CAP != Cap::none>(a, k + u * 32 * L::kRowBytes, v + u * 32 * L::kRowBytes, at, q,
                                    t * TK + 32 * u, qr.lo, qr.hi, st, acc);
   };
   int t = t0;
@@ -311,10 +319,8 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
       const char* k = lds + slot * kBytes;
 #pragma unroll
       for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, at, q);
-      if constexpr (!CAP) {
-        top = top_score(c2, s);
-      } else if constexpr (!L::kBf16) {
-        cap_scores<T>(a, s);
+      if constexpr (CAP != Cap::part) {
+        if constexpr (CAP == Cap::tanh) cap_scores<false>(a, s);
         top = top_score(c2, s);
       } else {
         f32x16 x[NS];
@@ -449,7 +455,7 @@ __device__ __forceinline__ int decode_steps(const AttnArgs& a, const Context& c,
   return (hi - lo + STEP - 1) / STEP;
 }
 
-template <typename T, int DP, bool CAP>
+template <typename T, int DP, Cap CAP>
 __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
     forward_decode(AttnArgs a, ForwardPlan fp) {
   using L = Tile<T, DP>;
@@ -482,6 +488,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
   for (int x; step >= (x = decode_steps<D::kStep>(a, c, qt)); ++qt) step -= x;
 
   const typename L::LaneAt at = L::lane_at();
+  const float c2 = CAP == Cap::none ? a.scale2 : 1.f;
   char* const ring = lds + w * NST * D::kStage;
   const uint32_t ring3 = lds_address(lds) + w * NST * D::kStage;
 
@@ -549,7 +556,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
       const int j0 = slot_of(t);
       if (j0 >= alo && j0 + 32 <= ahi) {
         f32x16 sc[1] = {L::scores(k, at, q)};
-        if constexpr (CAP) cap_scores<T>(a, sc);
+        if constexpr (CAP != Cap::none) cap_scores<CAP == Cap::part>(a, sc);
         if constexpr (L::kBf16) {
           // the first pieces of the values come beside the softmax
           constexpr int kAhead = 2 * NB < 8 ? 2 * NB : 8;
@@ -557,7 +564,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
 #pragma unroll
           for (int i = 0; i < kAhead; ++i) vf[i] = L::value_frag(v, at, i / NB, i % NB);
           __builtin_amdgcn_sched_barrier(0);
-          softmax_step(CAP ? 1.f : a.scale2, sc, st, acc);
+          softmax_step(c2, sc, st, acc);
           bf16x8 p[2];
 #pragma unroll
           for (int e = 0; e < 16; ++e) p[e / 8][e % 8] = static_cast<__bf16>(sc[0][e]);
@@ -567,11 +574,11 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
             if (i + kAhead < 2 * NB) vf[i % kAhead] = L::value_frag(v, at, (i + kAhead) / NB, (i + kAhead) % NB);
           }
         } else {
-          softmax_step(CAP ? 1.f : a.scale2, sc, st, acc);
+          softmax_step(c2, sc, st, acc);
           L::template add_values<false>(v, at, sc[0], acc);
         }
       } else {
-        odd |= edge_step<T, DP, CAP>(a, k, v, at, q, j0, qr.lo, qr.hi, st, acc);
+        odd |= edge_step<T, DP, CAP != Cap::none>(a, k, v, at, q, j0, qr.lo, qr.hi, st, acc);
       }
       __builtin_amdgcn_sched_barrier(0);
       fetch_blocks(a.c, b, slot_of(t + NST), hi, blocks);
@@ -752,18 +759,17 @@ __global__ void __launch_bounds__(256) forward_join(AttnArgs a, ForwardPlan fp) 
 
 template <typename T, int DP>
 hipError_t run_forward(const AttnArgs& a, const ForwardPlan& p, hipStream_t st) {
-  const bool cap = a.cap2 != 0.f;
-  hipError_t e;
-  if (p.decode) {
-    const dim3 block(64 * Decode<T, DP>::kWaves);
-    e = cap ? launch_on(forward_decode<T, DP, true>, dim3(p.grid), block, st, a, p)
-            : launch_on(forward_decode<T, DP, false>, dim3(p.grid), block, st, a, p);
-    if (p.splits == 1) return e;
-  } else {
-    e = cap ? launch_on(forward_chunk<T, DP, true>, dim3(p.grid), dim3(256), st, a, p)
-            : launch_on(forward_chunk<T, DP, false>, dim3(p.grid), dim3(256), st, a, p);
-    if (p.splits == 1) return e;
-  }
+  constexpr Cap kPart = sizeof(T) == 2 ? Cap::part : Cap::tanh;
+  const bool cap = a.cap2 != 0.f, part = a.cap2 <= static_cast<float>(kPartCap * kLog2e);
+  auto* kernel = p.decode ? !cap   ? forward_decode<T, DP, Cap::none>
+                            : part ? forward_decode<T, DP, kPart>
+                                   : forward_decode<T, DP, Cap::tanh>
+                 : !cap   ? forward_chunk<T, DP, Cap::none>
+                 : part   ? forward_chunk<T, DP, kPart>
+                          : forward_chunk<T, DP, Cap::tanh>;
+  const dim3 block(p.decode ? 64 * Decode<T, DP>::kWaves : 256);
+  const hipError_t e = launch_on(kernel, dim3(p.grid), block, st, a, p);
+  if (p.splits == 1) return e;
   if (e != hipSuccess) return e;
   return p.decode ? launch_on(forward_join<T, DP, 4>, dim3(p.grid, p.join_rows), dim3(256), st, a, p)
                   : launch_on(forward_join<T, DP, 1>, dim3(p.strips * a.hkv, p.join_rows / 4), dim3(256), st, a, p);

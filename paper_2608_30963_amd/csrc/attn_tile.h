@@ -553,13 +553,15 @@ __device__ __forceinline__ void softmax_step(float c, f32x16 (&s)[NS], Softmax& 
   for (int t = 0; t < NS; ++t) weights(c, s[t], st);
 }
 
-// Capped scores, in log2 units.
-template <typename T, int NS>
+// Capped scores, in log2 units; PART: by cap_part.
+template <bool PART, int NS>
 __device__ __forceinline__ void cap_scores(const AttnArgs& a, f32x16 (&s)[NS]) {
 #pragma unroll
   for (int t = 0; t < NS; ++t)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) s[t][v] = score2<sizeof(T) == 4>(a, s[t][v]);
+    for (int v = 0; v < 16; ++v)
+      s[t][v] = PART ? __builtin_fmaf(-2.f * a.cap2, cap_part(a, s[t][v]), a.cap2)
+                     : a.cap2 * cap_tanh(a, s[t][v]);
 }
 
 // Scores of slots that query lane n does not see (outside [lo, hi)) become
@@ -584,7 +586,7 @@ __device__ __forceinline__ bool edge_step(const AttnArgs& a, const char* k, cons
   using L = Tile<T, DP>;
   const bool odd = L::any_odd(v);
   f32x16 s[1] = {L::scores(k, at, q)};
-  if constexpr (CAP) cap_scores<T>(a, s);
+  if constexpr (CAP) cap_scores<false>(a, s);
   mask_scores(s[0], j0, lo, hi);
   softmax_step(CAP ? 1.f : a.scale2, s, st, acc);
   if (odd)
@@ -621,7 +623,7 @@ __device__ __forceinline__ bool careful_row(const AttnArgs& a, int b, int h, con
 #pragma unroll 1
     for (int e = half; e < a.d; e += 2) x += load_f32<T>(q + e) * load_f32<T>(kc + at + e);
     x = half_sum(x);
-    const float s = sees ? score2<true>(a, x) : -INFINITY;
+    const float s = sees ? score2(a, x) : -INFINITY;
     float top = s;
 #pragma unroll
     for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));

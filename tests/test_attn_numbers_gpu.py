@@ -50,3 +50,27 @@ def test_large_values_under_rising_scores(dtype, m, d):
     assert (np.abs(oh - ro) <= tol).all()
     assert (np.abs(A._f64(lse) - rl) <= delta + (n + 64) * EPS + 2.0 ** -22 * (1 + np.abs(rl))).all()
     att.close()
+
+
+@pytest.mark.parametrize("cap", [20.0, 100.0, 130.0, 1e4, 1e6, 1e9])
+@pytest.mark.parametrize("m,d", [(1, 128), (3, 256), (75, 64), (75, 128), (70, 256)])
+def test_bf16_scores_under_any_cap(m, d, cap):
+    """bf16 attention under caps from a score's size to far beyond: up to 128 a
+    score errs by 2^-22 of the cap, above by 2^-21 of its terms."""
+    T = U.torch()
+    print(f"[attn] bf16 cap {cap} {m} x {d}", flush=True)
+    n, hq = 400, 4
+    cache = A.Cache([n], 2, d, "bf16", 16)
+    q = A._rows(m, hq, d, "bf16", 3)
+    att = kvx.Attention(kvx.ModelShape(2, 2, d, 1e4), hq, kvx.KVX_BF16, softcap=cap)
+    out, lse = T.zeros_like(q), T.zeros(m, hq, device="cuda")
+    att.forward(kvx.make_attn_io(cache.struct, A._int([n]), q, out=out, lse=lse, layer=1, max_new=m,
+                                 q_start=A._int([0, m])), att.workspace())
+    T.cuda.synchronize()
+    ro, rl, mag, size = R.attend(A._f64(q), cache.f64(0, 1, 0), cache.f64(1, 1, 0), d ** -0.5, cap)
+    delta = (d + 8) * EPS * size + (2.0 ** -22 * cap if cap <= 128 else 2.0 ** -21 * size)
+    tol = mag * (2 * delta + (n + 64) * EPS + 2.0 ** -8)[..., None] + 2.0 ** -8 * np.abs(ro)
+    assert (np.abs(A._f64(out) - ro) <= tol).all(), (np.abs(A._f64(out) - ro) / tol).max()
+    ltol = delta + (n + 64) * EPS + 2.0 ** -22 * (1 + np.abs(rl))
+    assert (np.abs(A._f64(lse) - rl) <= ltol).all(), (np.abs(A._f64(lse) - rl) / ltol).max()
+    att.close()
