@@ -73,7 +73,7 @@ typedef struct {
   int32_t layer;             /* layer of the cache, 0-based */
   int32_t rows;              /* new tokens of all contexts */
   int32_t max_new;           /* most new tokens that any context has (>= 1; chooses
-                                the kernel, no result depends on it) */
+                                the kernel: results agree to the errors below) */
   const int32_t* q_start;    /* device [batch + 1], first row of each context, from 0
                                 to rows; NULL: one new token each (rows == batch) */
   const int32_t* tokens;     /* device [batch], cached tokens with the new ones */
@@ -154,8 +154,8 @@ kvx_status kvx_attn_workspace_bytes(const kvx_attn* attn, size_t* bytes);
  * memory of the caller's, 16-byte aligned, not read before it is written;
  * calls that share one must not overlap.  Scores, softmax statistics and sums
  * are fp32; weights are rounded to bf16 for their product with bf16 values.
- * Capped scores err by 2^-21 of the terms of their dot product, those of bf16
- * calls with caps up to 128 by 2^-22 of the cap.
+ * Capped scores err by 2^-21 of the terms of their dot product (here and in
+ * kvx_attn_mass), here those of bf16 calls with caps up to 128 by 2^-22 of the cap.
  * Values whose magnitudes add up to less than 2^104 over a context's slots give
  * finite outputs whatever the scores are.
  * Results depend on no order of execution: equal calls give equal bits. */

@@ -77,6 +77,7 @@ struct AttnArgs {
   float scale2;            // score scale * log2(e)
   float cap2;              // cap * log2(e), 0: none
   float tanh2;             // 2 scale / cap * log2(e)
+  float near, near_c[4];   // cap_near's range and coefficients
   const char* q;           // forward, mass
   int64_t q_sr, q_sh;      // elements
   char* out;
@@ -130,7 +131,7 @@ __device__ __forceinline__ float cap_part(const AttnArgs& a, float x) {
 }
 
 // tanh(y) with a relative error of 2^-22: below 0.6, where 1 - 2 r loses digits,
-// y + y^3 P(y^2), P the polynomial of least relative error there (3e-9).
+// y + y^3 P(y^2), P a polynomial of small relative error there (4.7e-9).
 __device__ __forceinline__ float cap_tanh(const AttnArgs& a, float x) {
   constexpr float kHalfLn2 = 0.34657359f;
   const float y = x * (a.tanh2 * kHalfLn2), z = y * y;
@@ -139,6 +140,16 @@ __device__ __forceinline__ float cap_tanh(const AttnArgs& a, float x) {
   p = __builtin_fmaf(z, p, 0.13331924378871918f);
   p = __builtin_fmaf(z, p, -0.33333298563957214f);
   return z < 0.36f ? __builtin_fmaf(y * z, p, y) : __builtin_fmaf(-2.f, cap_part(a, x), 1.f);
+}
+
+// cap2 tanh(y) + add for |x| < a.near, |y| < 0.5: x times a polynomial of x^2 whose
+// coefficients hold scale and cap (relative error 1.5e-8 and its roundings).
+__device__ __forceinline__ float cap_near(const AttnArgs& a, float x, float add) {
+  const float z = x * x;
+  float p = __builtin_fmaf(z, a.near_c[3], a.near_c[2]);
+  p = __builtin_fmaf(z, p, a.near_c[1]);
+  p = __builtin_fmaf(z, p, a.near_c[0]);
+  return __builtin_fmaf(x, __builtin_fmaf(z, p, a.scale2), add);
 }
 
 // Score in units of log2.

@@ -73,6 +73,21 @@ kvx_status prepare_cache(const kvx_attn* at, const kvx_cache& in, int32_t batch,
   return KVX_OK;
 }
 
+// The polynomial of tanh(y) / y in y^2 below 0.5, for scores of dot products.  No
+// range where a coefficient is past fp32 (caps far below a score's scale).
+void near_cap(const kvx_attn* at, AttnArgs& a) {
+  constexpr double c[4] = {-0.3333314389628958, 0.1332587895825113, -0.053045494297645907,
+                           0.017241491495620133};
+  const double y = at->scale / at->softcap;
+  double factor = at->scale * 1.4426950408889634;
+  a.near = static_cast<float>(0.5 / y);
+  for (int i = 0; i < 4; ++i) {
+    factor *= y * y;
+    a.near_c[i] = static_cast<float>(c[i] * factor);
+    if (!std::isfinite(a.near_c[i])) a.near = 0.f;
+  }
+}
+
 // Rows of a new tensor: (row, head) strides of `heads` head vectors.
 kvx_status check_rows(const kvx_attn* at, const void* p, const int64_t* s, int64_t heads,
                       int64_t rows) {
@@ -113,6 +128,7 @@ kvx_status prepare(const kvx_attn* at, const kvx_attn_io* io, AttnArgs& a) {
   const double log2e = 1.4426950408889634;
   a.scale2 = static_cast<float>(at->scale * log2e);
   a.cap2 = static_cast<float>(at->softcap * log2e);
+  if (at->softcap > 0.0) near_cap(at, a);
   a.tanh2 = at->softcap > 0.0 ? static_cast<float>(2.0 * at->scale / at->softcap * log2e) : 0.f;
   a.q = static_cast<const char*>(io->q);
   a.q_sr = io->q_stride[0];

@@ -34,32 +34,41 @@ __device__ __forceinline__ void copy_rest(const AttnArgs& a) {
   }
 }
 
-// How capped scores are formed: EXACT by cap_tanh, else by cap_part, which is
-// for chunks of bf16 keys.  They are bound by this arithmetic (1021 tokens over
-// 8k slots, heads 8 / 4 x 256: 56 us, with cap_tanh 72) and its error, 3e-7 of a
-// slot's weight there, is small beside that of keys of 8 bits.  Single tokens
-// wait for their keys either way.
-//
-// exp2(score - lse) of one score: `less` is -lse in log2 units, not EXACT plus
-// the cap; -inf for rows that are not there.
-template <bool CAP, bool EXACT>
+// exp2(score - lse) of one score: `less` is -lse in log2 units, -inf for rows
+// that are not there.  Weights are fp32 whatever the keys are, so capped scores
+// are formed by the tanh of relative precision.
+template <bool CAP>
 __device__ __forceinline__ float weight_of(const AttnArgs& a, float x, float less) {
-  return __builtin_amdgcn_exp2f(!CAP    ? __builtin_fmaf(x, a.scale2, less)
-                                : EXACT ? __builtin_fmaf(a.cap2, cap_tanh(a, x), less)
-                                        : __builtin_fmaf(-2.f * a.cap2, cap_part(a, x), less));
+  return __builtin_amdgcn_exp2f(CAP ? __builtin_fmaf(a.cap2, cap_tanh(a, x), less)
+                                    : __builtin_fmaf(x, a.scale2, less));
 }
 
-// Sum of the weights of the lane's slot over its 16 rows.
-template <bool CAP, bool EXACT>
+// Sum of the weights of the lane's slot over its 16 rows.  Where every score of the
+// wave is less than half its cap, which is the rule, a polynomial alone serves.
+// Measured (us; with it, without it, and by 1 - 2 / (1 + exp 2y), whose error in a
+// weight was ten times as large), cap 50: 1021 tokens over 8k slots, heads 8 / 4 x
+// 256: 68, 80, 66; 1024 over 8k, heads 28 / 4 x 128: 169, 203, 155; 64 contexts of
+// single tokens over up to 4k slots, heads 8 / 4 x 256: 69, 74, -.
+template <bool CAP>
 __device__ __forceinline__ float weigh(const AttnArgs& a, const f32x16& s, const float (&less)[16]) {
   float sum[2] = {0.f, 0.f};
+  if constexpr (CAP) {
+    float top = 0.f;
 #pragma unroll
-  for (int v = 0; v < 16; ++v) sum[v % 2] += weight_of<CAP, EXACT>(a, s[v], less[v]);
+    for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(s[v]));
+    if (!__any(!(top < a.near))) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum[v % 2] += __builtin_amdgcn_exp2f(cap_near(a, s[v], less[v]));
+      return sum[0] + sum[1];
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < 16; ++v) sum[v % 2] += weight_of<CAP>(a, s[v], less[v]);
   return sum[0] + sum[1];
 }
 
 // The same where rows may not see the lane's slot j; r0 is the first row.
-template <bool CAP, bool EXACT>
+template <bool CAP>
 __device__ __forceinline__ float weigh_seen(const AttnArgs& a, const Context& c, const f32x16& s,
                                             const float (&less)[16], int r0, int j) {
   const int h = threadIdx.x % 64 / 32;
@@ -67,7 +76,7 @@ __device__ __forceinline__ float weigh_seen(const AttnArgs& a, const Context& c,
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
     const QueryRow q = query_row(a, c, r0 + 8 * (v / 4) + 4 * h + v % 4);
-    const float p = weight_of<CAP, EXACT>(a, s[v], less[v]);
+    const float p = weight_of<CAP>(a, s[v], less[v]);
     if (j >= q.lo && j < q.hi) sum += p;
   }
   return sum;
@@ -180,8 +189,8 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
         const int j0 = slot_of(t);
         const f32x16 sc = L::template scores<true>(ring + t % NST * kStage, at, q);
         const float sum = half_sum(j0 >= alo && j0 + 32 <= ahi
-                                       ? weigh<CAP, true>(a, sc, less)
-                                       : weigh_seen<CAP, true>(a, c, sc, less, r0, j0 + n));
+                                       ? weigh<CAP>(a, sc, less)
+                                       : weigh_seen<CAP>(a, c, sc, less, r0, j0 + n));
         put(t, (from ? earlier[w][t % NST][n] : 0.f) + sum);
         __builtin_amdgcn_sched_barrier(0);
         fetch_blocks(a.c, b, slot_of(t + NST), hi, blocks);
@@ -216,7 +225,6 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
 
 template <typename T, int DP, bool CAP, int QW>
 __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk(AttnArgs a, int blocks_per) {
-  constexpr bool kExact = sizeof(T) == 4;
   using L = Tile<T, DP>;
   constexpr int KW = 8 / QW, kRows = 32 * QW, kBytes = kRows * L::kRowBytes;
   constexpr int kCopies = kBytes / 1024 / 8;  // of a wave
@@ -301,7 +309,7 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
     for (int x = 0; x < 4; ++x) {
       const f32x4 y = *reinterpret_cast<const f32x4*>(&lse[buf][qw * 32 + 8 * x + 4 * half]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) less[4 * x + e] = (CAP && !kExact ? a.cap2 : 0.f) - kLog2e * y[e];
+      for (int e = 0; e < 4; ++e) less[4 * x + e] = -kLog2e * y[e];
     }
     const f32x16 sc = L::template scores<false, 4>(lds + buf * kBytes + qw * 32 * L::kRowBytes, at, key);
     // whether all 32 rows see all of the wave's slots
@@ -310,9 +318,9 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
     seen_by(a, c, r0, r0, x, ahi);
     seen_by(a, c, min(r0 + 31, c.m * a.group - 1), min(r0 + 31, c.m * a.group - 1), alo, x);
     if (ja >= alo && ja + 32 <= ahi && r0 + 32 <= c.m * a.group)
-      sum += weigh<CAP, kExact>(a, sc, less);
+      sum += weigh<CAP>(a, sc, less);
     else
-      sum += weigh_seen<CAP, kExact>(a, c, sc, less, r0, j);
+      sum += weigh_seen<CAP>(a, c, sc, less, r0, j);
   }
   sum = half_sum(sum);
   // the row waves' sums, in their order

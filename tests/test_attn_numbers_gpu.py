@@ -74,3 +74,28 @@ def test_bf16_scores_under_any_cap(m, d, cap):
     ltol = delta + (n + 64) * EPS + 2.0 ** -22 * (1 + np.abs(rl))
     assert (np.abs(A._f64(lse) - rl) <= ltol).all(), (np.abs(A._f64(lse) - rl) / ltol).max()
     att.close()
+
+
+@pytest.mark.parametrize("cap", [1e-6, 0.5, 2.0, 20.0, 1000.0, 1e6])
+@pytest.mark.parametrize("m,d", [(1, 128), (75, 64), (75, 128), (70, 256)])
+def test_bf16_weights_under_any_cap(m, d, cap):
+    """Cached tokens' weights, which are fp32 whatever the keys are: a score errs
+    by 2^-21 of its terms, by single tokens and by chunks alike."""
+    T = U.torch()
+    print(f"[mass] bf16 cap {cap} {m} x {d}", flush=True)
+    n, hq = 400, 4
+    cache = A.Cache([n], 2, d, "bf16", 16)
+    q = A._rows(m, hq, d, "bf16", 3)
+    att = kvx.Attention(kvx.ModelShape(2, 2, d, 1e4), hq, kvx.KVX_BF16, softcap=cap)
+    k = cache.f64(0, 1, 0)
+    lse = T.from_numpy(R.attend(A._f64(q), k, k, d ** -0.5, cap)[1].astype(np.float32)).cuda()
+    mass = T.zeros(1, 2, n, device="cuda")
+    att.mass(kvx.make_attn_io(cache.struct, A._int([n]), q, lse=lse, layer=1, max_new=m, mass=mass,
+                              q_start=A._int([0, m])))
+    T.cuda.synchronize()
+    given = A._f64(lse)
+    ref, size = R.mass(A._f64(q), k, given, d ** -0.5, cap)
+    delta = ((d + 8) * EPS + 2.0 ** -21) * size
+    tol = ref * (2 * delta + (m * hq + 64) * EPS + 4 * EPS * (np.abs(given).max() + 1)) + 2.0 ** -126
+    assert (np.abs(A._f64(mass)[0] - ref) <= tol).all(), (np.abs(A._f64(mass)[0] - ref) / tol).max()
+    att.close()
