@@ -639,12 +639,42 @@ def kvx_attn_create(model, n_heads: int, dtype: int, softcap: float = 0.0, scale
     return h.value
 
 
+def _plain(what, t, dtype, size=None, last=None):
+    """Refuses a tensor that the library would read as something else: it takes
+    ``dtype`` elements one after another, ``size`` of them at least (``last``: in
+    rows of so many)."""
+    if not hasattr(t, "data_ptr"):
+        return  # none, or an address, which the caller answers for
+    if str(t.dtype) != "torch." + dtype:
+        raise ValueError(f"{what} is {t.dtype}, expected torch.{dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    if size is not None and t.numel() < size:
+        raise ValueError(f"{what} has {t.numel()} elements, expected {size}")
+    if last is not None and (t.dim() == 0 or t.shape[-1] != last):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected rows of {last}")
+
+
+def _one_device(tensors):
+    """Refuses tensors of different devices."""
+    found = {str(t.device) for t in tensors if hasattr(t, "data_ptr")}
+    if len(found) > 1:
+        raise ValueError(f"tensors on different devices: {sorted(found)}")
+
+
 def make_cache(k, v, block_table=None, stride=(0, 0, 0, 0), block_size: Optional[int] = None,
                num_blocks: Optional[int] = None, capacity: Optional[int] = None) -> Cache:
     """The kvx_cache struct of device tensors ``k``/``v``: contiguous
     [L][B][H][capacity][D], or with ``block_table`` ([B][max_blocks] int32)
     paged [L][num_blocks][H][block_size][D].  Other layouts: give ``stride``
     and the sizes that the shape does not show."""
+    if hasattr(k, "data_ptr") and hasattr(v, "data_ptr"):
+        if k.element_size() != v.element_size():
+            raise ValueError(f"k is {k.dtype}, v is {v.dtype}")
+        if not any(stride) and not (k.is_contiguous() and v.is_contiguous() and k.shape == v.shape):
+            raise ValueError("without strides, k and v must be contiguous and of one shape")
+    _plain("block_table", block_table, "int32")
+    _one_device((k, v, block_table))
     if block_table is None:
         c = Cache(_ptr(k), _ptr(v), (C.c_int64 * 4)(*[int(x) for x in stride]),
                   int(k.shape[3] if capacity is None else capacity), None, 0, 0, 0)
@@ -673,7 +703,26 @@ def make_attn_io(cache: Cache, tokens, q=None, *, layer: int = 0, q_start=None, 
     tensors (any row and head strides); ``mass`` [B][Hkv][mass_capacity].  The
     struct keeps its tensors alive."""
     first = next(t for t in (q, new_q, new_k) if t is not None)
-    io = AttnIO(int(tokens.shape[0]), int(layer), int(first.shape[0]), int(max_new),
+    batch, rows = int(tokens.shape[0]), int(first.shape[0])
+    k = getattr(cache, "tensors", (None,))[0]
+    for name, t in (("q", q), ("new_q", new_q), ("new_k", new_k), ("new_v", new_v), ("out", out)):
+        if t is None:
+            continue
+        like = q if name in ("new_q", "out") else new_k if name == "new_v" else None
+        if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != first.shape[2] or \
+                (like is not None and t.shape != like.shape):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}")
+        if t.element_size() != (k if hasattr(k, "element_size") else first).element_size():
+            raise ValueError(f"{name} is {t.dtype}, the cache is not")
+    _plain("tokens", tokens, "int32")
+    _plain("q_start", q_start, "int32", batch + 1)
+    _plain("pos", pos, "int32", last=rows)
+    _plain("prefix", prefix, "int32", batch)
+    _plain("lse", lse, "float32", None if q is None else rows * int(q.shape[1]))
+    _plain("mass", mass, "float32")
+    _plain("mass_in", mass_in, "float32", None if mass is None else mass.numel())
+    _one_device((k, tokens, q, q_start, new_q, new_k, new_v, pos, prefix, out, lse, mass_in, mass))
+    io = AttnIO(batch, int(layer), rows, int(max_new),
                 _ptr(q_start), _ptr(tokens), cache, _ptr(new_q), _ptr(new_k), _ptr(new_v),
                 _row_stride(new_q), _row_stride(new_k), _row_stride(new_v), _ptr(pos), _ptr(q),
                 _row_stride(q), int(window), _ptr(prefix), _ptr(out), _row_stride(out), _ptr(lse),
@@ -687,6 +736,17 @@ def make_evict_io(cache: Cache, tokens, mass, kept, keep: int, *, sink: int = 0,
                   mass_out=None, tokens_out=None, dst: Optional[Cache] = None) -> EvictIO:
     """Build the kvx_evict_io struct: ``mass`` [L][B][Hkv][mass_capacity],
     ``kept`` int32 [L][B][Hkv][keep]; ``dst`` None compacts in place."""
+    _plain("tokens", tokens, "int32")
+    _plain("mass", mass, "float32")
+    _plain("mass_out", mass_out, "float32", mass.numel())
+    _plain("kept", kept, "int32", mass.numel() // max(1, int(mass.shape[-1])) * int(keep))
+    _plain("tokens_out", tokens_out, "int32", int(tokens.shape[0]))
+    k = getattr(cache, "tensors", (None,))[0]
+    to = None if dst is None else getattr(dst, "tensors", (None,))[0]
+    if hasattr(to, "element_size") and hasattr(k, "element_size") and \
+            to.element_size() != k.element_size():
+        raise ValueError(f"dst is {to.dtype}, the cache {k.dtype}")
+    _one_device((k, to, tokens, mass, mass_out, kept, tokens_out))
     io = EvictIO(int(tokens.shape[0]), _ptr(tokens), int(keep), int(sink), int(recent), cache,
                  Cache() if dst is None else dst, _ptr(mass), _ptr(mass_out),
                  int(mass.shape[-1]), _ptr(kept), _ptr(tokens_out))
@@ -745,25 +805,75 @@ class Attention:
     def __init__(self, model, n_heads, dtype, softcap=0.0, scale=0.0, inv_freq=None,
                  pair_axis=None, n_axes=None):
         self.handle = None
+        self.model, self.n_heads, self.dtype = model, int(n_heads), int(dtype)
+        self.n_axes = n_axes if n_axes is not None else \
+            1 if pair_axis is None else max(int(x) for x in pair_axis) + 1
         self.handle = kvx_attn_create(model, n_heads, dtype, softcap, scale, inv_freq, pair_axis,
                                       n_axes)
 
     def workspace(self, io=None):
-        """A workspace for forward calls (any of this handle's, one at a time)."""
+        """A workspace for forward calls: any of this handle's, one at a time, so
+        that ``io`` need not be given."""
         import torch
         return torch.empty(kvx_attn_workspace_bytes(self.handle), dtype=torch.uint8,
                            device="cuda")
 
+    def _fits(self, io):
+        """Whether a struct's tensors are this model's and on a GPU; asked once of a
+        struct."""
+        m, tensors = self.model, getattr(io, "tensors", None)
+        if tensors is None:
+            return  # built by hand, which the caller answers for
+        heads, d, width = int(m.n_kv_heads), int(m.head_dim), 4 if self.dtype == KVX_F32 else 2
+        caches = [c for c in (tensors[0], tensors[-1]) if isinstance(c, Cache)]
+        given = [t for t in tensors if hasattr(t, "data_ptr")]
+        for c in caches:
+            k = getattr(c, "tensors", (None,))[0]
+            if not hasattr(k, "data_ptr"):
+                continue
+            given.append(k)
+            if k.element_size() != width:
+                raise ValueError(f"the cache is {k.dtype}, the model's numbers have {width} bytes")
+            if not any(c.stride) and (k.dim() != 5 or (k.shape[2], k.shape[4]) != (heads, d)):
+                raise ValueError(f"the cache has shape {tuple(k.shape)}, the model {heads} KV "
+                                 f"heads of {d}")
+        if not all(t.is_cuda for t in given):
+            raise ValueError("tensors must be on a GPU")
+        if isinstance(io, EvictIO):
+            sets = int(m.n_layers) * io.batch * heads
+            if tensors[2].numel() < sets * int(tensors[2].shape[-1]):
+                raise ValueError(f"mass has shape {tuple(tensors[2].shape)}")
+        else:
+            _, _, q, _, new_q, new_k, new_v, pos, _, out, _, _, mass = tensors
+            for name, t, n in (("q", q, self.n_heads), ("new_q", new_q, self.n_heads),
+                               ("new_k", new_k, heads), ("new_v", new_v, heads),
+                               ("out", out, self.n_heads)):
+                if t is not None and tuple(t.shape[1:]) != (n, d):
+                    raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {n} heads of {d}")
+            if hasattr(pos, "numel") and pos.numel() < self.n_axes * io.rows:
+                raise ValueError(f"pos has shape {tuple(pos.shape)}, expected {self.n_axes} axes")
+            if hasattr(mass, "numel") and mass.numel() < io.batch * heads * int(mass.shape[-1]):
+                raise ValueError(f"mass has shape {tuple(mass.shape)}")
+        io.fits = self
+
     def append(self, io, stream=None):
+        if getattr(io, "fits", None) is not self:
+            self._fits(io)
         kvx_attn_append(self.handle, io, stream)
 
     def forward(self, io, workspace, stream=None):
+        if getattr(io, "fits", None) is not self:
+            self._fits(io)
         kvx_attn_forward(self.handle, io, workspace, stream)
 
     def mass(self, io, stream=None):
+        if getattr(io, "fits", None) is not self:
+            self._fits(io)
         kvx_attn_mass(self.handle, io, stream)
 
     def evict(self, io, stream=None):
+        if getattr(io, "fits", None) is not self:
+            self._fits(io)
         kvx_attn_evict(self.handle, io, stream)
 
     def close(self):
