@@ -43,7 +43,8 @@ typedef struct {
   int32_t n_heads;           /* query heads, a multiple of model.n_kv_heads */
   int32_t dtype;             /* kvx_dtype of q, k, v, outputs and the cache */
   double scale;              /* score scale; 0: 1 / sqrt(head_dim) */
-  double softcap;            /* c > 0: scores s become c * tanh(s / c); 0: none */
+  double softcap;            /* c > 0: scores s become c * tanh(s / c); 0: none.  Both and
+                                scale / softcap are numbers that fp32 holds */
   int32_t n_axes;            /* position axes, 1..4 */
   const uint8_t* pair_axis;  /* host [head_dim/2], position axis of rotary pair
                                 (i, i + head_dim/2); NULL: all axis 0.  Copied. */

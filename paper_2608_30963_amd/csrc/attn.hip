@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
+#include <limits>
 #include <memory>
 #include <new>
 
@@ -15,6 +16,12 @@ using namespace kvx;
 namespace {
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
+constexpr double kLog2e = 1.4426950408889634;
+
+// Whether a positive number is a normal one in fp32.
+bool normal(double x) {
+  return x >= std::numeric_limits<float>::min() && x <= std::numeric_limits<float>::max();
+}
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -79,7 +86,7 @@ void near_cap(const kvx_attn* at, AttnArgs& a) {
   constexpr double c[4] = {-0.3333314389628958, 0.1332587895825113, -0.053045494297645907,
                            0.017241491495620133};
   const double y = at->scale / at->softcap;
-  double factor = at->scale * 1.4426950408889634;
+  double factor = at->scale * kLog2e;
   a.near = static_cast<float>(0.5 / y);
   for (int i = 0; i < 4; ++i) {
     factor *= y * y;
@@ -125,11 +132,10 @@ kvx_status prepare(const kvx_attn* at, const kvx_attn_io* io, AttnArgs& a) {
   a.by_group = fast_div(at->group);
   a.d = at->model.head_dim;
   a.window = io->window;
-  const double log2e = 1.4426950408889634;
-  a.scale2 = static_cast<float>(at->scale * log2e);
-  a.cap2 = static_cast<float>(at->softcap * log2e);
+  a.scale2 = static_cast<float>(at->scale * kLog2e);
+  a.cap2 = static_cast<float>(at->softcap * kLog2e);
   if (at->softcap > 0.0) near_cap(at, a);
-  a.tanh2 = at->softcap > 0.0 ? static_cast<float>(2.0 * at->scale / at->softcap * log2e) : 0.f;
+  a.tanh2 = at->softcap > 0.0 ? static_cast<float>(2.0 * at->scale / at->softcap * kLog2e) : 0.f;
   a.q = static_cast<const char*>(io->q);
   a.q_sr = io->q_stride[0];
   a.q_sh = io->q_stride[1];
@@ -282,6 +288,11 @@ kvx_status kvx_attn_create(const kvx_attn_desc* d, kvx_attn** out) {
       !std::isfinite(d->softcap) || d->softcap < 0.0)
     return KVX_EINVAL;
   if (m.head_dim % 16 || m.head_dim > 256) return KVX_EUNSUPPORTED;
+  // what the kernels take in fp32 (prepare) is there neither infinite nor zero
+  const double scale = d->scale > 0.0 ? d->scale : 1.0 / std::sqrt(double(m.head_dim));
+  if (!normal(scale * kLog2e) ||
+      (d->softcap > 0.0 && (!normal(d->softcap * kLog2e) || !normal(2.0 * scale / d->softcap * kLog2e))))
+    return KVX_EINVAL;
   const int half = m.head_dim / 2;
   for (int i = 0; i < half; ++i) {
     if (m.inv_freq && !std::isfinite(m.inv_freq[i])) return KVX_EINVAL;
@@ -294,7 +305,7 @@ kvx_status kvx_attn_create(const kvx_attn_desc* d, kvx_attn** out) {
   at->n_heads = d->n_heads;
   at->group = d->n_heads / m.n_kv_heads;
   at->dtype = d->dtype;
-  at->scale = d->scale > 0.0 ? d->scale : 1.0 / std::sqrt(double(m.head_dim));
+  at->scale = scale;
   at->softcap = d->softcap;
   at->n_axes = d->n_axes;
   // [128] revolutions per position, then [128] axes

@@ -109,3 +109,16 @@ def test_structs_of_another_model_are_refused(kw, word):
             getattr(_attention(**kw), call)(io)
     with pytest.raises(ValueError, match=word):
         _attention(**kw).forward(_io(), torch.zeros(8))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(softcap=1e-39), dict(softcap=1e-320), dict(softcap=3e38), dict(softcap=1e300),
+    dict(scale=1e39), dict(scale=1e-39), dict(softcap=1e38, scale=1e-3), dict(softcap=1e-30, scale=1e9)])
+def test_scales_and_caps_past_fp32_are_refused(kw):
+    """The kernels would have an infinite scale, or no cap where one was asked for."""
+    base = dict(model=kvx.Model(2, 2, 64, 1e4, None), n_heads=4, dtype=kvx.KVX_BF16, scale=0.0,
+                softcap=0.0, n_axes=1, pair_axis=None)
+    base.update(kw)
+    h = C.c_void_p(123)
+    assert kvx.load().kvx_attn_create(C.byref(kvx.AttnDesc(**base)), C.byref(h)) == kvx.KVX_EINVAL
+    assert h.value is None
