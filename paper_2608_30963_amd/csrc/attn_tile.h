@@ -239,12 +239,12 @@ __device__ __forceinline__ void copy16(const char* from, uint32_t offset, uint32
                         static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p)));
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
                "v"(offset), "s"(base)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void copy16(const char* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
                "v"(from)
-               : "memory");
+               : "memory", "m0");
 }
 
 // N such copies of one base, to lds + i * STEP: the wait states are spent once.
@@ -260,7 +260,7 @@ __device__ __forceinline__ void copy16_run(const char* from, const uint32_t* off
         "s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
         "s_add_u32 m0, m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(lds),
         "v"(off[0]), "v"(off[1]), "s"(base), "n"(STEP)
-        : "memory", "scc");
+        : "memory", "m0", "scc");
   } else {
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
@@ -268,7 +268,7 @@ __device__ __forceinline__ void copy16_run(const char* from, const uint32_t* off
         "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\t"
         "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5" ::"s"(lds),
         "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "n"(STEP)
-        : "memory", "scc");
+        : "memory", "m0", "scc");
     if constexpr (N > 4) copy16_run<N - 4, STEP>(from, off + 4, lds + 4 * STEP);
   }
 }
@@ -276,7 +276,7 @@ __device__ __forceinline__ void copy16_run(const char* from, const uint32_t* off
 // 4 bytes per lane, lane i's to lds + 4 i.
 __device__ __forceinline__ void copy4(const char* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from)
-               : "memory");
+               : "memory", "m0");
 }
 
 // The blocks of a tile's slots, one per 16: read by the scalar unit a tile

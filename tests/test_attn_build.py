@@ -47,3 +47,18 @@ def test_copies_of_single_tokens_do_not_wait_for_each_other(dp, tmp_path):
         assert copies >= 32, name
         assert reloads * 8 < copies, (name, reloads, copies)
     assert seen >= 4
+
+
+def test_written_registers_are_named():
+    """Written-out instructions that set M0 or the scalar condition say so: the
+    compiler may hold either across them."""
+    seen = 0
+    for f in sorted(os.listdir(B.CSRC)):
+        text = open(os.path.join(B.CSRC, f)).read()
+        for m in re.finditer(r"asm volatile\((.*?)\);", text, re.S):
+            body = m.group(1)
+            for register, written in (("m0", r"s_\w+ m0,"), ("scc", r"s_(add|sub|and|or)_")):
+                if re.search(written, body):
+                    seen += 1
+                    assert f'"{register}"' in body.rsplit(":", 1)[1], (f, body)
+    assert seen >= 7
