@@ -167,6 +167,7 @@ struct EvictArgs {
   CacheArgs src, dst;
   const int32_t* tokens;
   int32_t layers, batch, heads, row_bytes;
+  int32_t set0;  // (layer, context, KV head) of a launch's first workgroup
   int32_t keep, sink, recent;
   bool in_place;
   const float* mass;

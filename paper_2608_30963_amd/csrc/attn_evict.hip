@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kSelThreads, 8) evict_select(EvictArgs a) {
   __shared__ int counts[2][128];
   __shared__ int scan[kWaves];
   __shared__ int found[3];  // digit, rank left within it, its count
-  const int set = blockIdx.x, tid = threadIdx.x;
+  const int set = a.set0 + blockIdx.x, tid = threadIdx.x;
   const int b = set / a.heads % a.batch;
   const int n = min(max(a.tokens[b], 0), a.src.capacity), weighed = min(n, a.mass_capacity);
   const int keep = min(n, a.keep);
@@ -210,7 +210,7 @@ constexpr int kMoveUnroll = 8;  // 16-byte pieces of a thread in flight
 // 4 heads x 256, pages of 32: 1761 MB in 370 us, 4.8 TB/s; 28 layers of 2047 to
 // 1024, 2 heads x 128: 60 MB in 12 us.
 __global__ void __launch_bounds__(kMoveThreads) evict_move(EvictArgs a, int log_pieces, int rows) {
-  const int set = blockIdx.x, v = blockIdx.y, tid = threadIdx.x;
+  const int set = a.set0 + blockIdx.x, v = blockIdx.y, tid = threadIdx.x;
   const int h = set % a.heads, b = set / a.heads % a.batch, l = set / a.heads / a.batch;
   const int n = min(max(a.tokens[b], 0), a.src.capacity);
   const int keep = min(min(n, a.keep), a.dst.capacity);
@@ -278,9 +278,16 @@ hipError_t launch_evict(const kvx_attn* at, const EvictArgs& args, hipStream_t s
     while (per * ((int64_t(most) + rows - 1) / rows) > 65535) rows *= 2;
     parts = static_cast<int>(per * ((int64_t(most) + rows - 1) / rows));
   }
-  const hipError_t e = launch_on(evict_select, dim3(sets), dim3(kSelThreads), st, a);
-  if (e != hipSuccess) return e;
-  return launch_on(evict_move, dim3(sets, 2, parts), dim3(kMoveThreads), st, a, __builtin_ctz(pieces), rows);
+  // a launch has less than 2^32 threads along x
+  constexpr int kMost = 1 << 21;
+  for (a.set0 = 0; a.set0 < sets; a.set0 += kMost) {
+    const int some = std::min(sets - a.set0, kMost);
+    hipError_t e = launch_on(evict_select, dim3(some), dim3(kSelThreads), st, a);
+    if (e == hipSuccess)
+      e = launch_on(evict_move, dim3(some, 2, parts), dim3(kMoveThreads), st, a, __builtin_ctz(pieces), rows);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace kvx

@@ -125,3 +125,27 @@ def test_more_weights_than_an_index_holds_are_refused():
     T.cuda.synchronize()
     assert e.value.status == kvx.KVX_ESHAPE and (kept == -7).all()
     att.close()
+
+
+def test_more_selections_than_a_launch_has():
+    """4.3 million (layer, context, KV head) selections of one of two tokens."""
+    T = U.torch()
+    print("[evict] 4.3 million selections", flush=True)
+    layers, batch, hkv, d = 1050, 2, 2048, 16
+    assert layers * batch * hkv > 2 ** 22
+    g = T.Generator("cuda").manual_seed(0)
+    k, v = (T.randn(layers, batch, hkv, 2, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    w = T.rand(layers, batch, hkv, 2, device="cuda", generator=g)
+    dst = [T.zeros(layers, batch, hkv, 1, d, dtype=T.bfloat16, device="cuda") for _ in range(2)]
+    kept = T.full((layers, batch, hkv, 1), -7, dtype=T.int32, device="cuda")
+    left = A._int([0, 0])
+    att = kvx.Attention(kvx.ModelShape(layers, hkv, d, 1e4), hkv, kvx.KVX_BF16)
+    att.evict(kvx.make_evict_io(kvx.make_cache(k, v), A._int([2, 2]), w, kept, 1, tokens_out=left,
+                                dst=kvx.make_cache(dst[0], dst[1])))
+    T.cuda.synchronize()
+    want = (w[..., 1] > w[..., 0]).long()  # a tie keeps the first
+    assert left.tolist() == [1, 1]
+    assert T.equal(kept[..., 0].long(), want)
+    for s, t in zip((k, v), dst):
+        assert T.equal(t[..., 0, :], T.where(want[..., None] == 1, s[..., 1, :], s[..., 0, :]))
+    att.close()
