@@ -771,6 +771,8 @@ def kvx_attn_workspace_bytes(attn: int) -> int:
 
 def kvx_attn_forward(attn: int, io: AttnIO, workspace, stream=None) -> int:
     """``workspace``: a device tensor of at least kvx_attn_workspace_bytes."""
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("the workspace must be a contiguous tensor on a GPU")
     st = load().kvx_attn_forward(attn, C.byref(io), workspace.data_ptr(),
                                  workspace.numel() * workspace.element_size(),
                                  _stream_handle(stream))
