@@ -178,10 +178,17 @@ struct EvictArgs {
 };
 hipError_t launch_evict(const kvx_attn* at, const EvictArgs& a, hipStream_t st);
 
+// Whether a launch has less than 2^32 threads along x.  The runtime takes more
+// without an error and runs a part of them.
+inline bool launchable(int64_t groups, int threads) {
+  return groups * threads <= int64_t(UINT32_MAX);
+}
+
 // A launch with its own status: the runtime's last error may be another
 // call's.  Each argument is converted to the kernel's parameter type.
 template <typename... P, typename... A>
 hipError_t launch_on(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, const A&... a) {
+  if (!launchable(grid.x, block.x)) return hipErrorInvalidConfiguration;
   return [&](P... p) {
     void* args[] = {&p...};
     return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, args, 0, st);

@@ -56,7 +56,10 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
   // chunk), heads 28 / 4 x 128, 16 contexts of 4096 slots: 28 rows 36.6, 36.1; 56
   // rows 54.4, 44.0; 112 rows 83.0, 56.6; one of 128k: 7 rows 53, 239; 28 rows 62,
   // 241.  A few contexts of 1024 slots lose by it: 28 rows 18.7, 15.0.
-  p.decode = int64_t(max_new) * at->group <= kDecodeRows;
+  const int64_t strips = (int64_t(a.rows) * at->group + kChunkRows - 1) / kChunkRows +
+                         std::min(a.batch, a.rows);
+  const int64_t units = strips * a.hkv;
+  p.decode = int64_t(max_new) * at->group <= kDecodeRows || !launchable(units, 256);
   if (p.decode) {
     p.grid = at->n_cu;
     p.splits = 0;  // as many as the lengths give
@@ -65,14 +68,10 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
     // 16.8; 64 contexts of 300 slots, heads 64 / 8: 29.0, 25.8; 32 of 1024, heads
     // 28 / 4: 21.2, 21.6
     if (a.c.capacity <= 512) p.splits = 1;
-    p.join_rows = max_new * at->group;  // at most kDecodeRows
+    p.join_rows = static_cast<int>(std::min(int64_t(max_new) * at->group, int64_t(kDecodeRows)));
   } else {
-    const int64_t strips = (int64_t(a.rows) * at->group + kChunkRows - 1) / kChunkRows +
-                           std::min(a.batch, a.rows);
-    const int64_t units = strips * a.hkv;
     p.join_rows = kChunkRows;
     p.splits = splits_of(at, units);
-    if (units * p.splits > INT32_MAX) return hipErrorInvalidValue;
     p.strips = static_cast<int>(strips);
     p.grid = static_cast<int>(units * p.splits);
   }

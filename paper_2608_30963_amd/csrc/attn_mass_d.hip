@@ -337,12 +337,17 @@ __global__ void __launch_bounds__(512, DP * sizeof(T) <= 256 ? 2 : 1) mass_chunk
   }
 }
 
+// Workgroups of a context and head.
+template <int QW>
+int chunk_groups(const AttnArgs& a) {
+  constexpr int slots = 8 / QW * 32;
+  return (std::min(a.mass_capacity, a.c.capacity) + slots - 1) / slots;
+}
+
 template <typename T, int DP, int QW>
 hipError_t run_chunk(const AttnArgs& a, hipStream_t st) {
-  constexpr int slots = 8 / QW * 32;
-  const int per = (std::min(a.mass_capacity, a.c.capacity) + slots - 1) / slots;
+  const int per = chunk_groups<QW>(a);
   const int64_t grid = static_cast<int64_t>(per) * a.batch * a.hkv;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
   return a.cap2 != 0.f
              ? launch_on(mass_chunk<T, DP, true, QW>, dim3(static_cast<unsigned>(grid)), dim3(512), st, a, per)
              : launch_on(mass_chunk<T, DP, false, QW>, dim3(static_cast<unsigned>(grid)), dim3(512), st, a, per);
@@ -352,7 +357,9 @@ hipError_t run_chunk(const AttnArgs& a, hipStream_t st) {
 
 template <typename T, int DP>
 hipError_t run_mass(const AttnArgs& a, bool decode, int n_cu, hipStream_t st) {
-  if (decode) {
+  // workgroups go by the capacity, which may be reserved far beyond the tokens: those
+  // that no launch takes are left to the ring, which goes by the tokens
+  if (decode || !launchable(static_cast<int64_t>(chunk_groups<2>(a)) * a.batch * a.hkv, 512)) {
     const dim3 block(64 * ring_waves(32 * DP * sizeof(T)));
     return a.cap2 != 0.f ? launch_on(mass_decode<T, DP, true>, dim3(n_cu), block, st, a)
                          : launch_on(mass_decode<T, DP, false>, dim3(n_cu), block, st, a);

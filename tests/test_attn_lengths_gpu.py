@@ -213,3 +213,33 @@ def test_weights_of_slots_times_heads_past_32_bits(hq, n, m):
     got = A._f64(mass[0, 0, int(j[0]):])
     assert (np.abs(got - 0.5 - ref[0]) <= ref[0] * rel + 2 * EPS * (0.5 + ref[0]) + 2.0 ** -126).all()
     att.close()
+
+
+def test_weights_in_a_cache_of_far_more_slots_than_tokens():
+    """Room for 131072 slots in each of 1100 contexts of 70 tokens: more workgroups
+    by the room than a launch has."""
+    T = U.torch()
+    print("[mass] room for 144 million slots", flush=True)
+    batch, hkv, hq, d, page, n, m = 1100, 8, 128, 16, 16, 70, 3
+    room = 131072
+    assert room // 128 * batch * hkv * 512 > 2 ** 32
+    per = -(-n // page)
+    table = T.full((batch, room // page), 2 ** 30, dtype=T.int32, device="cuda")
+    table[:, :per] = T.arange(batch * per, dtype=T.int32, device="cuda").view(batch, per)
+    g = T.Generator("cuda").manual_seed(0)
+    k = T.randn(1, batch * per, hkv, page, d, device="cuda", generator=g).bfloat16()
+    q = T.randn(batch * m, hq, d, device="cuda", generator=g).bfloat16()
+    lse = T.full((batch * m, hq), 4.5, device="cuda")
+    mass = T.full((batch, hkv, room), 7.0, device="cuda")
+    att = kvx.Attention(kvx.ModelShape(1, hkv, d, 1e4), hq, kvx.KVX_BF16)
+    att.mass(kvx.make_attn_io(kvx.make_cache(k, k, table), A._int([n] * batch), q, lse=lse, mass=mass,
+                              max_new=m, q_start=A._int(range(0, batch * m + 1, m))))
+    T.cuda.synchronize()
+    assert (mass[:, :, n:] == 0).all()
+    kh, qh, got = A._f64(k), A._f64(q), A._f64(mass[:, :, :n])
+    for b in range(0, batch, 61):
+        rows = kh[0, b * per:b * per + per].transpose(0, 2, 1, 3).reshape(per * page, hkv, d)[:n]
+        ref, size = R.mass(qh[b * m:b * m + m], rows, np.full((m, hq), 4.5), d ** -0.5)
+        rel = 2 * A._delta(size, d, 0.0) + (m * hq + 64) * EPS + 4 * EPS * 5.5
+        assert (np.abs(got[b] - ref) <= ref * rel + 2.0 ** -126).all(), b
+    att.close()
