@@ -94,7 +94,8 @@ typedef struct {
   void* q;
   int64_t q_stride[2];
   /* forward and mass: visibility.  New token of slot p >= 0 sees slot j < n if
-   * (j <= p or j < prefix[b]) and (window == 0 or j > p - window). */
+   * (j <= p or j < prefix[b]) and (window == 0 or j > p - window).  A window counts
+   * slots: after an eviction it reaches further back than as many positions. */
   int32_t window;            /* >= 0 */
   const int32_t* prefix;     /* device [batch] or NULL (none) */
   /* forward: outputs; a row that sees nothing gets out 0, lse -inf */
@@ -171,7 +172,8 @@ kvx_status kvx_attn_mass(const kvx_attn* attn, const kvx_attn_io* io, void* stre
  * and of the others those of the largest mass, ties to the lowest slot, a NaN
  * counting as -inf.  Kept rows move to the front in their order.  Every head
  * of every layer keeps the same number, so one length per context serves.
- * Keys stay rotated at their original positions. */
+ * Keys stay rotated at their original positions.  In place, no two contexts may
+ * share a block of kept or dropped tokens. */
 kvx_status kvx_attn_evict(const kvx_attn* attn, const kvx_evict_io* io, void* stream);
 
 #ifdef __cplusplus

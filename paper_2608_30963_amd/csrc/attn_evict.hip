@@ -86,7 +86,8 @@ __device__ __forceinline__ int chunk_scan(uint32_t on, int rounds, int* count, i
 // exponent and two bits of the number, so that counts of like weights fall on
 // more than a few counters.  Up to 8192 slots the weights are read once and
 // stay in registers; longer contexts are read again for each of the steps.
-// Bound by latency: three rounds of LDS counters, their scan and the search.
+// Bound by latency: three rounds of LDS counters, their scan and the search (the
+// last decides nothing where no two weights share the first 22 bits).
 // Measured: 56 selections of 1024 of 2047 slots 11.8 us, 416 of 2048 of up to 8192
 // 24 us.
 __global__ void __launch_bounds__(kSelThreads, 8) evict_select(EvictArgs a) {
@@ -207,8 +208,8 @@ constexpr int kMoveUnroll = 8;  // 16-byte pieces of a thread in flight
 // before any is written.  In place that is safe for every later step too: kept
 // slots rise, so row i comes from slot >= i.
 // Bound by memory.  Measured: 26 layers, 4 contexts of up to 8192 slots to 2048,
-// 4 heads x 256, pages of 32: 1761 MB in 370 us, 4.8 TB/s; 28 layers of 2047 to
-// 1024, 2 heads x 128: 60 MB in 12 us.
+// 4 heads x 256, pages of 32: 1761 MB in 370 to 410 us, 4.3 to 4.8 TB/s; 28 layers of
+// 2047 to 1024, 2 heads x 128: 60 MB in 12 us.
 __global__ void __launch_bounds__(kMoveThreads) evict_move(EvictArgs a, int log_pieces, int rows) {
   const int set = a.set0 + blockIdx.x, v = blockIdx.y, tid = threadIdx.x;
   const int h = set % a.heads, b = set / a.heads % a.batch, l = set / a.heads / a.batch;

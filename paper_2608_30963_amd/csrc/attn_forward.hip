@@ -63,7 +63,8 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
   if (p.decode) {
     p.grid = at->n_cu;
     p.splits = 0;  // as many as the lengths give
-    // short contexts: a workgroup a unit, no join.  Measured (us, captured;
+    // caches of few slots (the host knows no lengths): a workgroup a unit, no
+    // join.  Measured (us, captured;
     // split, whole), heads 12 / 2: 128 slots 10.5, 7.5; 512 10.9, 11.4; 1024 11.5,
     // 16.8; 64 contexts of 300 slots, heads 64 / 8: 29.0, 25.8; 32 of 1024, heads
     // 28 / 4: 21.2, 21.6

@@ -46,13 +46,16 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const QueryRow& q, 
 // Chunks: S^T = K Q^T by 32 x 32 matrix instructions, so that a lane holds one
 // query's scores and its weights are the second operand of O^T = V^T P^T as
 // they stand: no weight changes lanes.  One pass with a running reference and
-// sum.  Bound by the matrix units, and where scores are capped or heads are 256
-// wide by what one or two waves of a SIMD can issue beside them.  Measured: 4096 tokens
-// after 12k, heads 64 / 8 x 128: 1.85 ms, 1.04 PFLOP/s, where the card's power
-// sets the clock (the same with zeros: 1.47 ms); 1531 tokens in 5627 slots, window 4096,
-// heads 8 / 4 x 256, capped: 114 us, 450 TFLOP/s; fp32, 3 contexts of up to 257
-// in 1024 slots, heads 12 / 2 x 128: 55 us, 46 TFLOP/s of 154, since its 232
-// workgroups do not divide the work evenly and start and join take a quarter.
+// sum.  Bound by the matrix units, and where heads are 256 wide by the LDS as
+// much: each of 4 waves reads all of a tile's keys and values for 32 rows, about
+// a thousand clocks, as its matrix work takes, and one wave a SIMD has to
+// overlap the two.  Measured: 4096 tokens after 12k, heads 64 / 8 x 128: 1.90 ms,
+// 1.01 PFLOP/s, where the card's power sets the clock (with zeros a fifth less
+// time); 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256, capped: 118 us,
+// 435 TFLOP/s; fp32, 3 contexts of up to 257 in 1024 slots, heads 12 / 2 x 128:
+// 56 us, 46 TFLOP/s of 154: a tile's scores, weights and products follow each
+// other, its 232 workgroups do not divide the work evenly, and start and join
+// take a quarter.
 //
 // 4 waves of 32 query rows share tiles of 64 slots (32 where rows have
 // over 256 bytes), copied straight into LDS ahead of their use: values DEPTH
@@ -63,10 +66,10 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const QueryRow& q, 
 // ---------------------------------------------------------------------------
 
 // How the tiles that all queries see form capped scores: bf16 ones, under caps up to
-// kPartCap, by cap_part, all others by cap_tanh.  Measured (us; cap_part,
-// cap_tanh), cap 50: 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256: 124,
+// kPartCap, by cap_part, all others by cap_tanh.  Measured (us, a few calls in a
+// row; cap_part, cap_tanh), cap 50: 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256: 125,
 // 153; 1024 in 8192, heads 28 / 4 x 128: 202, 279; 64 contexts of single tokens over up
-// to 8k slots, heads 28 / 4 x 128: 130, 134.
+// to 8k slots, heads 28 / 4 x 128: 124, 134.
 enum class Cap { none, part, tanh };
 
 template <typename T, int DP>
@@ -271,8 +274,8 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
   // before the first that all of the wave's queries see (windows), tiles that
   // all see, and the rest.  Where a score passes the reference by 2^kRoom in the
   // middle one, the sums are rescaled there; bf16 rows of 256 columns, short of
-  // registers, leave it and enter it again with that tile's.  Measured (us;
-  // there, left), scores of N(0, 1) and of ten times that: 4096 tokens in 16k, heads
+  // registers, leave it and enter it again with that tile's.  Measured (us, a
+  // few calls in a row; there, left), scores of N(0, 1) and of ten times that: 4096 tokens in 16k, heads
   // 64 / 8 x 128: 1834, 1855 and 1872, 1929; fp32, 3 x 257 in 1024, heads 12 / 2 x
   // 128: 59, 58 and 60, 67; capped, 1531 in 5627, heads 8 / 4 x 256: 135, 127 and 138, 133.
   constexpr bool kInLoop = sizeof(T) == 4 || DP <= 128;
@@ -433,7 +436,11 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
 // Measured, heads 28 / 4 x 128: 64 contexts of up to 8k slots, 605 MB in 118 us,
 // 5.1 TB/s; one of 128k, 268 MB in 61 us, of which the join of 64 pieces takes 10;
 // one of 300 slots, heads 12 / 2: 11.8 us, the latency of lengths, block
-// numbers, rows and two barriers one after another.
+// numbers, two rounds of rows (two stages of copies are asked for one after the
+// other) and two barriers.  Wider heads have fewer waves and stages, and registers
+// that are read back from scratch memory once or twice a tile: heads 8 / 4, 64
+// contexts of up to 8k slots: 256 columns 1208 MB in 353 us, 3.4 TB/s, 192 columns
+// 906 MB in 392; fp32, 16 of up to 4k, 256 columns: 309 MB in 252.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP>

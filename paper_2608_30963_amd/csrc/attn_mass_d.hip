@@ -45,10 +45,10 @@ __device__ __forceinline__ float weight_of(const AttnArgs& a, float x, float les
 
 // Sum of the weights of the lane's slot over its 16 rows.  Where every score of the
 // wave is less than half its cap, which is the rule, a polynomial alone serves.
-// Measured (us; with it, without it, and by 1 - 2 / (1 + exp 2y), whose error in a
-// weight was ten times as large), cap 50: 1021 tokens over 8k slots, heads 8 / 4 x
-// 256: 68, 80, 66; 1024 over 8k, heads 28 / 4 x 128: 169, 203, 155; 64 contexts of
-// single tokens over up to 4k slots, heads 8 / 4 x 256: 69, 74, -.
+// Measured (us, a few calls in a row; with it, without it, and by 1 - 2 / (1 + exp
+// 2y), whose error in a weight was ten times as large), cap 50: 1021 tokens over 8k
+// slots, heads 8 / 4 x 256: 68, 80, 66; 1024 over 8k, heads 28 / 4 x 128: 169, 203,
+// 155; 64 contexts of single tokens over up to 4k slots, heads 8 / 4 x 256: 69, 74, -.
 template <bool CAP>
 __device__ __forceinline__ float weigh(const AttnArgs& a, const f32x16& s, const float (&less)[16]) {
   float sum[2] = {0.f, 0.f};
@@ -86,9 +86,10 @@ __device__ __forceinline__ float weigh_seen(const AttnArgs& a, const Context& c,
 // Single tokens (and few): the query rows in registers, the slots streamed
 // through the waves' own rings.  Bound by memory: keys are read once, the line
 // of all work is cut into equal ranges as in forward's single tokens.  Measured:
-// 64 contexts of up to 4k slots, heads 28 / 4 x 128, 156 MB in 52 us, the kernel
-// 42 us (3.7 TB/s), of which about 10 pass before the first keys arrive: mass_in
-// past the tokens, lengths of 64 contexts, block numbers.
+// 64 contexts of up to 4k slots, heads 28 / 4 x 128, 156 MB in 53 us, the kernel
+// 43 us (3.6 TB/s), of which about 10 pass before the first keys arrive: mass_in
+// past the tokens, which the keys could be asked for ahead of, lengths of 64
+// contexts, block numbers.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP, bool CAP>
@@ -218,9 +219,9 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
 // their log-sum-exps are copied into LDS as many stages ahead of their use as
 // 128 KB hold: a stage is less work than a copy's latency.  No slot is
 // split over workgroups, so sums need no atomics and no second launch.  Bound by
-// the weights' arithmetic (an exponential a score, three with a cap) beside
-// the matrix units.  Measured: 1021 tokens in 8192 slots, heads 8 / 4 x 256,
-// capped: 56 us, 570 TFLOP/s.
+// the matrix units and the weights' arithmetic in turn, which a barrier a stage
+// keeps in step.  Measured: 1021 tokens in 8192 slots, heads 8 / 4 x 256,
+// capped: 60 us, 540 TFLOP/s.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP, bool CAP, int QW>
