@@ -149,3 +149,28 @@ def test_more_selections_than_a_launch_has():
     for s, t in zip((k, v), dst):
         assert T.equal(t[..., 0, :], T.where(want[..., None] == 1, s[..., 1, :], s[..., 0, :]))
     att.close()
+
+
+@pytest.mark.parametrize("over", [1, 500])
+def test_a_context_that_has_outgrown_its_cache(over):
+    """The cached slots are what is kept of, the last of them the recent ones."""
+    T = U.torch()
+    print(f"[evict] {over} tokens past the capacity", flush=True)
+    n, hkv, d, keep = 64, 2, 64, 20
+    cache = A.Cache([n], hkv, d, "bf16", 16)
+    w = np.random.default_rng(2).exponential(size=(2, 1, hkv, n)).astype(np.float32)
+    mass = T.from_numpy(w.copy()).cuda()
+    kept = T.full((2, 1, hkv, keep), -7, dtype=T.int32, device="cuda")
+    left = A._int([0])
+    att = kvx.Attention(kvx.ModelShape(2, hkv, d, 1e4), hkv, kvx.KVX_BF16)
+    att.evict(kvx.make_evict_io(cache.struct, A._int([n + over]), mass, kept, keep, sink=2, recent=5,
+                                mass_out=mass, tokens_out=left))
+    T.cuda.synchronize()
+    assert left.tolist() == [keep]
+    for l in range(2):
+        for h in range(hkv):
+            ref = R.keep(w[l, 0, h], keep, 2, 5)
+            assert (kept[l, 0, h].cpu().numpy() == ref).all()
+            for kv in range(2):
+                assert T.equal(cache.read(kv, l, 0, keep)[:, h], cache.rows[kv][l][0][ref, h])
+    att.close()
