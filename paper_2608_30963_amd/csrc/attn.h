@@ -77,7 +77,6 @@ struct AttnArgs {
   float scale2;            // score scale * log2(e)
   float cap2;              // cap * log2(e), 0: none
   float tanh2;             // 2 scale / cap * log2(e)
-  float near, near_c[4];   // cap_near's range and coefficients
   const char* q;           // forward, mass
   int64_t q_sr, q_sh;      // elements
   char* out;
@@ -86,6 +85,7 @@ struct AttnArgs {
   const float* mass_in;
   float* mass;
   int32_t mass_capacity;
+  float near, near_c[4];   // cap_near's range and coefficients
 };
 
 // A context's rows and slots, clamped to what the caller's buffers hold.  New

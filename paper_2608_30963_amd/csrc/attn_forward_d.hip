@@ -6,14 +6,6 @@
 namespace kvx {
 namespace {
 
-// Query rows [from, to) of those from r0 on that see anything: slots before them
-// are negative, windows after them start past the cache's last slot.
-__device__ __forceinline__ void seeing(const AttnArgs& a, const Context& c, int r0, int& from, int& to) {
-  from = max(0, -c.p0) * a.group - r0;  // slots times heads may pass 32 bits, rows do not
-  const int64_t last = a.window ? min<int64_t>(c.m, int64_t(c.n) + a.window - 1 - c.p0) : c.m;
-  to = static_cast<int>(max<int64_t>(last, 0)) * a.group - r0;
-}
-
 // out row of query (row, head) from O^T registers and its sum; lane (n, h) has
 // 4 columns of each 8.
 template <typename T, int NB>
@@ -64,13 +56,6 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const QueryRow& q, 
 // LDS has room.  The scores of tile t + 1 are formed beside the weights of tile t,
 // which need other units of the compute unit.
 // ---------------------------------------------------------------------------
-
-// How the tiles that all queries see form capped scores: bf16 ones, under caps up to
-// kPartCap, by cap_part, all others by cap_tanh.  Measured (us, a few calls in a
-// row; cap_part, cap_tanh), cap 50: 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256: 125,
-// 153; 1024 in 8192, heads 28 / 4 x 128: 202, 279; 64 contexts of single tokens over up
-// to 8k slots, heads 28 / 4 x 128: 124, 134.
-enum class Cap { none, part, tanh };
 
 template <typename T, int DP>
 constexpr int chunk_tile() { return DP * sizeof(T) <= 256 ? 64 : 32; }
@@ -304,7 +289,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
     // 32 slots at a time: the masks and checks want registers too
 #pragma unroll 1
     for (int u = 0; u < NS; ++u)
-      odd |= edge_step<T, DP, CAP != Cap::none>(a, k + u * 32 * L::kRowBytes, v + u * 32 * L::kRowBytes, at, q,
+      odd |= edge_step<T, DP, CAP>(a, k + u * 32 * L::kRowBytes, v + u * 32 * L::kRowBytes, at, q,
                                    t * TK + 32 * u, qr.lo, qr.hi, st, acc);
   };
   int t = t0;
@@ -323,7 +308,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
 #pragma unroll
       for (int u = 0; u < NS; ++u) s[u] = L::scores(k + u * 32 * L::kRowBytes, at, q);
       if constexpr (CAP != Cap::part) {
-        if constexpr (CAP == Cap::tanh) cap_scores<false>(a, s);
+        if constexpr (CAP == Cap::tanh) cap_scores<CAP>(a, s);
         top = top_score(c2, s);
       } else {
         f32x16 x[NS];
@@ -457,9 +442,8 @@ __device__ __forceinline__ int decode_steps(const AttnArgs& a, const Context& c,
   int lo, hi;
   const int r0 = qt * kDecodeRows;
   seen_by(a, c, r0, min(r0 + kDecodeRows, c.m * a.group) - 1, lo, hi);
-  if (lo >= hi) return 1;
   lo &= ~31;
-  return (hi - lo + STEP - 1) / STEP;
+  return max(1, (hi - lo + STEP - 1) / STEP);
 }
 
 template <typename T, int DP, Cap CAP>
@@ -563,7 +547,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
       const int j0 = slot_of(t);
       if (j0 >= alo && j0 + 32 <= ahi) {
         f32x16 sc[1] = {L::scores(k, at, q)};
-        if constexpr (CAP != Cap::none) cap_scores<CAP == Cap::part>(a, sc);
+        if constexpr (CAP != Cap::none) cap_scores<CAP>(a, sc);
         if constexpr (L::kBf16) {
           // the first pieces of the values come beside the softmax
           constexpr int kAhead = 2 * NB < 8 ? 2 * NB : 8;
@@ -585,7 +569,7 @@ __global__ void __launch_bounds__((64 * Decode<T, DP>::kWaves), 1)
           L::template add_values<false>(v, at, sc[0], acc);
         }
       } else {
-        odd |= edge_step<T, DP, CAP != Cap::none>(a, k, v, at, q, j0, qr.lo, qr.hi, st, acc);
+        odd |= edge_step<T, DP, CAP>(a, k, v, at, q, j0, qr.lo, qr.hi, st, acc);
       }
       __builtin_amdgcn_sched_barrier(0);
       fetch_blocks(a.c, b, slot_of(t + NST), hi, blocks);

@@ -142,11 +142,14 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
       const T* qp = reinterpret_cast<const T*>(a.q) + qr.row * a.q_sr + (h * a.group + qr.g) * a.q_sh;
       L::load_q(q, n < valid ? qp : nullptr, a.d);
       float less[16];
+      int first, last;
+      seeing(a, c, r0, first, last);
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const QueryRow u = query_row(a, c, r0 + 8 * (v / 4) + 4 * half + v % 4);
-        less[v] = u.lo < u.hi
-                      ? -kLog2e * a.lse[static_cast<int64_t>(u.row) * a.hq + h * a.group + u.g]
+        const int r = 8 * (v / 4) + 4 * half + v % 4, i = fdiv(a.by_group, r0 + r);
+        less[v] = r >= first && r < last
+                      ? -kLog2e * a.lse[static_cast<int64_t>(c.q0 + i) * a.hq + h * a.group +
+                                        (r0 + r - i * a.group)]
                       : -INFINITY;
       }
       // tiles that the rows see: from t0 to t1; the others keep their sums

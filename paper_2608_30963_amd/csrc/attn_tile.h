@@ -429,6 +429,14 @@ __device__ __forceinline__ void seen_by(const AttnArgs& a, const Context& c, int
   lo = min(first_seen(a, max(p0, 0)), hi);
 }
 
+// Query rows [from, to) of those from r0 on that see anything: slots before them
+// are negative, windows after them start past the cache's last slot.
+__device__ __forceinline__ void seeing(const AttnArgs& a, const Context& c, int r0, int& from, int& to) {
+  from = max(0, -c.p0) * a.group - r0;  // slots times heads may pass 32 bits, rows do not
+  const int64_t last = a.window ? min<int64_t>(c.m, int64_t(c.n) + a.window - 1 - c.p0) : c.m;
+  to = static_cast<int>(max<int64_t>(last, 0)) * a.group - r0;
+}
+
 // A workgroup's equal range of the line (KV head, context, step), where context
 // b has steps_of(b) steps.
 struct Share {
@@ -553,14 +561,21 @@ __device__ __forceinline__ void softmax_step(float c, f32x16 (&s)[NS], Softmax& 
   for (int t = 0; t < NS; ++t) weights(c, s[t], st);
 }
 
-// Capped scores, in log2 units; PART: by cap_part.
-template <bool PART, int NS>
+// How attention forms capped scores: bf16 ones, under caps up to kPartCap, by
+// cap_part, all others by cap_tanh.  Measured (us, a few calls in a row; cap_part,
+// cap_tanh), cap 50: 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256: 125,
+// 153; 1024 in 8192, heads 28 / 4 x 128: 202, 279; 64 contexts of single tokens over
+// up to 8k slots, heads 28 / 4 x 128: 124, 134.
+enum class Cap { none, part, tanh };
+
+// Capped scores, in log2 units.
+template <Cap CAP, int NS>
 __device__ __forceinline__ void cap_scores(const AttnArgs& a, f32x16 (&s)[NS]) {
 #pragma unroll
   for (int t = 0; t < NS; ++t)
 #pragma unroll
     for (int v = 0; v < 16; ++v)
-      s[t][v] = PART ? __builtin_fmaf(-2.f * a.cap2, cap_part(a, s[t][v]), a.cap2)
+      s[t][v] = CAP == Cap::part ? __builtin_fmaf(-2.f * a.cap2, cap_part(a, s[t][v]), a.cap2)
                      : a.cap2 * cap_tanh(a, s[t][v]);
 }
 
@@ -578,7 +593,7 @@ __device__ __forceinline__ void mask_scores(f32x16& s, int j0, int lo, int hi) {
 
 // A tile of 32 slots that not all of the wave's queries see.  Returns whether
 // it holds values that are not finite, which it leaves out.
-template <typename T, int DP, bool CAP>
+template <typename T, int DP, Cap CAP>
 __device__ __forceinline__ bool edge_step(const AttnArgs& a, const char* k, const char* v,
                                           const typename Tile<T, DP>::LaneAt& at,
                                           const uint4 (&q)[Tile<T, DP>::kQ], int j0, int lo, int hi,
@@ -586,9 +601,9 @@ __device__ __forceinline__ bool edge_step(const AttnArgs& a, const char* k, cons
   using L = Tile<T, DP>;
   const bool odd = L::any_odd(v);
   f32x16 s[1] = {L::scores(k, at, q)};
-  if constexpr (CAP) cap_scores<false>(a, s);
+  if constexpr (CAP != Cap::none) cap_scores<CAP>(a, s);
   mask_scores(s[0], j0, lo, hi);
-  softmax_step(CAP ? 1.f : a.scale2, s, st, acc);
+  softmax_step(CAP == Cap::none ? a.scale2 : 1.f, s, st, acc);
   if (odd)
     L::template add_values<true>(v, at, s[0], acc);
   else
