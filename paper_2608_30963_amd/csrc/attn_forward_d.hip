@@ -41,10 +41,10 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const QueryRow& q, 
 // sum.  Bound by the matrix units, and where heads are 256 wide by the LDS as
 // much: each of 4 waves reads all of a tile's keys and values for 32 rows, about
 // a thousand clocks, as its matrix work takes, and one wave a SIMD has to
-// overlap the two.  Measured: 4096 tokens after 12k, heads 64 / 8 x 128: 1.90 ms,
-// 1.01 PFLOP/s, where the card's power sets the clock (with zeros a fifth less
-// time); 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256, capped: 118 us,
-// 435 TFLOP/s; fp32, 3 contexts of up to 257 in 1024 slots, heads 12 / 2 x 128:
+// overlap the two.  Measured: 4096 tokens after 12k, heads 64 / 8 x 128: 1.88 ms,
+// 1.02 PFLOP/s, where the card's power sets the clock (with zeros a fifth less
+// time); 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256, capped: 116 us,
+// 445 TFLOP/s; fp32, 3 contexts of up to 257 in 1024 slots, heads 12 / 2 x 128:
 // 56 us, 46 TFLOP/s of 154: a tile's scores, weights and products follow each
 // other, its 232 workgroups do not divide the work evenly, and start and join
 // take a quarter.
@@ -424,8 +424,8 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1)
 // numbers, two rounds of rows (two stages of copies are asked for one after the
 // other) and two barriers.  Wider heads have fewer waves and stages, and registers
 // that are read back from scratch memory once or twice a tile: heads 8 / 4, 64
-// contexts of up to 8k slots: 256 columns 1208 MB in 353 us, 3.4 TB/s, 192 columns
-// 906 MB in 392; fp32, 16 of up to 4k, 256 columns: 309 MB in 252.
+// contexts of up to 8k slots: 256 columns 1208 MB in 357 us, 3.4 TB/s, 192 columns
+// 906 MB in 381; fp32, 16 of up to 4k, 256 columns: 309 MB in 252.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP>

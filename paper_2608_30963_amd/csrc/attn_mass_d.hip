@@ -86,8 +86,8 @@ __device__ __forceinline__ float weigh_seen(const AttnArgs& a, const Context& c,
 // Single tokens (and few): the query rows in registers, the slots streamed
 // through the waves' own rings.  Bound by memory: keys are read once, the line
 // of all work is cut into equal ranges as in forward's single tokens.  Measured:
-// 64 contexts of up to 4k slots, heads 28 / 4 x 128, 156 MB in 53 us, the kernel
-// 43 us (3.6 TB/s), of which about 10 pass before the first keys arrive: mass_in
+// 64 contexts of up to 4k slots, heads 28 / 4 x 128, 156 MB in 52 us, the kernel
+// 42 us (3.7 TB/s), of which about 10 pass before the first keys arrive: mass_in
 // past the tokens, which the keys could be asked for ahead of, lengths of 64
 // contexts, block numbers.
 // ---------------------------------------------------------------------------
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__((64 * ring_waves(32 * DP * sizeof(T))), 1) mas
 // split over workgroups, so sums need no atomics and no second launch.  Bound by
 // the matrix units and the weights' arithmetic in turn, which a barrier a stage
 // keeps in step.  Measured: 1021 tokens in 8192 slots, heads 8 / 4 x 256,
-// capped: 60 us, 540 TFLOP/s.
+// capped: 59 us, 545 TFLOP/s.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP, bool CAP, int QW>
