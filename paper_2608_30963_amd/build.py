@@ -46,7 +46,7 @@ def _check(r, what):
 def build(out: str = LIB, verbose: bool = False) -> str:
     """Compile the host library, the translator fit, the translator-variant
     composition, the staged (unfused) translation, decoding on the translated
-    cache and the fused kernel's three precision variants as separate objects (in parallel), then link
+    cache (also in 8 bits and by drafted trees) and the fused kernel's three precision variants as separate objects (in parallel), then link
     libkvx.so."""
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
@@ -55,7 +55,8 @@ def build(out: str = LIB, verbose: bool = False) -> str:
              ("compose", os.path.join(CSRC, "compose.hip"), []),
              ("staged", os.path.join(CSRC, "staged.hip"), [])]
     units += [(name, os.path.join(CSRC, name + ".hip"), [])
-              for name in ("attn", "attn_forward", "attn_mass", "attn_evict")]
+              for name in ("attn", "attn_forward", "attn_mass", "attn_evict", "attn_serve",
+                           "attn_cache8", "attn_tree", "attn_view")]
     units += [(f"{name}_{dp}", os.path.join(CSRC, name + "_d.hip"), [f"-DKVX_ATTN_DP={dp}"])
               for name in ("attn_forward", "attn_mass") for dp in (64, 128, 256)]
     for i, name in enumerate(("bf16x2", "bf16", "f16")):

@@ -110,6 +110,20 @@ __device__ __forceinline__ Context context(const AttnArgs& a, int b) {
   return c;
 }
 
+// The context of a row: the last whose first row is not after it.
+__device__ __forceinline__ int context_of(const AttnArgs& a, int row) {
+  if (!a.q_start) return row;
+  int lo = 0, hi = a.batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (a.q_start[mid] <= row)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
 // Slots [lo, hi) that the new token of slot p sees; empty for p < 0, and where
 // a window starts past the cache's last slot.
 __device__ __forceinline__ int first_seen(const AttnArgs& a, int p) {

@@ -1,0 +1,192 @@
+// attn_view.h -- what a row sees under a view (kvx_serve.h), and caches of 8
+// bits: codes, their scales and their numbers.
+#pragma once
+
+#include "attn.h"
+#include "kvx_serve.h"
+
+namespace kvx {
+
+// Numbers of 8 bits, as the types of a cache.
+struct code_i8 {
+  uint8_t x;
+};
+struct code_e4m3 {
+  uint8_t x;
+};
+
+// Where scales lie: those of slot j of context b and head h are pair block * sb
+// + h * sh + (j % block_size) * st, the block and block_size the codes'.
+struct ScaleArgs {
+  uint32_t* p;  // low half: the key's bf16, high half: the value's
+  int64_t sl, sb, sh, st;
+};
+
+// One layer's forward under a view.
+struct AttnView : AttnArgs {
+  int32_t sink;
+  const uint32_t* tree;  // NULL: none
+  int32_t words;
+  const int32_t* depth;  // NULL: rows in order
+  ScaleArgs scale;       // caches of 8 bits
+};
+
+// The slots that one row sees: [lo, hi), [0, sink) below hi, and the set bits of
+// mask, bit k standing for slot p0 + k, below end.
+struct Sight {
+  int lo, hi, sink;
+  int p0, end, words;
+  const uint32_t* mask;  // NULL: none
+};
+
+__device__ __forceinline__ Sight sight(const AttnView& a, const Context& c, int i) {
+  Sight s;
+  const int p = c.p0 + i;  // slot
+  s.p0 = c.p0;
+  s.end = c.n;
+  s.words = a.words;
+  s.mask = nullptr;
+  if (a.tree) {
+    const int64_t row = static_cast<int64_t>(c.q0) + i;
+    const int d = a.depth ? min(max(a.depth[row], 0), max(c.m - 1, 0)) : i;
+    s.lo = first_seen(a, c.p0 + d);
+    s.hi = p < 0 ? 0 : min(max(c.p0, 0), c.n);
+    if (p >= 0) s.mask = a.tree + row * a.words;
+  } else {
+    s.lo = first_seen(a, p);
+    s.hi = end_seen(c, p);
+  }
+  s.lo = min(s.lo, s.hi);
+  s.sink = min(a.sink, s.hi);
+  return s;
+}
+
+__device__ __forceinline__ uint32_t low_bits(int n) {
+  return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+}
+
+// Which of the slots j0 .. j0 + 31 the row sees, slot j0 + i in bit i.
+__device__ __forceinline__ uint32_t seen_bits(const Sight& s, int j0) {
+  uint32_t bits = low_bits(s.hi - j0) & (~low_bits(s.lo - j0) | low_bits(s.sink - j0));
+  if (s.mask && j0 + 32 > s.p0 && j0 < s.end) {
+    const int o = j0 - s.p0, w = o >> 5;
+    const uint64_t lo = w >= 0 && w < s.words ? s.mask[w] : 0u;
+    const uint64_t hi = w + 1 >= 0 && w + 1 < s.words ? s.mask[w + 1] : 0u;
+    bits |= static_cast<uint32_t>((hi << 32 | lo) >> (o & 31)) & low_bits(s.end - j0);
+  }
+  return bits;
+}
+
+// Whether the row sees anything.
+__device__ __forceinline__ bool sees_any(const Sight& s) {
+  if (s.lo < s.hi || s.sink > 0) return true;
+  if (!s.mask) return false;
+  uint32_t any = 0;
+  const int first = max(0, -s.p0);  // nodes of negative slots are not there
+  for (int w = 0; w < s.words; ++w)
+    any |= s.mask[w] & ~low_bits(first - 32 * w) & low_bits(s.end - s.p0 - 32 * w);
+  return any != 0;
+}
+
+// ---------------------------------------------------------------------------
+// Codes
+// ---------------------------------------------------------------------------
+
+// A row's scale 2^e by its largest magnitude, taken from that number's bits:
+// top = f 2^k, f in [1/2, 1), and the largest code is M = g 2^r, g of f's range,
+// so that top <= M 2^e from e = k - r on, or one more where f > g.
+template <typename C>
+__device__ __forceinline__ int scale_exponent(float top) {
+  constexpr bool kI8 = std::is_same<C, code_i8>::value;
+  const uint32_t b = __float_as_uint(top);
+  const uint32_t past = (b & 0x7fffffu) > (kI8 ? 0x7e0000u : 0x600000u) ? 1 : 0;
+  return max(static_cast<int>((b >> 23) + past) - 126 - (kI8 ? 7 : 9), -100);
+}
+
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+
+// Codes of four numbers that are already divided by their scale.
+template <typename C>
+__device__ __forceinline__ uint32_t encode4(const float (&x)[4]) {
+  if constexpr (std::is_same<C, code_i8>::value) {
+    uint32_t u = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u |= (static_cast<uint32_t>(static_cast<int>(rintf(x[i]))) & 255u) << 8 * i;
+    return u;
+  } else {
+    int u = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], u, true));
+  }
+}
+
+// The numbers of four codes, times a scale.
+template <typename C>
+__device__ __forceinline__ void decode4(uint32_t u, float scale, float (&x)[4]) {
+  if constexpr (std::is_same<C, code_i8>::value) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = static_cast<float>(static_cast<signed char>(u >> 8 * i)) * scale;
+  } else {
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+    x[0] = a[0] * scale;
+    x[1] = a[1] * scale;
+    x[2] = b[0] * scale;
+    x[3] = b[1] * scale;
+  }
+}
+
+// One number of a row.
+template <typename S>
+__device__ __forceinline__ float number(const S* p, float scale) {
+  if constexpr (sizeof(S) == 1) {
+    float x[4];
+    decode4<S>(p->x, scale, x);
+    return x[0];
+  } else {
+    return load_f32<S>(p);
+  }
+}
+
+__device__ __forceinline__ float key_scale(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float value_scale(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
+
+struct PackArgs {
+  CacheArgs plain, coded;  // all layers
+  ScaleArgs scale;
+  const int32_t* tokens;
+  int32_t layers, batch, heads, d;
+};
+
+struct TreeArgs {
+  int32_t batch, rows, axes;
+  const int32_t* q_start;
+  const int32_t* tokens;
+  const int32_t* parent;
+  int32_t window, sink;
+  const int32_t* shift;
+  int32_t words;
+  uint32_t* mask;
+  int32_t* depth;
+  int32_t* pos;
+};
+
+struct AcceptArgs {
+  CacheArgs c;  // all layers
+  ScaleArgs scale;  // p NULL: none
+  const int32_t* q_start;
+  const int32_t* tokens;
+  const int32_t* path;
+  int32_t max_path;
+  const int32_t* count;
+  int32_t* tokens_out;
+  int32_t layers, batch, heads, row_bytes, es;
+};
+
+// Launchers; each returns the launch's own status.
+hipError_t launch_pack(const kvx_attn* at, const PackArgs& a, int code, bool pack, hipStream_t st);
+hipError_t launch_tree(const TreeArgs& a, hipStream_t st);
+hipError_t launch_accept(const kvx_attn* at, const AcceptArgs& a, hipStream_t st);
+// code: kvx_code of the cache, -1: the model's dtype
+hipError_t launch_view(const kvx_attn* at, const AttnView& a, int code, int max_new, void* workspace,
+                       hipStream_t st);
+
+}  // namespace kvx

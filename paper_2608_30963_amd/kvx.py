@@ -6,7 +6,9 @@ The entry points carry the C names -- ``kvx_plan_create``,
 ``kvx_fit_accumulate``, ``kvx_fit_solve``, ``kvx_fit_reset``,
 ``kvx_fit_destroy`` (include/kvx_fit.h), ``kvx_attn_create``,
 ``kvx_attn_append``, ``kvx_attn_forward``, ``kvx_attn_mass``,
-``kvx_attn_evict``, ``kvx_attn_destroy`` (include/kvx_attn.h) -- and take torch
+``kvx_attn_evict``, ``kvx_attn_destroy`` (include/kvx_attn.h),
+``kvx_attn_append_coded``, ``kvx_attn_pack``, ``kvx_attn_unpack``, ``kvx_attn_tree``,
+``kvx_attn_forward_view``, ``kvx_attn_accept`` (include/kvx_serve.h) -- and take torch
 tensors for device buffers (torch provides device memory and streams; it
 computes nothing here).  Every step of the translation, of the fit and of
 decoding on the translated cache runs in the library's HIP kernels.
@@ -28,9 +30,10 @@ KVX_OK, KVX_EINVAL, KVX_ESHAPE, KVX_EUNSUPPORTED, KVX_ENOMEM, KVX_EHIP, KVX_EDAT
 KVX_F32, KVX_BF16 = 0, 1
 KVX_PREC_BF16X2, KVX_PREC_BF16, KVX_PREC_F16, KVX_PREC_BF16X2_OUTLIER = 0, 1, 2, 3
 KVX_FACTORS_LOWRANK, KVX_FACTORS_MIXTURE = 1, 2
+KVX_CODE_I8, KVX_CODE_E4M3 = 0, 1
 KVX_STAGE_POOL, KVX_STAGE_PROJECT, KVX_STAGE_STORE, KVX_STAGE_ALL = 1, 2, 4, 7
 
-# Exported C symbols, as declared in include/kvx.h, kvx_fit.h and kvx_attn.h.
+# Exported C symbols, as declared in include/kvx.h, kvx_fit.h, kvx_attn.h and kvx_serve.h.
 SYMBOLS = ("kvx_plan_create", "kvx_plan_create_factored", "kvx_translate", "kvx_plan_destroy",
            "kvx_status_string",
            "kvx_last_hip_error", "kvx_plan_query", "kvx_staged_workspace_bytes",
@@ -38,7 +41,8 @@ SYMBOLS = ("kvx_plan_create", "kvx_plan_create_factored", "kvx_translate", "kvx_
            "kvx_fit_solve", "kvx_fit_solve_noalloc", "kvx_fit_reset", "kvx_fit_rows",
            "kvx_fit_query", "kvx_fit_destroy", "kvx_attn_create", "kvx_attn_destroy",
            "kvx_attn_append", "kvx_attn_workspace_bytes", "kvx_attn_forward", "kvx_attn_mass",
-           "kvx_attn_evict")
+           "kvx_attn_evict", "kvx_attn_append_coded", "kvx_attn_pack", "kvx_attn_unpack",
+           "kvx_attn_tree", "kvx_attn_forward_view", "kvx_attn_accept")
 
 
 class KvxError(RuntimeError):
@@ -117,6 +121,7 @@ class Cache(C.Structure):
 
 
 class AttnIO(C.Structure):
+    view = None  # an AttnView, of calls that have one
     _fields_ = [("batch", C.c_int32), ("layer", C.c_int32), ("rows", C.c_int32),
                 ("max_new", C.c_int32), ("q_start", C.c_void_p), ("tokens", C.c_void_p),
                 ("cache", Cache), ("new_q", C.c_void_p), ("new_k", C.c_void_p),
@@ -133,6 +138,34 @@ class EvictIO(C.Structure):
                 ("sink", C.c_int32), ("recent", C.c_int32), ("src", Cache), ("dst", Cache),
                 ("mass", C.c_void_p), ("mass_out", C.c_void_p), ("mass_capacity", C.c_int32),
                 ("kept", C.c_void_p), ("tokens_out", C.c_void_p)]
+
+
+class Cache8(C.Structure):
+    _fields_ = [("codes", Cache), ("scale", C.c_void_p), ("scale_stride", C.c_int64 * 4),
+                ("code", C.c_int32)]
+
+
+class AttnView(C.Structure):
+    _fields_ = [("cache8", C.c_void_p), ("sink", C.c_int32), ("tree", C.c_void_p),
+                ("tree_words", C.c_int32), ("depth", C.c_void_p)]
+
+
+class PackIO(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("tokens", C.c_void_p), ("cache", Cache),
+                ("cache8", C.c_void_p)]
+
+
+class TreeIO(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("rows", C.c_int32), ("q_start", C.c_void_p),
+                ("tokens", C.c_void_p), ("parent", C.c_void_p), ("window", C.c_int32),
+                ("sink", C.c_int32), ("shift", C.c_void_p), ("words", C.c_int32),
+                ("mask", C.c_void_p), ("depth", C.c_void_p), ("pos", C.c_void_p)]
+
+
+class AcceptIO(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("q_start", C.c_void_p), ("tokens", C.c_void_p),
+                ("path", C.c_void_p), ("max_path", C.c_int32), ("count", C.c_void_p),
+                ("cache", Cache), ("cache8", C.c_void_p), ("tokens_out", C.c_void_p)]
 
 
 _lib = None
@@ -203,6 +236,20 @@ def load(path: str = LIB_PATH):
     lib.kvx_attn_mass.restype = C.c_int
     lib.kvx_attn_evict.argtypes = [C.c_void_p, C.POINTER(EvictIO), C.c_void_p]
     lib.kvx_attn_evict.restype = C.c_int
+    lib.kvx_attn_append_coded.argtypes = [C.c_void_p, C.POINTER(AttnIO), C.POINTER(Cache8),
+                                          C.c_void_p]
+    lib.kvx_attn_append_coded.restype = C.c_int
+    lib.kvx_attn_pack.argtypes = [C.c_void_p, C.POINTER(PackIO), C.c_void_p]
+    lib.kvx_attn_pack.restype = C.c_int
+    lib.kvx_attn_unpack.argtypes = lib.kvx_attn_pack.argtypes
+    lib.kvx_attn_unpack.restype = C.c_int
+    lib.kvx_attn_tree.argtypes = [C.c_void_p, C.POINTER(TreeIO), C.c_void_p]
+    lib.kvx_attn_tree.restype = C.c_int
+    lib.kvx_attn_forward_view.argtypes = [C.c_void_p, C.POINTER(AttnIO), C.POINTER(AttnView),
+                                          C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.kvx_attn_forward_view.restype = C.c_int
+    lib.kvx_attn_accept.argtypes = [C.c_void_p, C.POINTER(AcceptIO), C.c_void_p]
+    lib.kvx_attn_accept.restype = C.c_int
     _lib = lib
     return lib
 
@@ -695,16 +742,46 @@ def _row_stride(t):
     return (C.c_int64 * 2)(t.stride(0), t.stride(1))
 
 
-def make_attn_io(cache: Cache, tokens, q=None, *, layer: int = 0, q_start=None, max_new: int = 1,
+def make_cache8(k, v, scale, block_table=None, stride=(0, 0, 0, 0), scale_stride=(0, 0, 0, 0),
+                block_size: Optional[int] = None, num_blocks: Optional[int] = None,
+                capacity: Optional[int] = None, code: Optional[int] = None) -> Cache8:
+    """The kvx_cache8 struct of device tensors: codes ``k``/``v`` as make_cache takes
+    them, of torch.int8 or torch.float8_e4m3fn (others: give ``code``), and
+    ``scale``, bfloat16 of the codes' shape with 2 (key, value) in head_dim's place."""
+    if k.element_size() != 1:
+        raise ValueError(f"codes have one byte, k is {k.dtype}")
+    if code is None:
+        code = {"torch.int8": KVX_CODE_I8, "torch.float8_e4m3fn": KVX_CODE_E4M3}.get(str(k.dtype))
+        if code is None or k.dtype != v.dtype:
+            raise ValueError(f"codes are int8 or float8_e4m3fn, k is {k.dtype}, v is {v.dtype}")
+    codes = make_cache(k, v, block_table, stride, block_size, num_blocks, capacity)
+    _one_device((k, scale))
+    if str(scale.dtype) != "torch.bfloat16":
+        raise ValueError(f"scale is {scale.dtype}, expected torch.bfloat16")
+    if not any(scale_stride):
+        _plain("scale", scale, "bfloat16", last=2)
+        if scale.shape[:-1] != k.shape[:-1]:
+            raise ValueError(f"scale has shape {tuple(scale.shape)}, the codes {tuple(k.shape)}")
+    c = Cache8(codes, _ptr(scale), (C.c_int64 * 4)(*[int(x) for x in scale_stride]), int(code))
+    c.tensors, c.scales = codes.tensors, scale
+    return c
+
+
+def make_attn_io(cache, tokens, q=None, *, layer: int = 0, q_start=None, max_new: int = 1,
                  new_q=None, new_k=None, new_v=None, pos=None, window: int = 0, prefix=None,
-                 out=None, lse=None, mass_in=None, mass=None) -> AttnIO:
+                 out=None, lse=None, mass_in=None, mass=None, sink: int = 0, tree=None,
+                 depth=None) -> AttnIO:
     """Build the kvx_attn_io struct of one layer's append, forward and mass
     calls: ``q``, ``new_q``, ``new_k``, ``new_v``, ``out`` are [rows][heads][D]
     tensors (any row and head strides); ``mass`` [B][Hkv][mass_capacity].  The
-    struct keeps its tensors alive."""
+    struct keeps its tensors alive.  A cache of make_cache8, ``sink`` and a
+    ``tree`` (masks [rows][words] and ``depth`` as make_tree_io's) make it a call
+    under a view (kvx_attn_view), which has append and forward."""
     first = next(t for t in (q, new_q, new_k) if t is not None)
     batch, rows = int(tokens.shape[0]), int(first.shape[0])
+    coded = cache if isinstance(cache, Cache8) else None
     k = getattr(cache, "tensors", (None,))[0]
+    width = 2 if coded is not None else (k if hasattr(k, "element_size") else first).element_size()
     for name, t in (("q", q), ("new_q", new_q), ("new_k", new_k), ("new_v", new_v), ("out", out)):
         if t is None:
             continue
@@ -712,7 +789,7 @@ def make_attn_io(cache: Cache, tokens, q=None, *, layer: int = 0, q_start=None, 
         if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != first.shape[2] or \
                 (like is not None and t.shape != like.shape):
             raise ValueError(f"{name} has shape {tuple(t.shape)}")
-        if t.element_size() != (k if hasattr(k, "element_size") else first).element_size():
+        if t.element_size() != width:
             raise ValueError(f"{name} is {t.dtype}, the cache is not")
     _plain("tokens", tokens, "int32")
     _plain("q_start", q_start, "int32", batch + 1)
@@ -721,14 +798,77 @@ def make_attn_io(cache: Cache, tokens, q=None, *, layer: int = 0, q_start=None, 
     _plain("lse", lse, "float32", None if q is None else rows * int(q.shape[1]))
     _plain("mass", mass, "float32")
     _plain("mass_in", mass_in, "float32", None if mass is None else mass.numel())
-    _one_device((k, tokens, q, q_start, new_q, new_k, new_v, pos, prefix, out, lse, mass_in, mass))
+    _plain("tree", tree, "int32", rows)
+    _plain("depth", depth, "int32", rows)
+    if tree is not None and (tree.dim() != 2 or int(tree.shape[0]) < rows):
+        raise ValueError(f"tree has shape {tuple(tree.shape)}, expected {rows} rows of masks")
+    _one_device((k, tokens, q, q_start, new_q, new_k, new_v, pos, prefix, out, lse, mass_in, mass,
+                 tree, depth))
     io = AttnIO(batch, int(layer), rows, int(max_new),
-                _ptr(q_start), _ptr(tokens), cache, _ptr(new_q), _ptr(new_k), _ptr(new_v),
+                _ptr(q_start), _ptr(tokens), Cache() if coded is not None else cache, _ptr(new_q),
+                _ptr(new_k), _ptr(new_v),
                 _row_stride(new_q), _row_stride(new_k), _row_stride(new_v), _ptr(pos), _ptr(q),
                 _row_stride(q), int(window), _ptr(prefix), _ptr(out), _row_stride(out), _ptr(lse),
                 _ptr(mass_in), _ptr(mass), 0 if mass is None else int(mass.shape[-1]))
     io.tensors = (cache, tokens, q, q_start, new_q, new_k, new_v, pos, prefix, out, lse, mass_in,
                mass)
+    if coded is not None or sink or tree is not None:
+        io.view = AttnView(None if coded is None else C.addressof(coded), int(sink), _ptr(tree),
+                           0 if tree is None else int(tree.shape[1]), _ptr(depth))
+        io.view.tensors = (coded, tree, depth)
+    return io
+
+
+def make_pack_io(cache: Cache, cache8: Cache8, tokens) -> PackIO:
+    """Build the kvx_pack_io struct: a cache of the model's dtype and one of 8 bits, of
+    which pack and unpack convert the first ``tokens`` slots of every context."""
+    _plain("tokens", tokens, "int32")
+    k, k8 = (getattr(c, "tensors", (None,))[0] for c in (cache, cache8))
+    _one_device((k, k8, tokens))
+    io = PackIO(int(tokens.shape[0]), _ptr(tokens), cache, C.addressof(cache8))
+    io.tensors = (cache, cache8, tokens)
+    return io
+
+
+def make_tree_io(tokens, parent, mask, *, depth=None, pos=None, q_start=None, window: int = 0,
+                 sink: int = 0, shift=None) -> TreeIO:
+    """Build the kvx_tree_io struct: ``parent`` [rows] of the drafted nodes, ``mask``
+    [rows][words] int32, ``depth`` [rows] and ``pos`` [axes][rows] are written."""
+    batch, rows = int(tokens.shape[0]), int(parent.shape[0])
+    _plain("tokens", tokens, "int32")
+    _plain("parent", parent, "int32")
+    _plain("mask", mask, "int32", rows)
+    if mask.dim() != 2 or int(mask.shape[0]) < rows:
+        raise ValueError(f"mask has shape {tuple(mask.shape)}, expected {rows} rows")
+    _plain("depth", depth, "int32", rows)
+    _plain("pos", pos, "int32", last=rows)
+    _plain("q_start", q_start, "int32", batch + 1)
+    _plain("shift", shift, "int32", batch)
+    _one_device((tokens, parent, mask, depth, pos, q_start, shift))
+    io = TreeIO(batch, rows, _ptr(q_start), _ptr(tokens), _ptr(parent), int(window), int(sink),
+                _ptr(shift), int(mask.shape[1]), _ptr(mask), _ptr(depth), _ptr(pos))
+    io.tensors = (tokens, parent, mask, depth, pos, q_start, shift)
+    return io
+
+
+def make_accept_io(cache, tokens, path, count, *, q_start=None, tokens_out=None) -> AcceptIO:
+    """Build the kvx_accept_io struct: ``path`` [B][max_path] and ``count`` [B] of the
+    accepted nodes, a cache of make_cache or make_cache8."""
+    batch = int(tokens.shape[0])
+    coded = cache if isinstance(cache, Cache8) else None
+    _plain("tokens", tokens, "int32")
+    _plain("path", path, "int32")
+    if path.dim() != 2 or int(path.shape[0]) < batch:
+        raise ValueError(f"path has shape {tuple(path.shape)}, expected {batch} rows")
+    _plain("count", count, "int32", batch)
+    _plain("q_start", q_start, "int32", batch + 1)
+    _plain("tokens_out", tokens_out, "int32", batch)
+    k = getattr(cache, "tensors", (None,))[0]
+    _one_device((k, tokens, path, count, q_start, tokens_out))
+    io = AcceptIO(batch, _ptr(q_start), _ptr(tokens), _ptr(path), int(path.shape[1]), _ptr(count),
+                  Cache() if coded is not None else cache,
+                  None if coded is None else C.addressof(coded), _ptr(tokens_out))
+    io.tensors = (cache, tokens, path, count, q_start, tokens_out)
     return io
 
 
@@ -795,14 +935,63 @@ def kvx_attn_evict(attn: int, io: EvictIO, stream=None) -> int:
     return st
 
 
+def kvx_attn_append_coded(attn: int, io: AttnIO, cache8: Cache8, stream=None) -> int:
+    st = load().kvx_attn_append_coded(attn, C.byref(io), C.byref(cache8), _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_append_coded")
+    return st
+
+
+def kvx_attn_pack(attn: int, io: PackIO, stream=None) -> int:
+    st = load().kvx_attn_pack(attn, C.byref(io), _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_pack")
+    return st
+
+
+def kvx_attn_unpack(attn: int, io: PackIO, stream=None) -> int:
+    st = load().kvx_attn_unpack(attn, C.byref(io), _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_unpack")
+    return st
+
+
+def kvx_attn_tree(attn: int, io: TreeIO, stream=None) -> int:
+    st = load().kvx_attn_tree(attn, C.byref(io), _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_tree")
+    return st
+
+
+def kvx_attn_forward_view(attn: int, io: AttnIO, view: Optional[AttnView], workspace,
+                          stream=None) -> int:
+    """``workspace``: a device tensor of at least kvx_attn_workspace_bytes."""
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("the workspace must be a contiguous tensor on a GPU")
+    st = load().kvx_attn_forward_view(attn, C.byref(io), None if view is None else C.byref(view),
+                                      workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(),
+                                      _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_forward_view")
+    return st
+
+
+def kvx_attn_accept(attn: int, io: AcceptIO, stream=None) -> int:
+    st = load().kvx_attn_accept(attn, C.byref(io), _stream_handle(stream))
+    if st != KVX_OK:
+        raise KvxError(st, "kvx_attn_accept")
+    return st
+
+
 def kvx_attn_destroy(attn: Optional[int]) -> None:
     load().kvx_attn_destroy(C.c_void_p(attn) if attn else None)
 
 
 class Attention:
     """RAII wrapper around the attention side of a target model.  The calls
-    take structs of make_attn_io / make_evict_io, which a decoding loop builds
-    once per layer."""
+    take structs of make_attn_io / make_evict_io / make_pack_io / make_tree_io /
+    make_accept_io, which a decoding loop builds once (per layer)."""
 
     def __init__(self, model, n_heads, dtype, softcap=0.0, scale=0.0, inv_freq=None,
                  pair_axis=None, n_axes=None):
@@ -827,25 +1016,38 @@ class Attention:
         if tensors is None:
             return  # built by hand, which the caller answers for
         heads, d, width = int(m.n_kv_heads), int(m.head_dim), 4 if self.dtype == KVX_F32 else 2
-        caches = [c for c in (tensors[0], tensors[-1]) if isinstance(c, Cache)]
+        caches = [c for c in (tensors[0], tensors[1], tensors[-1]) if isinstance(c, (Cache, Cache8))]
         given = [t for t in tensors if hasattr(t, "data_ptr")]
+        if getattr(io, "view", None) is not None:
+            given += [t for t in io.view.tensors if hasattr(t, "data_ptr")]
         for c in caches:
             k = getattr(c, "tensors", (None,))[0]
             if not hasattr(k, "data_ptr"):
                 continue
             given.append(k)
-            if k.element_size() != width:
+            if isinstance(c, Cache8):
+                given.append(c.scales)
+                c = c.codes
+            elif k.element_size() != width:
                 raise ValueError(f"the cache is {k.dtype}, the model's numbers have {width} bytes")
             if not any(c.stride) and (k.dim() != 5 or (k.shape[2], k.shape[4]) != (heads, d)):
                 raise ValueError(f"the cache has shape {tuple(k.shape)}, the model {heads} KV "
                                  f"heads of {d}")
+            if isinstance(io, (PackIO, AcceptIO)) and not any(c.stride) and \
+                    (int(k.shape[0]) < int(m.n_layers) or
+                     (c.block_table is None and int(k.shape[1]) < io.batch)):
+                raise ValueError(f"the cache has shape {tuple(k.shape)}, the model {m.n_layers} "
+                                 f"layers, the call {io.batch} contexts")
         if not all(t.is_cuda for t in given):
             raise ValueError("tensors must be on a GPU")
         if isinstance(io, EvictIO):
             sets = int(m.n_layers) * io.batch * heads
             if tensors[2].numel() < sets * int(tensors[2].shape[-1]):
                 raise ValueError(f"mass has shape {tuple(tensors[2].shape)}")
-        else:
+        elif isinstance(io, TreeIO):
+            if hasattr(tensors[4], "numel") and tensors[4].numel() < self.n_axes * io.rows:
+                raise ValueError(f"pos has shape {tuple(tensors[4].shape)}, expected {self.n_axes} axes")
+        elif isinstance(io, AttnIO):
             _, _, q, _, new_q, new_k, new_v, pos, _, out, _, _, mass = tensors
             for name, t, n in (("q", q, self.n_heads), ("new_q", new_q, self.n_heads),
                                ("new_k", new_k, heads), ("new_v", new_v, heads),
@@ -861,22 +1063,51 @@ class Attention:
     def append(self, io, stream=None):
         if getattr(io, "fits", None) is not self:
             self._fits(io)
-        kvx_attn_append(self.handle, io, stream)
+        coded = io.view.tensors[0] if io.view is not None else None
+        if coded is not None:
+            kvx_attn_append_coded(self.handle, io, coded, stream)
+        else:
+            kvx_attn_append(self.handle, io, stream)
 
     def forward(self, io, workspace, stream=None):
         if getattr(io, "fits", None) is not self:
             self._fits(io)
-        kvx_attn_forward(self.handle, io, workspace, stream)
+        if io.view is not None:
+            kvx_attn_forward_view(self.handle, io, io.view, workspace, stream)
+        else:
+            kvx_attn_forward(self.handle, io, workspace, stream)
 
     def mass(self, io, stream=None):
         if getattr(io, "fits", None) is not self:
             self._fits(io)
+        if io.view is not None:
+            raise ValueError("weights are not formed under a view: 8 bits, sinks or a tree")
         kvx_attn_mass(self.handle, io, stream)
 
     def evict(self, io, stream=None):
         if getattr(io, "fits", None) is not self:
             self._fits(io)
         kvx_attn_evict(self.handle, io, stream)
+
+    def pack(self, io, stream=None):
+        if getattr(io, "fits", None) is not self:
+            self._fits(io)
+        kvx_attn_pack(self.handle, io, stream)
+
+    def unpack(self, io, stream=None):
+        if getattr(io, "fits", None) is not self:
+            self._fits(io)
+        kvx_attn_unpack(self.handle, io, stream)
+
+    def tree(self, io, stream=None):
+        if getattr(io, "fits", None) is not self:
+            self._fits(io)
+        kvx_attn_tree(self.handle, io, stream)
+
+    def accept(self, io, stream=None):
+        if getattr(io, "fits", None) is not self:
+            self._fits(io)
+        kvx_attn_accept(self.handle, io, stream)
 
     def close(self):
         if self.handle:
