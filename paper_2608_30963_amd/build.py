@@ -56,9 +56,12 @@ def build(out: str = LIB, verbose: bool = False) -> str:
              ("staged", os.path.join(CSRC, "staged.hip"), [])]
     units += [(name, os.path.join(CSRC, name + ".hip"), [])
               for name in ("attn", "attn_forward", "attn_mass", "attn_evict", "attn_serve",
-                           "attn_cache8", "attn_tree", "attn_view")]
+                           "attn_cache8", "attn_tree")]
     units += [(f"{name}_{dp}", os.path.join(CSRC, name + "_d.hip"), [f"-DKVX_ATTN_DP={dp}"])
               for name in ("attn_forward", "attn_mass") for dp in (64, 128, 256)]
+    units += [(f"attn_view_{dp}_{coded}", os.path.join(CSRC, "attn_view_d.hip"),
+               [f"-DKVX_ATTN_DP={dp}", f"-DKVX_ATTN_CODED={coded}"])
+              for dp in (64, 128, 256) for coded in (0, 1)]
     for i, name in enumerate(("bf16x2", "bf16", "f16")):
         units.append((f"fused_{name}", os.path.join(CSRC, "fused_launch.hip"),
                       [f"-DKVX_LAUNCH_PREC={i}"]))

@@ -1,8 +1,9 @@
 // attn_forward.h -- the attention kernels' launchers, one translation unit per
-// head_dim (attn_forward_d.hip), and the partial results that they share.
+// head_dim (attn_forward_d.hip, attn_view_d.hip), and the partial results that
+// they share.
 #pragma once
 
-#include "attn.h"
+#include "attn_view.h"
 
 namespace kvx {
 
@@ -21,6 +22,7 @@ struct JoinHead {
   int32_t h;       // KV head
   int32_t first;   // index of the unit's first piece
   int32_t from, to;  // query rows that see anything
+  int32_t b;         // context
 };
 
 constexpr int kChunkRows = 128;  // query rows of a workgroup of the chunk kernel
@@ -38,5 +40,7 @@ struct ForwardPlan {
 
 template <typename T, int DP>
 hipError_t run_forward(const AttnArgs& a, const ForwardPlan& p, hipStream_t st);
+template <typename S, int DP>
+hipError_t run_view(const AttnView& a, const ForwardPlan& p, hipStream_t st);
 
 }  // namespace kvx

@@ -84,4 +84,39 @@ hipError_t launch_forward(const kvx_attn* at, const AttnArgs& a, int max_new, vo
   }
 }
 
+// The most slots that a row of a context sees, as far as the host knows.
+static int64_t most_seen(const AttnView& a, int max_new) {
+  const int64_t all = a.c.capacity;
+  return a.window ? std::min<int64_t>(all, int64_t(a.window) + a.sink + max_new) : all;
+}
+
+hipError_t launch_view(const kvx_attn* at, const AttnView& a, int code, int max_new, void* workspace,
+                       hipStream_t st) {
+  ForwardPlan p{};
+  p.heads = static_cast<JoinHead*>(workspace);
+  p.pieces = reinterpret_cast<float*>(static_cast<char*>(workspace) + head_bytes(at));
+  const int64_t strips = (int64_t(a.rows) * at->group + kChunkRows - 1) / kChunkRows +
+                         std::min(a.batch, a.rows);
+  const int64_t units = strips * a.hkv;
+  const int64_t seen = most_seen(a, max_new);
+  p.decode = int64_t(max_new) * at->group <= kDecodeRows || !launchable(units, 256);
+  if (p.decode) {
+    p.grid = at->n_cu;
+    p.splits = seen <= 512 ? 1 : 0;
+    p.join_rows = static_cast<int>(std::min(int64_t(max_new) * at->group, int64_t(kDecodeRows)));
+  } else {
+    p.join_rows = kChunkRows;
+    p.splits = splits_of(at, units);
+    p.strips = static_cast<int>(strips);
+    p.grid = static_cast<int>(units * p.splits);
+  }
+  const int dp = padded_dim(at->model.head_dim);
+#define KVX_BY_WIDTH(S) \
+  (dp == 64 ? run_view<S, 64>(a, p, st) : dp == 128 ? run_view<S, 128>(a, p, st) : run_view<S, 256>(a, p, st))
+  if (code == KVX_CODE_I8) return KVX_BY_WIDTH(code_i8);
+  if (code == KVX_CODE_E4M3) return KVX_BY_WIDTH(code_e4m3);
+  return at->dtype == KVX_F32 ? KVX_BY_WIDTH(float) : KVX_BY_WIDTH(bf16_t);
+#undef KVX_BY_WIDTH
+}
+
 }  // namespace kvx

@@ -63,6 +63,7 @@ __device__ __forceinline__ bool finite(float x) {
 // (keys) or 128 bytes (values).
 template <typename T, int DP>
 struct Tile {
+  static constexpr int kElem = sizeof(T);
   static constexpr int kChunks = DP * sizeof(T) / 16;
   static constexpr int kKeyAt = kChunks < 16 ? 4 : 8;   // addresses of a lane's key pieces
   static constexpr int kRowBytes = DP * sizeof(T);
@@ -250,12 +251,14 @@ __device__ __forceinline__ void copy16(const char* from, uint32_t lds) {
 // N such copies of one base, to lds + i * STEP: the wait states are spent once.
 template <int N, int STEP>
 __device__ __forceinline__ void copy16_run(const char* from, const uint32_t* off, uint32_t lds) {
-  static_assert(N == 2 || N % 4 == 0, "");
+  static_assert(N <= 2 || N % 4 == 0, "");
   const uint64_t p = reinterpret_cast<uint64_t>(from);
   const uint64_t base = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p >> 32))) << 32 |
                         static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p)));
   lds = __builtin_amdgcn_readfirstlane(lds);
-  if constexpr (N == 2) {
+  if constexpr (N == 1) {
+    copy16(from, off[0], lds);
+  } else if constexpr (N == 2) {
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
         "s_add_u32 m0, m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(lds),
@@ -297,15 +300,21 @@ __device__ __forceinline__ void fetch_blocks(const CacheArgs& c, int b, int j0, 
   for (int k = 0; k < TK / 16; ++k) out.id[k] = t[fdiv(c.bs, min(j0 + 16 * k, hi - 1))];
 }
 
+// The slots [lo, hi) that a unit sees.
+struct Range {
+  int lo, hi;
+  __device__ __forceinline__ bool inside(int j0, int n) const { return j0 >= lo && j0 + n <= hi; }
+  __device__ __forceinline__ int nearest(int j) const { return min(max(j, lo), hi - 1); }
+};
+
 // Copies rows j0 .. j0 + TK - 1 of a cache (keys at kb, values at vb of one
 // head) into LDS at lk and lv, each wave w of WAVES its share, each lane the
-// chunk that belongs at its place.  Slots outside [lo, hi) are replaced by the
-// nearest inside.
-template <typename T, int DP, int TK, int WAVES, bool KEYS = true, bool VALUES = true>
+// chunk that belongs at its place (L: the rows' layout).  Slots that the unit
+// does not see are replaced by the nearest that it does.
+template <typename L, int TK, int WAVES, bool KEYS, bool VALUES, typename R_>
 __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, const char* vb, int b,
-                                          int j0, int lo, int hi, const Blocks<TK>& blocks, int d, int w,
+                                          int j0, const R_& range, const Blocks<TK>& blocks, int d, int w,
                                           uint32_t lk, uint32_t lv) {
-  using L = Tile<T, DP>;
   constexpr int R = L::kRowsPerCopy;                          // rows of a copy instruction
   constexpr int kCopies = TK * L::kRowBytes / 1024 / WAVES;   // of a wave, keys or values
   constexpr int kStep = WAVES * R;                            // rows from one to the wave's next
@@ -318,14 +327,14 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
     asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(lane));
   }
   const int sub = lane / L::kChunks;
-  const uint32_t st = static_cast<uint32_t>(c.st) * sizeof(T);
+  const uint32_t st = static_cast<uint32_t>(c.st) * L::kElem;
   // copy i moves rows i kStep + w R + sub: the swizzle of its low bits is the
   // lane's, that of the high ones a constant
-  const int low = w * R + sub, bytes = d * static_cast<int>(sizeof(T));
+  const int low = w * R + sub, bytes = d * L::kElem;
   const int ck = ((lane % L::kChunks) ^ L::key_swz(low)) * 16;
   const int cv = ((lane % L::kChunks) ^ L::value_swz(low)) * 16;
-  const int64_t sb = c.sb * static_cast<int64_t>(sizeof(T));
-  if (kCopies <= 8 && j0 >= lo && j0 + TK <= hi && c.run >= TK && d == DP) {
+  const int64_t sb = c.sb * L::kElem;
+  if (kCopies <= 8 && range.inside(j0, TK) && c.run >= TK && bytes == L::kRowBytes) {
     // the whole tile lies in one block, rows have all of DP: one base (not for
     // more copies, whose offsets would fill the registers)
     const int32_t id = c.table ? blocks.id[0] : b;
@@ -342,7 +351,7 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
       for (int i = 0; i < kCopies; ++i) off[i] = (i * kStep + sub) * st + (cv ^ (L::value_swz(i * kStep) * 16));
       copy16_run<kCopies, WAVES * 1024>(vb + at, off, lv + w * 1024);
     }
-  } else if (j0 >= lo && j0 + TK <= hi && c.run >= 16) {
+  } else if (range.inside(j0, TK) && c.run >= 16) {
 #pragma unroll
     for (int i = 0; i < kCopies; i += kRun) {
       const int row = i * kStep + w * R, j = j0 + row;  // the first of kRun copies in one block
@@ -350,14 +359,15 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
       uint32_t slot = j;
       if (c.table) {
         id = blocks.id[i * kStep / 16];
-        if constexpr (kStep > 16)
-          if (w * R >= 16) id = blocks.id[i * kStep / 16 + 1];
+#pragma unroll
+        for (int x = 1; x < kStep / 16; ++x)
+          if (w * R >= 16 * x) id = blocks.id[i * kStep / 16 + x];
         slot = j - fdiv(c.bs, j) * c.bs.d;
       }
       const int64_t at = id * sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
       const uint32_t to = (i * WAVES + w) * 1024;
       if constexpr (kRun > 1) {
-        if (d == DP) {
+        if (bytes == L::kRowBytes) {
           uint32_t off[kRun];
           if constexpr (KEYS) {
 #pragma unroll
@@ -385,8 +395,8 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
     }
   } else {
     // lane i finds row i's place
-    const int j = min(max(j0 + lane % TK, lo), hi - 1);
-    const int64_t at = cache_offset(c, cache_block(c, b, j), j) * static_cast<int64_t>(sizeof(T));
+    const int j = range.nearest(j0 + lane % TK);
+    const int64_t at = cache_offset(c, cache_block(c, b, j), j) * L::kElem;
     const uint32_t at_lo = static_cast<uint32_t>(at), at_hi = static_cast<uint32_t>(at >> 32);
 #pragma unroll 1
     for (int i = 0; i < kCopies; ++i) {
@@ -403,12 +413,21 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
   }
 }
 
+template <typename T, int DP, int TK, int WAVES, bool KEYS = true, bool VALUES = true>
+__device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, const char* vb, int b,
+                                          int j0, int lo, int hi, const Blocks<TK>& blocks, int d, int w,
+                                          uint32_t lk, uint32_t lv) {
+  copy_tile<Tile<T, DP>, TK, WAVES, KEYS, VALUES>(c, kb, vb, b, j0, Range{lo, hi}, blocks, d, w, lk, lv);
+}
+
 // Query rows of a KV head's unit are (new token, head of the group), the group
 // fastest: all heads that share a KV head share its tiles.
 struct QueryRow {
   int row, g;  // row of the new tokens, head within the group
   int lo, hi;  // slots that it sees; empty past the context's last row
 };
+
+__device__ __forceinline__ bool sees_any(const QueryRow& q) { return q.lo < q.hi; }
 
 __device__ __forceinline__ QueryRow query_row(const AttnArgs& a, const Context& c, int r) {
   QueryRow q;
@@ -428,6 +447,34 @@ __device__ __forceinline__ void seen_by(const AttnArgs& a, const Context& c, int
   hi = end_seen(c, p1);
   lo = min(first_seen(a, max(p0, 0)), hi);
 }
+
+// What query rows r0 .. r1 see: [lo, hi) together, [alo, ahi) all of them.
+struct Reach : Range {
+  int alo, ahi;
+  // no row sees any of slots j .. j + n - 1
+  __device__ __forceinline__ bool misses(int j, int n) const { return j >= hi || j + n <= lo; }
+  __device__ __forceinline__ bool all_see(int j, int n) const { return j >= alo && j + n <= ahi; }
+};
+
+__device__ __forceinline__ Reach reach(const AttnArgs& a, const Context& c, int r0, int r1) {
+  Reach r;
+  int x;
+  seen_by(a, c, r0, r1, r.lo, r.hi);
+  seen_by(a, c, r0, r0, x, r.ahi);  // the least that any row's end is
+  seen_by(a, c, r1, r1, r.alo, x);  // the most that any row's start is
+  return r;
+}
+
+// A unit's tiles of TK slots, numbered first .. first + count - 1.
+template <int TK>
+struct Line {
+  int first, count;
+  __device__ __forceinline__ explicit Line(const Reach& r)
+      : first(r.lo / TK), count(r.lo < r.hi ? (r.hi + TK - 1) / TK - r.lo / TK : 0) {}
+  __device__ __forceinline__ int slot(int t) const { return t * TK; }
+  // the first tile that ends past slot `to`
+  __device__ __forceinline__ int until(int to) const { return to / TK; }
+};
 
 // Query rows [from, to) of those from r0 on that see anything: slots before them
 // are negative, windows after them start past the cache's last slot.

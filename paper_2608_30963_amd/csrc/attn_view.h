@@ -65,6 +65,12 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
   return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
 }
 
+// Pair of slot j in block `block`, of head 0.
+__device__ __forceinline__ int64_t scale_offset(const CacheArgs& c, const ScaleArgs& s, int32_t block, int j) {
+  const int slot = c.table ? j - fdiv(c.bs, j) * static_cast<int>(c.bs.d) : j;
+  return block * s.sb + slot * s.st;
+}
+
 // Which of the slots j0 .. j0 + 31 the row sees, slot j0 + i in bit i.
 __device__ __forceinline__ uint32_t seen_bits(const Sight& s, int j0) {
   uint32_t bits = low_bits(s.hi - j0) & (~low_bits(s.lo - j0) | low_bits(s.sink - j0));
