@@ -1,0 +1,490 @@
+// attn_few.h -- attention of up to 16 query rows of a KV head under a view:
+// single tokens of most models.
+//
+// As single tokens' kernel (attn_forward_kernels.h), with 16 x 16 matrix
+// instructions: half of its sums, scores and weights, so that twice the waves
+// fit a compute unit.  Lane (n, g) = (lane % 16, lane / 16) holds query n's
+// scores of slots 16 u + 4 g + v (register v of block u), which are the weights'
+// operand as they stand if the contraction over 32 slots takes them in that
+// order, and columns 16 db + 4 g + v of its sum.
+#pragma once
+
+#include "attn_forward.h"
+#include "attn_view_tile.h"
+
+namespace kvx {
+namespace {
+
+constexpr int kFewRows = 16;
+
+// The values of x over the lanes of a query.
+__device__ __forceinline__ void both_rows(float x, float& a, float& b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float query_max(float x) {
+  float a, b;
+  both_rows(x, a, b);
+  return half_max(fmaxf(a, b));
+}
+__device__ __forceinline__ float query_sum(float x) {
+  float a, b;
+  both_rows(x, a, b);
+  return half_sum(a + b);
+}
+
+// A tile of 32 slots in LDS, rows of DP numbers of S.  16-byte chunk c of row r
+// lies at c ^ swz(r), so that the 16 rows of a chunk (keys), or the rows that half
+// a wave's transposing read takes (values), cover all of the LDS's 64 banks.
+template <typename S, int DP>
+struct FewTile {
+  static constexpr bool kCoded = sizeof(S) == 1;
+  static constexpr int kElem = sizeof(S), kRowBytes = DP * kElem, kChunks = kRowBytes / 16;
+  static constexpr int kRowsPerCopy = 64 / kChunks, kBytes = 32 * kRowBytes, kCopies = kBytes / 1024;
+  static constexpr int kQ = DP / 32;  // operands of a query
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+  static __device__ __forceinline__ constexpr int key_swz(int r) {
+    return kChunks == 4 ? (r >> 2) & 3 : kChunks == 8 ? (r >> 1) & 7 : r & 15;
+  }
+  static __device__ __forceinline__ constexpr int value_swz(int r) {
+    if constexpr (!kCoded) return kChunks == 8 ? (r >> 1 & 3) << 1 : (r & 7) << 1;
+    return kChunks == 4   ? (r >> 2 & 1) | (r >> 4 & 1) << 1
+           : kChunks == 8 ? (r >> 1 & 3) | (r >> 4 & 1) << 2
+                          : (r & 7) | (r >> 4 & 1) << 3;
+  }
+
+  struct LaneAt {
+    int k;  // keys: row 16 u + n, chunk 4 x + g is at (k ^ 64 x) + 16 u rows
+    int v;  // values: column block db at v ^ 32 db (codes: 16 db), + 16 u rows
+  };
+  static __device__ __forceinline__ LaneAt lane_at() {
+    const int lane = threadIdx.x % 64, i = lane % 16, g = lane / 16;
+    LaneAt at;
+    at.k = i * kRowBytes + (g ^ key_swz(i)) * 16;
+    if constexpr (kCoded) {  // 8 rows x 16 codes: 4 g + 0..3 and 16 rows on
+      const int row = 4 * g + i / 2 % 4 + 16 * (i / 8);
+      at.v = row * kRowBytes + value_swz(row) * 16 + i % 2 * 8;
+    } else {  // 4 rows x 16 numbers
+      const int row = 4 * g + i / 4;
+      at.v = row * kRowBytes + (i % 4 / 2 ^ value_swz(row)) * 16 + i % 2 * 8;
+    }
+    return at;
+  }
+
+  // The query operands of lane (n, g): columns 32 x + 8 g + 0..7 (codes, which a
+  // lane reads 16 at a time: 64 (x / 2) + 16 g + 8 (x % 2) + 0..7).
+  static __device__ __forceinline__ void load_q(uint4 (&q)[kQ], const bf16_t* row, int d) {
+    const int g = threadIdx.x % 64 / 16;
+#pragma unroll
+    for (int x = 0; x < kQ; ++x) {
+      const int e = kCoded ? x / 2 * 64 + g * 16 + x % 2 * 8 : x * 32 + g * 8;
+      q[x] = row && e < d ? *reinterpret_cast<const uint4*>(row + e) : uint4{0, 0, 0, 0};
+    }
+  }
+
+  // Dot products of the 32 rows with the queries, keys times `scale` (e4m3: of rows
+  // n and 16 + n; others: 1).
+  static __device__ __forceinline__ void scores(f32x4 (&s)[2], const char* k, const LaneAt& at,
+                                                const uint4 (&q)[kQ], const float (&scale)[2]) {
+    constexpr int kReads = kCoded ? kQ / 2 : kQ;
+    uint4 piece[2][kReads];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int x = 0; x < kReads; ++x)
+        piece[u][x] = *reinterpret_cast<const uint4*>(k + (at.k ^ 64 * x) + u * 16 * kRowBytes);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < kQ; ++x)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8 a;
+        if constexpr (kCoded) {
+          const uint4 p = piece[u][x / 2];
+          a = x % 2 ? code_numbers<S>(p.z, p.w, scale[u]) : code_numbers<S>(p.x, p.y, scale[u]);
+        } else {
+          a = __builtin_bit_cast(bf16x8, piece[u][x]);
+        }
+        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, q[x]), s[u], 0, 0, 0);
+      }
+  }
+
+  // The values' operand of columns 16 db + 0..15, as it is read.
+  struct Raw {
+    i32x2 x[kCoded ? 1 : 2];
+  };
+  static __device__ __forceinline__ Raw value_raw(const char* v, const LaneAt& at, int db) {
+    Raw r;
+    if constexpr (kCoded) {
+      r.x[0] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(v + (at.v ^ 16 * db)));
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        r.x[u] = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                               (lds_s16x4*)(v + (at.v ^ 32 * db) + u * 16 * kRowBytes)));
+    }
+    return r;
+  }
+  static __device__ __forceinline__ bf16x8 value_numbers(const Raw& r) {
+    if constexpr (kCoded) {
+      return code_numbers<S>(r.x[0][0], r.x[0][1]);
+    } else {
+      union {
+        i32x2 i[2];
+        bf16x8 x;
+      } u;
+      u.i[0] = r.x[0];
+      u.i[1] = r.x[1];
+      return u.x;
+    }
+  }
+
+  static __device__ __forceinline__ bool any_odd(const char* v) {
+    if constexpr (kCoded)
+      return CodeTile<S, DP>::any_odd(v);
+    else
+      return Tile<S, DP>::any_odd(v);
+  }
+};
+
+// A tile's scores become weights and are added up (as code_step and edge_step).
+// `between` is run when the keys, and `values` before the values are read.
+template <typename S, int DP, Cap CAP, bool EDGE, typename Between, typename Values>
+__device__ __forceinline__ bool few_step(const AttnView& a, const char* k, const char* v, const char* pairs,
+                                         const typename FewTile<S, DP>::LaneAt& at,
+                                         const uint4 (&q)[FewTile<S, DP>::kQ], int j0, const Sight& row,
+                                         Softmax& st, f32x4 (&acc)[DP / 16], Between between, Values values) {
+  using L = FewTile<S, DP>;
+  constexpr bool kCoded = L::kCoded, kI8 = std::is_same<S, code_i8>::value;
+  constexpr int NB = DP / 16, kAhead = NB < 8 ? NB : 8;
+  const int lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
+  const uint32_t bits = EDGE ? seen_bits(row, j0) >> 4 * g : 0;
+  auto sees = [&](int u, int x) __attribute__((always_inline)) { return bits >> (16 * u + x) & 1; };
+  float mine[2] = {1.f, 1.f};
+  uint32_t pair[2][4];
+  if constexpr (kCoded) {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(pairs);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (!kI8) mine[u] = key_scale(p[16 * u + n]);
+      const uint4 y = *reinterpret_cast<const uint4*>(p + 16 * u + 4 * g);
+      pair[u][0] = y.x;
+      pair[u][1] = y.y;
+      pair[u][2] = y.z;
+      pair[u][3] = y.w;
+    }
+  }
+  f32x4 s[2];
+  L::scores(s, k, at, q, mine);
+  __builtin_amdgcn_sched_barrier(0);
+  between();
+  __builtin_amdgcn_sched_barrier(0);
+  float top = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      float y = s[u][x];
+      if constexpr (kI8) y *= key_scale(pair[u][x]);
+      y = CAP == Cap::none   ? y * a.scale2
+          : CAP == Cap::part ? __builtin_fmaf(-2.f * a.cap2, cap_part(a, y), a.cap2)
+                             : a.cap2 * cap_tanh(a, y);
+      if (EDGE && !sees(u, x)) y = -INFINITY;
+      s[u][x] = y;
+      top = fmaxf(top, y);
+    }
+  top = query_max(top);
+  if (exceeds(st, top, 8.f)) {
+    const float m = fmaxf(st.m2, top);
+    const float alpha = m == st.m2 ? 1.f : __builtin_amdgcn_exp2f(st.m2 - m);
+    st.m2 = m;
+    st.l *= alpha;
+#pragma unroll
+    for (int db = 0; db < NB; ++db) acc[db] *= alpha;
+  }
+  const float ref = st.m2 == -INFINITY ? 0.f : st.m2;
+  bf16x8 p;
+  float sum = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      float w = __builtin_amdgcn_exp2f(s[u][x] - ref);
+      sum += w;
+      if constexpr (kCoded) {
+        w *= value_scale(pair[u][x]);
+        if (EDGE && !sees(u, x)) w = 0.f;  // not 0 times a NaN
+      }
+      // rounded once to bf16 for the matrix instruction, with its value's scale
+      p[4 * u + x] = static_cast<__bf16>(w);
+    }
+  st.l += sum;
+  values();
+  const bool odd = EDGE && L::any_odd(v);
+  typename L::Raw raw[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) raw[i] = L::value_raw(v, at, i);
+#pragma unroll
+  for (int db = 0; db < NB; ++db) {
+    bf16x8 x = L::value_numbers(raw[db % kAhead]);
+    if (db + kAhead < NB) raw[db % kAhead] = L::value_raw(v, at, db + kAhead);
+    if (EDGE && odd) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (!finite(static_cast<float>(x[e]))) x[e] = static_cast<__bf16>(0.f);
+    }
+    acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p, acc[db], 0, 0, 0);
+  }
+  return odd;
+}
+
+template <typename S, int DP>
+struct Few {
+  using L = FewTile<S, DP>;
+  static constexpr int kStage = 2 * L::kBytes + (L::kCoded ? 128 : 0);  // and pairs of scales
+  static constexpr int kWaves = kStage <= 17 * 1024 ? 8 : 4;
+  static constexpr int kStages = 144 * 1024 / kWaves / kStage < 4 ? 144 * 1024 / kWaves / kStage : 4;
+  static constexpr int kRing = kStages * kStage;
+  static constexpr int kStep = kWaves * 32;  // slots of a workgroup's step
+  static_assert(kStages >= 1 && kWaves * kRing <= 160 * 1024 && kRing >= kFewRows * DP * 4 + 128, "");
+};
+
+template <typename S, int DP>
+__device__ __forceinline__ int few_steps(const AttnView& a, const Context& c, int qt) {
+  const int r0 = qt * kFewRows;
+  const ViewLine<32> line(reach(a, c, r0, min(r0 + kFewRows, c.m * a.group) - 1));
+  return max(1, (line.count + Few<S, DP>::kWaves - 1) / Few<S, DP>::kWaves);
+}
+
+template <typename S, int DP, Cap CAP>
+__global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), 1) forward_few(AttnView a, ForwardPlan fp) {
+  using L = FewTile<S, DP>;
+  using F = Few<S, DP>;
+  constexpr int NW = F::kWaves, NT = 64 * NW, NST = F::kStages, NB = DP / 16;
+  __shared__ __attribute__((aligned(16))) char lds[NW * F::kRing];
+  const int tid = threadIdx.x, lane = tid % 64, n = lane % 16, g = lane / 16;
+  const int w = __builtin_amdgcn_readfirstlane(tid / 64);
+  JoinHead* head = fp.heads + blockIdx.x;
+
+  // a unit is one step of the line where units are not split
+  const bool whole = fp.splits == 1;
+  const Share share = line_share(a, [&](int b) {
+    const Context c = context(a, b);
+    const int qts = (c.m * a.group + kFewRows - 1) / kFewRows;
+    if (whole) return static_cast<int64_t>(qts);
+    int64_t s = 0;
+    for (int qt = 0; qt < qts; ++qt) s += few_steps<S, DP>(a, c, qt);
+    return s;
+  });
+  if (tid == 0 && !whole) head->pieces = 0;
+  const int64_t s0 = share.s0, s1 = share.s1, per = share.per;
+  if (s0 >= s1) return;
+  int h = share.h, b = share.b, step = share.step;
+  Context c = context(a, b);
+  int qt = whole ? step : 0;
+  if (whole) step = 0;
+  for (int x; step >= (x = few_steps<S, DP>(a, c, qt)); ++qt) step -= x;
+
+  const typename L::LaneAt at = L::lane_at();
+  char* const ring = lds + w * F::kRing;
+  const uint32_t ring3 = lds_address(lds) + w * F::kRing;
+
+  for (int64_t s = s0; s < s1;) {
+    // one unit: steps [step, step + cnt) of its `all`
+    const int all = few_steps<S, DP>(a, c, qt);
+    const int cnt = whole ? all : static_cast<int>(min<int64_t>(all - step, s1 - s));
+    const int r0 = qt * kFewRows, valid = min(kFewRows, c.m * a.group - r0);
+    const ViewReach range = reach(a, c, r0, r0 + valid - 1);
+    const ViewLine<32> line(range);
+    const int tiles = min(cnt, max(line.count - (step * NW + w) + NW - 1, 0) / NW);
+    const ViewRow qr = query_row(a, c, r0 + n);
+    uint4 q[L::kQ];
+    const bf16_t* qp = reinterpret_cast<const bf16_t*>(a.q) + qr.row * a.q_sr + (h * a.group + qr.g) * a.q_sh;
+    L::load_q(q, n < valid ? qp : nullptr, a.d);
+    const char* kb = a.c.k + h * a.c.sh * static_cast<int64_t>(sizeof(S));
+    const char* vb = a.c.v + h * a.c.sh * static_cast<int64_t>(sizeof(S));
+    f32x4 acc[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    Softmax st;
+    __syncthreads();  // LDS is free of the last unit's join
+    if (a.d < DP) {
+      // copies leave the chunks past head_dim alone: zeros
+      for (int i = lane; i < F::kRing / 16; i += 64) reinterpret_cast<uint4*>(ring)[i] = uint4{0, 0, 0, 0};
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+
+    auto slot_of = [&](int t) __attribute__((always_inline)) { return line.slot(step * NW + w + t * NW); };
+    // a tile's keys (with the scales) and its values are asked for apart, each
+    // where the last ones of its stage have been read
+    constexpr int kKeys = L::kCopies + (L::kCoded ? 1 : 0), kValues = L::kCopies;
+    Blocks<32> kblocks, vblocks;
+    auto copy_keys = [&](int t) __attribute__((always_inline)) {
+      const int j0 = slot_of(t);
+      const uint32_t to = ring3 + t % NST * F::kStage;
+      copy_tile<L, 32, 1, true, false>(a.c, kb, vb, b, j0, range, kblocks, a.d, 0, to, 0);
+      if constexpr (L::kCoded) {
+        const int i = lane % 32, j = range.nearest(j0 + i);
+        int32_t block = b;
+        if (a.c.table) {
+          if (a.c.run >= 16 && range.inside(j0, 32))
+            block = i < 16 ? kblocks.id[0] : kblocks.id[1];
+          else
+            block = cache_block(a.c, b, j);
+        }
+        if (lane < 32)
+          copy4(reinterpret_cast<const char*>(a.scale.p + scale_offset(a.c, a.scale, block, j) + h * a.scale.sh),
+                to + 2 * L::kBytes);
+      }
+      vblocks = kblocks;
+    };
+    auto copy_values = [&](int t) __attribute__((always_inline)) {
+      copy_tile<L, 32, 1, false, true>(a.c, kb, vb, b, slot_of(t), range, vblocks, a.d, 0, 0,
+                                       ring3 + t % NST * F::kStage + L::kBytes);
+    };
+    // block numbers are asked for where no wait for LDS follows soon: such a
+    // wait covers scalar loads too
+    auto fetch = [&](int t) __attribute__((always_inline)) { fetch_blocks(a.c, b, slot_of(t), range.hi, kblocks); };
+    bool odd = false;
+    if (tiles > 0) fetch(0);
+    for (int t = 0; t < NST && t < tiles; ++t) {
+      copy_keys(t);
+      copy_values(t);
+      fetch(t + 1);
+    }
+    // the queries are here: the compiler must not wait for them in the loop
+    __builtin_amdgcn_s_waitcnt(0);
+    for (int t = 0; t < tiles; ++t) {
+      __builtin_amdgcn_sched_barrier(0);
+      // all has been asked for up to tile t + NST - 1
+      const bool more = t + NST - 1 < tiles, next = t + NST < tiles;
+      if (more)
+        vm_wait<kValues + (NST - 1) * (kKeys + kValues)>();
+      else
+        vm_wait<0>();
+      const char* k = ring + t % NST * F::kStage;
+      const char* v = k + L::kBytes;
+      const int j0 = slot_of(t);
+      auto between = [&]() __attribute__((always_inline)) {
+        if (!next) return;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // keys and scales are read
+        copy_keys(t + NST);
+      };
+      auto values = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (next)
+          vm_wait<(NST - 1) * (kKeys + kValues) + kKeys>();
+        else if (more)
+          vm_wait<(NST - 1) * (kKeys + kValues)>();
+        else
+          vm_wait<0>();
+      };
+      if (range.all_see(j0, 32))
+        few_step<S, DP, CAP, false>(a, k, v, v + L::kBytes, at, q, j0, qr.s, st, acc, between, values);
+      else
+        odd |= few_step<S, DP, CAP, true>(a, k, v, v + L::kBytes, at, q, j0, qr.s, st, acc, between, values);
+      __builtin_amdgcn_sched_barrier(0);
+      if (next) {
+        copy_values(t + NST);
+        fetch(t + NST + 1);
+      }
+    }
+
+    // the waves' results through LDS: each in its own ring, rows of DP floats,
+    // 16-byte pieces swizzled by the row; then (m2, l)
+    const float l = query_sum(st.l);
+    if (n < valid) {
+      float4* o = reinterpret_cast<float4*>(ring) + n * (DP / 4);
+#pragma unroll
+      for (int db = 0; db < NB; ++db)
+        o[(4 * db + g) ^ (n & 7)] = float4{acc[db][0], acc[db][1], acc[db][2], acc[db][3]};
+      if (g == 0) reinterpret_cast<float2*>(ring + kFewRows * DP * 4)[n] = float2{st.m2, l};
+    }
+    if (odd) {
+#pragma unroll 1
+      for (int r = 0; r < valid; ++r) {
+        const ViewRow u = query_row(a, c, r0 + r);
+        float o[DP / 64];
+        Softmax sm;
+        const bf16_t* qu = reinterpret_cast<const bf16_t*>(a.q) + u.row * a.q_sr + (h * a.group + u.g) * a.q_sh;
+        if (!careful_row<S, bf16_t, DP>(a, b, h, qu, u.s, tiles, slot_of, sm, o)) continue;
+#pragma unroll
+        for (int i = 0; i < DP / 64; ++i) {
+          const int e = i * 64 + lane;
+          reinterpret_cast<float*>(ring)[r * DP + ((e / 4) ^ (r & 7)) * 4 + e % 4] = o[i];
+        }
+        if (lane == 0) reinterpret_cast<float2*>(ring + kFewRows * DP * 4)[r] = float2{sm.m2, sm.l};
+      }
+    }
+    __syncthreads();
+    const bool begins = step == 0, ends = step + cnt == all;
+    float* part = fp.pieces + (2 * static_cast<size_t>(blockIdx.x) + (begins ? 1 : 0)) * piece_floats(kFewRows, DP);
+    for (int i = tid; i < valid * (DP / 4); i += NT) {
+      const int r = i / (DP / 4), e = i % (DP / 4);
+      float2 ml[NW];
+      float m2 = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < NW; ++x) {
+        ml[x] = reinterpret_cast<const float2*>(lds + x * F::kRing + kFewRows * DP * 4)[r];
+        m2 = fmaxf(m2, ml[x].x);
+      }
+      float lsum = 0.f;
+      float4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < NW; ++x) {
+        const float f = ml[x].x == m2 ? 1.f : __builtin_amdgcn_exp2f(ml[x].x - m2);
+        const float4 y = reinterpret_cast<const float4*>(lds + x * F::kRing)[r * (DP / 4) + (e ^ (r & 7))];
+        lsum += f * ml[x].y;
+        o.x += f * y.x;
+        o.y += f * y.y;
+        o.z += f * y.z;
+        o.w += f * y.w;
+      }
+      if (begins && ends) {
+        const ViewRow u = query_row(a, c, r0 + r);
+        const bool sees = sees_any(u);
+        if (4 * e < a.d) {
+          bf16_t* to = reinterpret_cast<bf16_t*>(a.out) + u.row * a.o_sr + (h * a.group + u.g) * a.o_sh + 4 * e;
+          const float x[4] = {o.x, o.y, o.z, o.w};
+          bf16_t y[4];
+#pragma unroll
+          for (int z = 0; z < 4; ++z) y[z] = store_cvt<bf16_t>(sees ? x[z] / lsum : 0.f);
+          *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, y);
+        }
+        if (a.lse && e == 0)
+          a.lse[static_cast<int64_t>(u.row) * a.hq + h * a.group + u.g] =
+              sees ? (m2 + __builtin_amdgcn_logf(lsum)) * kLn2 : -INFINITY;
+      } else {
+        reinterpret_cast<float4*>(part + 2 * kFewRows)[i] = o;
+        if (e == 0) reinterpret_cast<float2*>(part)[r] = float2{m2, lsum};
+      }
+    }
+    if (begins && !ends && tid == 0) {
+      // the unit's other pieces are the first ones of the next workgroups
+      const int64_t end = s - step + all;
+      *head = JoinHead{static_cast<int32_t>((end - 1) / per - blockIdx.x + 1), valid, c.q0, r0, h,
+                       static_cast<int32_t>(2 * blockIdx.x + 1), 0, 0, b};
+    }
+    s += whole ? 1 : cnt;
+    step = 0;
+    if (s < s1) {
+      // the next q tile, of this context or one with new tokens after it
+      ++qt;
+      while (qt * kFewRows >= c.m * a.group) {
+        qt = 0;
+        if (++b == a.batch) {
+          b = 0;
+          ++h;
+        }
+        c = context(a, b);
+      }
+    }
+  }
+}
+
+}  // namespace
+}  // namespace kvx

@@ -30,6 +30,7 @@ constexpr int kDecodeRows = 32;
 
 struct ForwardPlan {
   bool decode;
+  bool few;       // decode, of up to kFewRows query rows: forward_few
   int grid;       // workgroups
   int splits;     // pieces of a unit; 1: none is split; decode: 0, as the work divides
   int strips;     // chunk: q tiles of all contexts, at most

@@ -102,6 +102,7 @@ hipError_t launch_view(const kvx_attn* at, const AttnView& a, int code, int max_
   p.decode = int64_t(max_new) * at->group <= kDecodeRows || !launchable(units, 256);
   if (p.decode) {
     p.grid = at->n_cu;
+    p.few = int64_t(max_new) * at->group <= 16 && at->dtype == KVX_BF16;
     p.splits = seen <= 512 ? 1 : 0;
     p.join_rows = static_cast<int>(std::min(int64_t(max_new) * at->group, int64_t(kDecodeRows)));
   } else {

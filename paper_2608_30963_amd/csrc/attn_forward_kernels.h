@@ -3,6 +3,7 @@
 // bits), A: AttnArgs, or AttnView for calls under a view.
 #pragma once
 
+#include "attn_few.h"
 #include "attn_forward.h"
 #include "attn_tile.h"
 #include "attn_view_tile.h"
@@ -503,8 +504,8 @@ struct Decode {
   static constexpr bool kCoded = sizeof(S) == 1;
   // keys and values of 32 slots, and pairs of scales
   static constexpr int kStage = 2 * 32 * DP * sizeof(S) + (kCoded ? 128 : 0);
-  static constexpr int kWaves = kCoded ? 4 : ring_waves(kStage);
-  static constexpr int kStages = kCoded ? (DP == 256 ? 2 : 4) : ring_stages(kStage);
+  static constexpr int kWaves = kCoded ? (DP == 256 ? 4 : 8) : ring_waves(kStage);
+  static constexpr int kStages = kCoded ? (DP == 64 ? 4 : 2) : ring_stages(kStage);
   static constexpr int kStep = kWaves * 32;  // slots of a workgroup's step
   static_assert(kWaves * kStages * kStage <= 160 * 1024 && kStages * kStage >= 32 * DP * 4 + 256, "");
 };
@@ -800,7 +801,7 @@ __global__ void __launch_bounds__(256) forward_join(A a, ForwardPlan fp) {
   const JoinHead hd = fp.heads[blockIdx.x];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, w = wave % W;
   if (hd.pieces == 0) return;
-  const int unit_rows = fp.decode ? kDecodeRows : kChunkRows;
+  const int unit_rows = fp.few ? kFewRows : fp.decode ? kDecodeRows : kChunkRows;
   const size_t size = piece_floats(unit_rows, DP);
   // decode: piece 0 is slot 1 of its workgroup, the others slot 0 of the next ones
   auto piece = [&](int p) __attribute__((always_inline)) {
@@ -868,7 +869,15 @@ hipError_t run_attention(const A& a, const ForwardPlan& p, hipStream_t st) {
                  : !cap   ? forward_chunk<S, DP, Cap::none, A>
                  : part   ? forward_chunk<S, DP, kPart, A>
                           : forward_chunk<S, DP, Cap::tanh, A>;
-  const dim3 block(p.decode ? 64 * Decode<S, DP>::kWaves : 256);
+  dim3 block(p.decode ? 64 * Decode<S, DP>::kWaves : 256);
+  if constexpr (std::is_same<A, AttnView>::value && sizeof(S) <= 2) {
+    if (p.few) {
+      kernel = !cap   ? forward_few<S, DP, Cap::none>
+               : part ? forward_few<S, DP, Cap::part>
+                      : forward_few<S, DP, Cap::tanh>;
+      block = dim3(64 * Few<S, DP>::kWaves);
+    }
+  }
   const hipError_t e = launch_on(kernel, dim3(p.grid), block, st, a, p);
   if (p.splits == 1) return e;
   if (e != hipSuccess) return e;

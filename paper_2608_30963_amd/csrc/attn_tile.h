@@ -372,13 +372,13 @@ __device__ __forceinline__ void copy_tile(const CacheArgs& c, const char* kb, co
           if constexpr (KEYS) {
 #pragma unroll
             for (int x = 0; x < kRun; ++x)
-              off[x] = (x * kStep + sub) * st + (ck ^ (L::key_swz(x * kStep) * 16));
+              off[x] = (x * kStep + sub) * st + (ck ^ (L::key_swz((i + x) * kStep) * 16));
             copy16_run<kRun, WAVES * 1024>(kb + at, off, lk + to);
           }
           if constexpr (VALUES) {
 #pragma unroll
             for (int x = 0; x < kRun; ++x)
-              off[x] = (x * kStep + sub) * st + (cv ^ (L::value_swz(x * kStep) * 16));
+              off[x] = (x * kStep + sub) * st + (cv ^ (L::value_swz((i + x) * kStep) * 16));
             copy16_run<kRun, WAVES * 1024>(vb + at, off, lv + to);
           }
           continue;
