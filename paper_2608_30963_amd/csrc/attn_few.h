@@ -151,106 +151,62 @@ struct FewTile {
   }
 };
 
-// A tile's scores become weights and are added up (as code_step and edge_step).
-// `between` is run when the keys, and `values` before the values are read.
-template <typename S, int DP, Cap CAP, bool EDGE, typename Between, typename Values>
-__device__ __forceinline__ bool few_step(const AttnView& a, const char* k, const char* v, const char* pairs,
-                                         const typename FewTile<S, DP>::LaneAt& at,
-                                         const uint4 (&q)[FewTile<S, DP>::kQ], int j0, const Sight& row,
-                                         Softmax& st, f32x4 (&acc)[DP / 16], Between between, Values values) {
-  using L = FewTile<S, DP>;
-  constexpr bool kCoded = L::kCoded, kI8 = std::is_same<S, code_i8>::value;
-  constexpr int NB = DP / 16, kAhead = NB < 8 ? NB : 8;
-  const int lane = threadIdx.x % 64, n = lane % 16, g = lane / 16;
-  const uint32_t bits = EDGE ? seen_bits(row, j0) >> 4 * g : 0;
-  auto sees = [&](int u, int x) __attribute__((always_inline)) { return bits >> (16 * u + x) & 1; };
-  float mine[2] = {1.f, 1.f};
-  uint32_t pair[2][4];
-  if constexpr (kCoded) {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(pairs);
+// Copies the 32 rows from slot j0 on into LDS at `to`: keys, or values, of the
+// head at `from`.  id: blocks of the first and second 16, where those lie in one
+// block each.
+template <typename L, bool KEYS>
+__device__ __forceinline__ void few_copy(const CacheArgs& c, const char* from, int b, int j0, const ViewReach& range,
+                                         const int (&id)[2], int d, uint32_t to) {
+  constexpr int R = L::kRowsPerCopy, kHalf = L::kCopies / 2;  // copies of 16 rows
+  const int lane = threadIdx.x % 64, sub = lane / L::kChunks, bytes = d * L::kElem;
+  auto swz = [](int r) { return KEYS ? L::key_swz(r) : L::value_swz(r); };
+  const int chunk = (lane % L::kChunks ^ swz(sub)) * 16;
+  const uint32_t st = static_cast<uint32_t>(c.st) * L::kElem;
+  if (range.inside(j0, 32) && c.run >= 16) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      if constexpr (!kI8) mine[u] = key_scale(p[16 * u + n]);
-      const uint4 y = *reinterpret_cast<const uint4*>(p + 16 * u + 4 * g);
-      pair[u][0] = y.x;
-      pair[u][1] = y.y;
-      pair[u][2] = y.z;
-      pair[u][3] = y.w;
-    }
-  }
-  f32x4 s[2];
-  L::scores(s, k, at, q, mine);
-  __builtin_amdgcn_sched_barrier(0);
-  between();
-  __builtin_amdgcn_sched_barrier(0);
-  float top = -INFINITY;
+      const int j = j0 + 16 * u;
+      const uint32_t slot = c.table ? j - fdiv(c.bs, j) * c.bs.d : j;
+      const char* at = from + (c.table ? id[u] : b) * (c.sb * L::kElem) + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
+      if (bytes == L::kRowBytes) {
+        uint32_t off[kHalf];
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
+        for (int i = 0; i < kHalf; ++i) off[i] = (i * R + sub) * st + (chunk ^ swz(16 * u + i * R) * 16);
+        copy16_run<kHalf, 1024>(at, off, to + u * kHalf * 1024);
+      } else {
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      float y = s[u][x];
-      if constexpr (kI8) y *= key_scale(pair[u][x]);
-      y = CAP == Cap::none   ? y * a.scale2
-          : CAP == Cap::part ? __builtin_fmaf(-2.f * a.cap2, cap_part(a, y), a.cap2)
-                             : a.cap2 * cap_tanh(a, y);
-      if (EDGE && !sees(u, x)) y = -INFINITY;
-      s[u][x] = y;
-      top = fmaxf(top, y);
-    }
-  top = query_max(top);
-  if (exceeds(st, top, 8.f)) {
-    const float m = fmaxf(st.m2, top);
-    const float alpha = m == st.m2 ? 1.f : __builtin_amdgcn_exp2f(st.m2 - m);
-    st.m2 = m;
-    st.l *= alpha;
-#pragma unroll
-    for (int db = 0; db < NB; ++db) acc[db] *= alpha;
-  }
-  const float ref = st.m2 == -INFINITY ? 0.f : st.m2;
-  bf16x8 p;
-  float sum = 0.f;
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      float w = __builtin_amdgcn_exp2f(s[u][x] - ref);
-      sum += w;
-      if constexpr (kCoded) {
-        w *= value_scale(pair[u][x]);
-        if (EDGE && !sees(u, x)) w = 0.f;  // not 0 times a NaN
+        for (int i = 0; i < kHalf; ++i) {
+          const int e = chunk ^ swz(16 * u + i * R) * 16;
+          if (e < bytes) copy16(at, (i * R + sub) * st + e, to + (u * kHalf + i) * 1024);
+        }
       }
-      // rounded once to bf16 for the matrix instruction, with its value's scale
-      p[4 * u + x] = static_cast<__bf16>(w);
     }
-  st.l += sum;
-  values();
-  const bool odd = EDGE && L::any_odd(v);
-  typename L::Raw raw[kAhead];
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) raw[i] = L::value_raw(v, at, i);
-#pragma unroll
-  for (int db = 0; db < NB; ++db) {
-    bf16x8 x = L::value_numbers(raw[db % kAhead]);
-    if (db + kAhead < NB) raw[db % kAhead] = L::value_raw(v, at, db + kAhead);
-    if (EDGE && odd) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (!finite(static_cast<float>(x[e]))) x[e] = static_cast<__bf16>(0.f);
+  } else {
+    // lane i finds row i's place
+    const int j = range.nearest(j0 + lane % 32);
+    const int64_t at = cache_offset(c, cache_block(c, b, j), j) * L::kElem;
+    const uint32_t at_lo = static_cast<uint32_t>(at), at_hi = static_cast<uint32_t>(at >> 32);
+    // here, and wherever a branch loads: left to itself the compiler waits for the
+    // load, and so for all copies, where the branches meet
+    __builtin_amdgcn_s_waitcnt(0);
+#pragma unroll 1
+    for (int i = 0; i < L::kCopies; ++i) {
+      const int row = i * R + sub, e = chunk ^ swz(i * R) * 16;
+      const int64_t o = static_cast<int64_t>(static_cast<uint64_t>(__shfl(at_hi, row)) << 32 | __shfl(at_lo, row));
+      if (e < bytes) copy16(from + o + e, to + i * 1024);
     }
-    acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p, acc[db], 0, 0, 0);
   }
-  return odd;
 }
 
 template <typename S, int DP>
 struct Few {
   using L = FewTile<S, DP>;
   static constexpr int kStage = 2 * L::kBytes + (L::kCoded ? 128 : 0);  // and pairs of scales
-  static constexpr int kWaves = kStage <= 17 * 1024 ? 8 : 4;
-  static constexpr int kStages = 144 * 1024 / kWaves / kStage < 4 ? 144 * 1024 / kWaves / kStage : 4;
+  static constexpr int kWaves = kStage <= 20 * 1024 ? 4 : 2;
+  static constexpr int kStages = 80 * 1024 / kWaves / kStage < 4 ? 80 * 1024 / kWaves / kStage : 4;
   static constexpr int kRing = kStages * kStage;
   static constexpr int kStep = kWaves * 32;  // slots of a workgroup's step
-  static_assert(kStages >= 1 && kWaves * kRing <= 160 * 1024 && kRing >= kFewRows * DP * 4 + 128, "");
+  static_assert(kStages >= 1 && kWaves * kRing <= 80 * 1024 && kRing >= kFewRows * DP * 4 + 128, "");
 };
 
 template <typename S, int DP>
@@ -261,9 +217,10 @@ __device__ __forceinline__ int few_steps(const AttnView& a, const Context& c, in
 }
 
 template <typename S, int DP, Cap CAP>
-__global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), 1) forward_few(AttnView a, ForwardPlan fp) {
+__global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kWaves / 2)) forward_few(AttnView a, ForwardPlan fp) {
   using L = FewTile<S, DP>;
   using F = Few<S, DP>;
+  constexpr bool kI8 = std::is_same<S, code_i8>::value;
   constexpr int NW = F::kWaves, NT = 64 * NW, NST = F::kStages, NB = DP / 16;
   __shared__ __attribute__((aligned(16))) char lds[NW * F::kRing];
   const int tid = threadIdx.x, lane = tid % 64, n = lane % 16, g = lane / 16;
@@ -319,62 +276,131 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), 1) forward_few(Attn
     }
 
     auto slot_of = [&](int t) __attribute__((always_inline)) { return line.slot(step * NW + w + t * NW); };
-    // a tile's keys (with the scales) and its values are asked for apart, each
-    // where the last ones of its stage have been read
+    // A tile's keys (with the scales) and its values are asked for apart, each
+    // where the last ones of its stage have been read.  Block numbers: lane i has
+    // that of tile base + i / 2 and its slots 16 (i % 2) on: one load for 32 tiles
+    // (scalar loads for each would be waited for with the next reads of LDS: 64
+    // contexts of up to 8k slots in blocks of 16 took 6 us more).
     constexpr int kKeys = L::kCopies + (L::kCoded ? 1 : 0), kValues = L::kCopies;
-    Blocks<32> kblocks, vblocks;
-    auto copy_keys = [&](int t) __attribute__((always_inline)) {
-      const int j0 = slot_of(t);
-      const uint32_t to = ring3 + t % NST * F::kStage;
-      copy_tile<L, 32, 1, true, false>(a.c, kb, vb, b, j0, range, kblocks, a.d, 0, to, 0);
-      if constexpr (L::kCoded) {
-        const int i = lane % 32, j = range.nearest(j0 + i);
-        int32_t block = b;
-        if (a.c.table) {
-          if (a.c.run >= 16 && range.inside(j0, 32))
-            block = i < 16 ? kblocks.id[0] : kblocks.id[1];
-          else
-            block = cache_block(a.c, b, j);
-        }
-        if (lane < 32)
-          copy4(reinterpret_cast<const char*>(a.scale.p + scale_offset(a.c, a.scale, block, j) + h * a.scale.sh),
-                to + 2 * L::kBytes);
-      }
-      vblocks = kblocks;
+    const bool table = a.c.table && a.c.run >= 16 && tiles > 0;
+    auto numbers = [&](int t) __attribute__((always_inline)) {
+      const int j = min(slot_of(t + lane / 2) + 16 * (lane % 2), range.hi - 1);
+      return a.c.table[static_cast<int64_t>(b) * a.c.max_blocks + fdiv(a.c.bs, j)];
     };
-    auto copy_values = [&](int t) __attribute__((always_inline)) {
-      copy_tile<L, 32, 1, false, true>(a.c, kb, vb, b, slot_of(t), range, vblocks, a.d, 0, 0,
-                                       ring3 + t % NST * F::kStage + L::kBytes);
-    };
-    // block numbers are asked for where no wait for LDS follows soon: such a
-    // wait covers scalar loads too
-    auto fetch = [&](int t) __attribute__((always_inline)) { fetch_blocks(a.c, b, slot_of(t), range.hi, kblocks); };
+    int base = 0, ids = 0, id[2] = {0, 0};
+    if (table) ids = numbers(0);
     bool odd = false;
-    if (tiles > 0) fetch(0);
-    for (int t = 0; t < NST && t < tiles; ++t) {
-      copy_keys(t);
-      copy_values(t);
-      fetch(t + 1);
-    }
-    // the queries are here: the compiler must not wait for them in the loop
+    // the queries and numbers are here: the compiler must not wait for them in
+    // the loop, where that would be a wait for all copies
     __builtin_amdgcn_s_waitcnt(0);
-    for (int t = 0; t < tiles; ++t) {
-      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+    for (int t = -NST; t < tiles; ++t) {
+      const int ahead = t + NST;
       // all has been asked for up to tile t + NST - 1
-      const bool more = t + NST - 1 < tiles, next = t + NST < tiles;
-      if (more)
-        vm_wait<kValues + (NST - 1) * (kKeys + kValues)>();
-      else
-        vm_wait<0>();
-      const char* k = ring + t % NST * F::kStage;
-      const char* v = k + L::kBytes;
-      const int j0 = slot_of(t);
-      auto between = [&]() __attribute__((always_inline)) {
-        if (!next) return;
+      const bool more = ahead - 1 < tiles, next = ahead < tiles;
+      const char* const stage = ring + (t + NST) % NST * F::kStage;
+      const int j0 = slot_of(max(t, 0));
+      f32x4 sc[2] = {};
+      uint32_t pair[2][4] = {}, bits = ~0u;
+      bool edge = false;
+      if (t >= 0) {
+        if (more)
+          vm_wait<kValues + (NST - 1) * (kKeys + kValues)>();
+        else
+          vm_wait<0>();
+        float mine[2] = {1.f, 1.f};
+        if constexpr (L::kCoded) {
+          const uint32_t* p = reinterpret_cast<const uint32_t*>(stage + 2 * L::kBytes);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            if constexpr (!kI8) mine[u] = key_scale(p[16 * u + n]);
+            const uint4 y = *reinterpret_cast<const uint4*>(p + 16 * u + 4 * g);
+            pair[u][0] = y.x;
+            pair[u][1] = y.y;
+            pair[u][2] = y.z;
+            pair[u][3] = y.w;
+          }
+        }
+        L::scores(sc, stage, at, q, mine);
+        edge = !range.all_see(j0, 32);
+        if (edge) {
+          bits = seen_bits(qr.s, j0) >> 4 * g;
+          __builtin_amdgcn_s_waitcnt(0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (next) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // keys and scales are read
-        copy_keys(t + NST);
-      };
-      auto values = [&]() __attribute__((always_inline)) {
+        const int k0 = slot_of(ahead);
+        const uint32_t to = ring3 + ahead % NST * F::kStage;
+        if (table) {
+          if (ahead - base >= 32) {
+            base = ahead;
+            ids = numbers(ahead);
+            __builtin_amdgcn_s_waitcnt(0);
+          }
+          id[0] = __builtin_amdgcn_readlane(ids, 2 * (ahead - base));
+          id[1] = __builtin_amdgcn_readlane(ids, 2 * (ahead - base) + 1);
+        }
+        few_copy<L, true>(a.c, kb, b, k0, range, id, a.d, to);
+        if constexpr (L::kCoded) {
+          const int i = lane % 32, j = range.nearest(k0 + i);
+          int32_t block = b;
+          if (a.c.table) {
+            if (a.c.run >= 16 && range.inside(k0, 32))
+              block = i < 16 ? id[0] : id[1];
+            else {
+              block = cache_block(a.c, b, j);
+              __builtin_amdgcn_s_waitcnt(0);
+            }
+          }
+          if (lane < 32)
+            copy4(reinterpret_cast<const char*>(a.scale.p + scale_offset(a.c, a.scale, block, j) + h * a.scale.sh),
+                  to + 2 * L::kBytes);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (t >= 0) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            float y = sc[u][x];
+            if constexpr (kI8) y *= key_scale(pair[u][x]);
+            y = CAP == Cap::none   ? y * a.scale2
+                : CAP == Cap::part ? __builtin_fmaf(-2.f * a.cap2, cap_part(a, y), a.cap2)
+                                   : a.cap2 * cap_tanh(a, y);
+            y = bits >> (16 * u + x) & 1 ? y : -INFINITY;
+            sc[u][x] = y;
+            top = fmaxf(top, y);
+          }
+        top = query_max(top);
+        if (exceeds(st, top, 8.f)) {
+          const float m = fmaxf(st.m2, top);
+          const float alpha = m == st.m2 ? 1.f : __builtin_amdgcn_exp2f(st.m2 - m);
+          st.m2 = m;
+          st.l *= alpha;
+#pragma unroll
+          for (int db = 0; db < NB; ++db) acc[db] *= alpha;
+        }
+        const float ref = st.m2 == -INFINITY ? 0.f : st.m2;
+        bf16x8 p;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            float y = __builtin_amdgcn_exp2f(sc[u][x] - ref);
+            sum += y;
+            if constexpr (L::kCoded) {
+              y *= value_scale(pair[u][x]);
+              y = bits >> (16 * u + x) & 1 ? y : 0.f;  // not 0 times a NaN
+            }
+            // rounded once to bf16 for the matrix instruction, with its value's scale
+            p[4 * u + x] = static_cast<__bf16>(y);
+          }
+        st.l += sum;
         __builtin_amdgcn_sched_barrier(0);
         if (next)
           vm_wait<(NST - 1) * (kKeys + kValues) + kKeys>();
@@ -382,16 +408,35 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), 1) forward_few(Attn
           vm_wait<(NST - 1) * (kKeys + kValues)>();
         else
           vm_wait<0>();
-      };
-      if (range.all_see(j0, 32))
-        few_step<S, DP, CAP, false>(a, k, v, v + L::kBytes, at, q, j0, qr.s, st, acc, between, values);
-      else
-        odd |= few_step<S, DP, CAP, true>(a, k, v, v + L::kBytes, at, q, j0, qr.s, st, acc, between, values);
-      __builtin_amdgcn_sched_barrier(0);
-      if (next) {
-        copy_values(t + NST);
-        fetch(t + NST + 1);
+        const char* const v = stage + L::kBytes;
+        if (__builtin_expect(edge && L::any_odd(v), 0)) {
+          odd = true;
+#pragma unroll
+          for (int db = 0; db < NB; ++db) {
+            bf16x8 x = L::value_numbers(L::value_raw(v, at, db));
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (!finite(static_cast<float>(x[e]))) x[e] = static_cast<__bf16>(0.f);
+            acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p, acc[db], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        } else {
+          constexpr int kAhead = NB < 8 ? NB : 8;
+          typename L::Raw raw[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) raw[i] = L::value_raw(v, at, i);
+#pragma unroll
+          for (int db = 0; db < NB; ++db) {
+            const bf16x8 x = L::value_numbers(raw[db % kAhead]);
+            if (db + kAhead < NB) raw[db % kAhead] = L::value_raw(v, at, db + kAhead);
+            acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p, acc[db], 0, 0, 0);
+          }
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
+      if (next)
+        few_copy<L, false>(a.c, vb, b, slot_of(ahead), range, id, a.d,
+                           ring3 + ahead % NST * F::kStage + L::kBytes);
     }
 
     // the waves' results through LDS: each in its own ring, rows of DP floats,
