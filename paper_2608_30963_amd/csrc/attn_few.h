@@ -15,8 +15,6 @@
 namespace kvx {
 namespace {
 
-constexpr int kFewRows = 16;
-
 // The values of x over the lanes of a query.
 __device__ __forceinline__ void both_rows(float x, float& a, float& b) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -202,11 +200,12 @@ template <typename S, int DP>
 struct Few {
   using L = FewTile<S, DP>;
   static constexpr int kStage = 2 * L::kBytes + (L::kCoded ? 128 : 0);  // and pairs of scales
-  static constexpr int kWaves = kStage <= 20 * 1024 ? 4 : 2;
-  static constexpr int kStages = 80 * 1024 / kWaves / kStage < 4 ? 80 * 1024 / kWaves / kStage : 4;
+  static constexpr int kWaves = 4, kGroups = few_groups(DP, sizeof(S));
+  static constexpr int kRoom = 160 * 1024 / kGroups / kWaves / kStage;
+  static constexpr int kStages = kRoom < 4 ? kRoom : 4;
   static constexpr int kRing = kStages * kStage;
   static constexpr int kStep = kWaves * 32;  // slots of a workgroup's step
-  static_assert(kStages >= 1 && kWaves * kRing <= 80 * 1024 && kRing >= kFewRows * DP * 4 + 128, "");
+  static_assert(kStages >= 1 && kWaves * kRing * kGroups <= 160 * 1024 && kRing >= kFewRows * DP * 4 + 128, "");
 };
 
 template <typename S, int DP>
@@ -217,7 +216,7 @@ __device__ __forceinline__ int few_steps(const AttnView& a, const Context& c, in
 }
 
 template <typename S, int DP, Cap CAP>
-__global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kWaves / 2)) forward_few(AttnView a, ForwardPlan fp) {
+__global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroups)) forward_few(AttnView a, ForwardPlan fp) {
   using L = FewTile<S, DP>;
   using F = Few<S, DP>;
   constexpr bool kI8 = std::is_same<S, code_i8>::value;

@@ -27,6 +27,12 @@ struct JoinHead {
 
 constexpr int kChunkRows = 128;  // query rows of a workgroup of the chunk kernel
 constexpr int kDecodeRows = 32;
+constexpr int kFewRows = 16;
+
+// Workgroups of forward_few that a compute unit takes at once, by the padded
+// head_dim and a number's bytes: two, so that one's start and joins pass beside
+// the other's copies, where LDS has room for both.
+constexpr int few_groups(int dp, int bytes) { return dp * bytes <= 256 ? 2 : 1; }
 
 struct ForwardPlan {
   bool decode;

@@ -103,7 +103,7 @@ hipError_t launch_view(const kvx_attn* at, const AttnView& a, int code, int max_
   if (p.decode) {
     p.grid = at->n_cu;
     p.few = int64_t(max_new) * at->group <= 16 && at->dtype == KVX_BF16;
-    if (p.few) p.grid = 2 * at->n_cu;
+    if (p.few) p.grid = at->n_cu * few_groups(padded_dim(at->model.head_dim), code < 0 ? 2 : 1);
     p.splits = seen <= 512 ? 1 : 0;
     p.join_rows = static_cast<int>(std::min(int64_t(max_new) * at->group, int64_t(kDecodeRows)));
   } else {
