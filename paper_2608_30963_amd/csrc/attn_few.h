@@ -141,29 +141,55 @@ struct FewTile {
     }
   }
 
-  static __device__ __forceinline__ bool any_odd(const char* v) {
-    if constexpr (kCoded)
-      return CodeTile<S, DP>::any_odd(v);
-    else
-      return Tile<S, DP>::any_odd(v);
+  // Whether any of the 32 rows' values is not finite (bit 0), and of a row whose
+  // bit is set in `rows` (bit 1).  An exponent of ones (a code's seven low bits)
+  // passes into the bit above it by one more.
+  static __device__ __forceinline__ int odd_values(const char* v, uint32_t rows) {
+    if constexpr (std::is_same<S, code_i8>::value) return 0;
+    const uint32_t ones = kCoded ? 0x7f7f7f7fu : 0x7f807f80u, more = kCoded ? 0x01010101u : 0x00800080u;
+    const int lane = threadIdx.x % 64;
+    uint32_t any = 0, seen = 0;
+#pragma unroll
+    for (int i = 0; i < 32 * kChunks / 64; ++i) {
+      const int place = i * 64 + lane;
+      const uint4 x = *reinterpret_cast<const uint4*>(v + place * 16);
+      const uint32_t y = ((x.x & ones) + more) | ((x.y & ones) + more) | ((x.z & ones) + more) | ((x.w & ones) + more);
+      any |= y;
+      seen |= rows >> place / kChunks & 1 ? y : 0;
+    }
+    const uint32_t top = kCoded ? 0x80808080u : 0x80008000u;
+    return (__any(any & top) ? 1 : 0) | (__any(seen & top) ? 2 : 0);
   }
 };
 
-// Copies the 32 rows from slot j0 on into LDS at `to`: keys, or values, of the
-// head at `from`.  id: blocks of the first and second 16, where those lie in one
-// block each.
+// The 16 slots that are copied for slots j .. j + 15: themselves where the unit
+// sees any of them, else those around the nearest that it does.
+__device__ __forceinline__ int sixteen(const ViewReach& r, int j) {
+  const bool seen = j < r.sink || (j + 16 > r.lo && j < r.hi && r.lo < r.hi);
+  return seen ? j : r.nearest(j) & ~15;
+}
+
+// Whether the 32 slots from j0 on are copied in two runs of 16, each in one block:
+// slots of a run that the unit does not see come along, as whatever they hold.
+__device__ __forceinline__ bool by_sixteen(const CacheArgs& c, int last) {
+  return c.run >= 16 && (c.table || last + 16 <= c.capacity);
+}
+
+// Copies 32 rows into LDS at `to`: keys, or values, of the head at `from`, in runs
+// from slots first[0] and first[1] on, in blocks id, or (runs false) of slots j0 ..
+// j0 + 31, the nearest seen ones instead of those that the unit does not see.
 template <typename L, bool KEYS>
-__device__ __forceinline__ void few_copy(const CacheArgs& c, const char* from, int b, int j0, const ViewReach& range,
-                                         const int (&id)[2], int d, uint32_t to) {
+__device__ __forceinline__ void few_copy(const CacheArgs& c, const char* from, int b, bool runs, const int (&first)[2],
+                                         const int (&id)[2], int j0, const ViewReach& range, int d, uint32_t to) {
   constexpr int R = L::kRowsPerCopy, kHalf = L::kCopies / 2;  // copies of 16 rows
   const int lane = threadIdx.x % 64, sub = lane / L::kChunks, bytes = d * L::kElem;
   auto swz = [](int r) { return KEYS ? L::key_swz(r) : L::value_swz(r); };
   const int chunk = (lane % L::kChunks ^ swz(sub)) * 16;
   const uint32_t st = static_cast<uint32_t>(c.st) * L::kElem;
-  if (range.inside(j0, 32) && c.run >= 16) {
+  if (runs) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int j = j0 + 16 * u;
+      const int j = first[u];
       const uint32_t slot = c.table ? j - fdiv(c.bs, j) * c.bs.d : j;
       const char* at = from + (c.table ? id[u] : b) * (c.sb * L::kElem) + static_cast<int64_t>(static_cast<uint64_t>(slot) * st);
       if (bytes == L::kRowBytes) {
@@ -283,12 +309,12 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroup
     constexpr int kKeys = L::kCopies + (L::kCoded ? 1 : 0), kValues = L::kCopies;
     const bool table = a.c.table && a.c.run >= 16 && tiles > 0;
     auto numbers = [&](int t) __attribute__((always_inline)) {
-      const int j = min(slot_of(t + lane / 2) + 16 * (lane % 2), range.hi - 1);
+      const int j = sixteen(range, min(slot_of(t + lane / 2), range.hi - 1 & ~31) + 16 * (lane % 2));
       return a.c.table[static_cast<int64_t>(b) * a.c.max_blocks + fdiv(a.c.bs, j)];
     };
-    int base = 0, ids = 0, id[2] = {0, 0};
+    int base = 0, ids = 0, id[2] = {0, 0}, first[2] = {0, 0};
     if (table) ids = numbers(0);
-    bool odd = false;
+    bool odd = false, runs = false;
     // the queries and numbers are here: the compiler must not wait for them in
     // the loop, where that would be a wait for all copies
     __builtin_amdgcn_s_waitcnt(0);
@@ -332,6 +358,13 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroup
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // keys and scales are read
         const int k0 = slot_of(ahead);
         const uint32_t to = ring3 + ahead % NST * F::kStage;
+        first[0] = k0;
+        first[1] = k0 + 16;
+        if (!range.inside(k0, 32)) {
+          first[0] = sixteen(range, k0);
+          first[1] = sixteen(range, k0 + 16);
+        }
+        runs = by_sixteen(a.c, max(first[0], first[1]));
         if (table) {
           if (ahead - base >= 32) {
             base = ahead;
@@ -341,18 +374,17 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroup
           id[0] = __builtin_amdgcn_readlane(ids, 2 * (ahead - base));
           id[1] = __builtin_amdgcn_readlane(ids, 2 * (ahead - base) + 1);
         }
-        few_copy<L, true>(a.c, kb, b, k0, range, id, a.d, to);
+        few_copy<L, true>(a.c, kb, b, runs, first, id, k0, range, a.d, to);
         if constexpr (L::kCoded) {
-          const int i = lane % 32, j = range.nearest(k0 + i);
-          int32_t block = b;
-          if (a.c.table) {
-            if (a.c.run >= 16 && range.inside(k0, 32))
-              block = i < 16 ? id[0] : id[1];
-            else {
-              block = cache_block(a.c, b, j);
-              __builtin_amdgcn_s_waitcnt(0);
-            }
+          const int i = lane % 32;
+          int j = i < 16 ? first[0] + i : first[1] + i - 16;
+          int32_t block = i < 16 ? id[0] : id[1];
+          if (!runs) {
+            j = range.nearest(k0 + i);
+            block = cache_block(a.c, b, j);
+            __builtin_amdgcn_s_waitcnt(0);
           }
+          if (!a.c.table) block = b;
           if (lane < 32)
             copy4(reinterpret_cast<const char*>(a.scale.p + scale_offset(a.c, a.scale, block, j) + h * a.scale.sh),
                   to + 2 * L::kBytes);
@@ -408,8 +440,13 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroup
         else
           vm_wait<0>();
         const char* const v = stage + L::kBytes;
-        if (__builtin_expect(edge && L::any_odd(v), 0)) {
-          odd = true;
+        // values that the unit does not see count as zero; if it sees any that is not
+        // finite, rows are computed again
+        int strange = 0;
+        if (edge)
+          strange = L::odd_values(v, low_bits(range.hi - j0) & (~low_bits(range.lo - j0) | low_bits(range.sink - j0)));
+        odd |= strange > 1;
+        if (__builtin_expect(strange, 0)) {
 #pragma unroll
           for (int db = 0; db < NB; ++db) {
             bf16x8 x = L::value_numbers(L::value_raw(v, at, db));
@@ -434,7 +471,7 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroup
       }
       __builtin_amdgcn_sched_barrier(0);
       if (next)
-        few_copy<L, false>(a.c, vb, b, slot_of(ahead), range, id, a.d,
+        few_copy<L, false>(a.c, vb, b, runs, first, id, slot_of(ahead), range, a.d,
                            ring3 + ahead % NST * F::kStage + L::kBytes);
     }
 
