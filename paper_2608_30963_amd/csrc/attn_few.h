@@ -162,13 +162,6 @@ struct FewTile {
   }
 };
 
-// The 16 slots that are copied for slots j .. j + 15: themselves where the unit
-// sees any of them, else those around the nearest that it does.
-__device__ __forceinline__ int sixteen(const ViewReach& r, int j) {
-  const bool seen = j < r.sink || (j + 16 > r.lo && j < r.hi && r.lo < r.hi);
-  return seen ? j : r.nearest(j) & ~15;
-}
-
 // Whether the 32 slots from j0 on are copied in two runs of 16, each in one block:
 // slots of a run that the unit does not see come along, as whatever they hold.
 __device__ __forceinline__ bool by_sixteen(const CacheArgs& c, int last) {

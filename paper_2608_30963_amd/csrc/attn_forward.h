@@ -23,6 +23,7 @@ struct JoinHead {
   int32_t first;   // index of the unit's first piece
   int32_t from, to;  // query rows that see anything
   int32_t b;         // context
+  int32_t step;      // chunk: from one piece's index to the next one's
 };
 
 constexpr int kChunkRows = 128;  // query rows of a workgroup of the chunk kernel

@@ -107,10 +107,12 @@ hipError_t launch_view(const kvx_attn* at, const AttnView& a, int code, int max_
     p.splits = seen <= 512 ? 1 : 0;
     p.join_rows = static_cast<int>(std::min(int64_t(max_new) * at->group, int64_t(kDecodeRows)));
   } else {
+    // with fewer strips than the card takes workgroups at a time they are cut
+    const int64_t slots = std::min(int64_t(at->n_cu) * resident(at), most_pieces(at));
     p.join_rows = kChunkRows;
-    p.splits = splits_of(at, units);
+    p.splits = units < slots ? 2 : 1;
     p.strips = static_cast<int>(strips);
-    p.grid = static_cast<int>(units * p.splits);
+    p.grid = static_cast<int>(std::max(units, p.splits > 1 ? slots : 0));
   }
   const int dp = padded_dim(at->model.head_dim);
 #define KVX_BY_WIDTH(S) \

@@ -161,55 +161,79 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
   constexpr int TK = chunk_tile<T, DP>(), NS = TK / 32, NB = DP / 32;
   constexpr int kBytes = TK * L::kRowBytes;  // keys or values of a tile
   constexpr int kDepth = kCoded ? 1 : chunk_depth<T, DP>();
-  constexpr int kKeys = kCoded ? 2 : kDepth + 2, kValues = kDepth + 1;
+  // codes of 128 columns: two tiles of keys, so that two workgroups fit a unit
+  constexpr int kKeys = kCoded && DP == 128 ? 2 : kDepth + 2, kValues = kDepth + 1;
   constexpr int kCopies = kBytes / 1024 / 4;  // of a wave, keys or values
   constexpr int kCodes = kCoded ? TK * DP : 0;  // bytes of a tile's keys or values as codes
   __shared__ __attribute__((aligned(16))) char lds[(kKeys + kValues) * kBytes + 2 * kCodes];
   const int lane = threadIdx.x % 64, n = lane % 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 
-  // (head, piece, strip): consecutive units of an XCD share a head's cache;
-  // later strips, which see more, first
-  int id = xcd_remap(blockIdx.x, gridDim.x);
-  const int h = id / (fp.strips * fp.splits);
-  id -= h * fp.strips * fp.splits;
-  const int split = id / fp.strips, strip = fp.strips - 1 - id % fp.strips;
+  int h, b = -1, qt = 0, split, strip, pieces = fp.splits, first, step;
+  if constexpr (kView) {
+    const ChunkShare sh = chunk_share<TK>(a, fp.splits > 1);
+    if (fp.splits > 1 && blockIdx.x == 0) {
+      // strips that the caller's bounds allow for and that are not there
+      const int none = fp.strips - sh.strips;
+      for (int i = threadIdx.x; i < none * a.hkv; i += 256)
+        fp.heads[i / none * fp.strips + sh.strips + i % none].pieces = 0;
+    }
+    if (__builtin_amdgcn_readfirstlane(sh.b) < 0) return;
+    h = __builtin_amdgcn_readfirstlane(sh.h);
+    b = __builtin_amdgcn_readfirstlane(sh.b);
+    qt = __builtin_amdgcn_readfirstlane(sh.qt);
+    strip = __builtin_amdgcn_readfirstlane(sh.strip);
+    split = __builtin_amdgcn_readfirstlane(sh.piece);
+    pieces = __builtin_amdgcn_readfirstlane(sh.pieces);
+    first = __builtin_amdgcn_readfirstlane(sh.first);
+    step = __builtin_amdgcn_readfirstlane(sh.step);
+  } else {
+    // (head, piece, strip): consecutive units of an XCD share a head's cache;
+    // later strips, which see more, first
+    int id = xcd_remap(blockIdx.x, gridDim.x);
+    h = id / (fp.strips * fp.splits);
+    id -= h * fp.strips * fp.splits;
+    split = id / fp.strips;
+    strip = fp.strips - 1 - id % fp.strips;
+    first = (h * fp.strips + strip) * fp.splits;
+    step = 1;
 
-  // the strip's context: 64 contexts a step
-  int b = -1, qt = 0, before = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    int cnt = 0;
-    if (b0 + lane < a.batch) {
-      const Context c = context(a, b0 + lane);
-      cnt = (c.m * a.group + kChunkRows - 1) / kChunkRows;
-    }
-    int sum = cnt;
+    // the strip's context: 64 contexts a step
+    int before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+      int cnt = 0;
+      if (b0 + lane < a.batch) {
+        const Context c = context(a, b0 + lane);
+        cnt = (c.m * a.group + kChunkRows - 1) / kChunkRows;
+      }
+      int sum = cnt;
 #pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const int y = __shfl_up(sum, i);
-      if (lane >= i) sum += y;
+      for (int i = 1; i < 64; i <<= 1) {
+        const int y = __shfl_up(sum, i);
+        if (lane >= i) sum += y;
+      }
+      const uint64_t past = __ballot(before + sum > strip);
+      if (past) {
+        const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
+        b = b0 + f;
+        qt = strip - before - (__shfl(sum, f) - __shfl(cnt, f));
+        break;
+      }
+      before += __shfl(sum, 63);
     }
-    const uint64_t past = __ballot(before + sum > strip);
-    if (past) {
-      const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
-      b = b0 + f;
-      qt = strip - before - (__shfl(sum, f) - __shfl(cnt, f));
-      break;
+    if (b < 0) {
+      if (fp.splits > 1 && split == 0 && threadIdx.x == 0) fp.heads[h * fp.strips + strip].pieces = 0;
+      return;
     }
-    before += __shfl(sum, 63);
+    b = __builtin_amdgcn_readfirstlane(b);
+    qt = __builtin_amdgcn_readfirstlane(qt);
   }
   JoinHead* head = fp.heads + h * fp.strips + strip;
-  if (b < 0) {
-    if (fp.splits > 1 && split == 0 && threadIdx.x == 0) head->pieces = 0;
-    return;
-  }
-  b = __builtin_amdgcn_readfirstlane(b);
-  qt = __builtin_amdgcn_readfirstlane(qt);
   const Context c = context(a, b);
   const int r0 = qt * kChunkRows, valid = min(kChunkRows, c.m * a.group - r0);
   const auto range = reach(a, c, r0, r0 + valid - 1);
   const typename LineOf<TK, A>::type line(range);
-  const int per = (line.count + fp.splits - 1) / fp.splits;
+  const int per = (line.count + pieces - 1) / pieces;
   const int t0 = line.first + split * per, t1 = min(t0 + per, line.first + line.count);
 
   const auto qr = query_row(a, c, r0 + w * 32 + n);
@@ -246,36 +270,69 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
   const typename L::LaneAt at = L::lane_at();
   // the queries are here: the compiler must not wait for them in the loop
   __builtin_amdgcn_s_waitcnt(0);
-  // codes: a lane's rows of a wave's copies, and the scales of the tile whose
-  // keys, and of that whose values, were asked for last
+  // Codes: copy i of a wave takes R rows, a lane 16 codes of one, within 16 slots
+  // that lie in one block; block numbers as forward_few's, one load for 64 of them.
+  // The scales are of the tile whose keys, and of that whose values, were asked
+  // for last.
   using R = CodeRows<DP>;
   constexpr int kCodeCopies = kCoded ? kCodes / 4096 : 1, kCodeStep = 4 * R::kRowsPerCopy;
-  constexpr int kCodesAt = (kKeys + kValues) * kBytes;
+  constexpr int kCodesAt = (kKeys + kValues) * kBytes, kSixteens = TK / 16;
+  const int sub = lane / R::kChunks, code0 = lane % R::kChunks * 16;
   uint32_t kpair[kCodeCopies] = {}, vpair[kCodeCopies] = {};
-  auto copy_keys = [&](int t, int slot) __attribute__((always_inline)) {
-    const int j0 = line.slot(t);
+  int base = t0, ids = 0;
+  auto numbers = [&](int t) __attribute__((always_inline)) {
     if constexpr (kCoded) {
-      copy_tile<R, TK, 4, true, false>(a.c, kb, vb, b, j0, range, kblocks, a.d, w, l3 + kCodesAt, 0);
+      const int j0 = min(line.slot(t + lane / kSixteens), (range.hi - 1) / TK * TK);
+      return a.c.table[static_cast<int64_t>(b) * a.c.max_blocks + fdiv(a.c.bs, sixteen(range, j0 + 16 * (lane % kSixteens)))];
+    }
+    return 0;
+  };
+  auto copy_codes = [&](int t, const char* from, bool keys) __attribute__((always_inline)) {
+    if constexpr (kCoded) {
+      const int j0 = line.slot(t);
+      const bool table = a.c.table != nullptr;
+      const bool runs = a.c.run >= 16 && (table || max(range.nearest(j0 + TK - 1) | 15, j0 + TK - 1) < a.c.capacity);
+      if (runs && table && t - base >= 64 / kSixteens) {
+        base = t;
+        ids = numbers(t);
+        __builtin_amdgcn_s_waitcnt(0);
+      }
 #pragma unroll
       for (int i = 0; i < kCodeCopies; ++i) {
-        const int row0 = i * kCodeStep + w * R::kRowsPerCopy, j = range.nearest(j0 + row0 + lane / R::kChunks);
-        int32_t block = b;
-        if (a.c.table) block = a.c.run >= 16 && range.inside(j0, TK) ? kblocks.id[row0 / 16] : cache_block(a.c, b, j);
-        kpair[i] = a.scale.p[scale_offset(a.c, a.scale, block, j) + h * a.scale.sh];
+        const int row0 = i * kCodeStep + w * R::kRowsPerCopy;
+        const uint32_t to = l3 + kCodesAt + (keys ? 0 : kCodes) + (i * 4 + w) * 1024;
+        if (runs) {
+          const int j = (range.inside(j0, TK) ? j0 + (row0 & ~15) : sixteen(range, j0 + (row0 & ~15))) + row0 % 16;
+          const int32_t block = table ? __builtin_amdgcn_readlane(ids, (t - base) * kSixteens + row0 / 16) : b;
+          const uint32_t slot = table ? j - fdiv(a.c.bs, j) * a.c.bs.d : j;
+          const int64_t at = block * a.c.sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * static_cast<uint32_t>(a.c.st));
+          if (code0 < a.d) copy16(from + at, sub * static_cast<uint32_t>(a.c.st) + code0, to);
+          if (keys) kpair[i] = a.scale.p[block * a.scale.sb + h * a.scale.sh + slot * a.scale.st + sub * a.scale.st];
+        } else {
+          const int j = range.nearest(j0 + row0 + sub);
+          const int32_t block = cache_block(a.c, b, j);
+          if (keys) kpair[i] = a.scale.p[scale_offset(a.c, a.scale, block, j) + h * a.scale.sh];
+          const char* at = from + cache_offset(a.c, block, j) + code0;
+          __builtin_amdgcn_s_waitcnt(0);
+          if (code0 < a.d) copy16(at, to);
+        }
+        if (!keys) vpair[i] = kpair[i];  // the same tile's, whose keys are here
       }
-    } else {
-      copy_tile<L, TK, 4, true, false>(a.c, kb, vb, b, j0, range, kblocks, a.d, w, l3 + slot * kBytes, 0);
     }
-    vblocks = kblocks;
-    fetch_blocks(a.c, b, line.slot(t + 1), range.hi, kblocks);
+  };
+  auto copy_keys = [&](int t, int slot) __attribute__((always_inline)) {
+    if constexpr (kCoded) {
+      copy_codes(t, kb, true);
+    } else {
+      copy_tile<L, TK, 4, true, false>(a.c, kb, vb, b, line.slot(t), range, kblocks, a.d, w, l3 + slot * kBytes, 0);
+      vblocks = kblocks;
+      fetch_blocks(a.c, b, line.slot(t + 1), range.hi, kblocks);
+    }
   };
   auto copy_values = [&](int t, int slot) __attribute__((always_inline)) {
-    if constexpr (kCoded) {
-      copy_tile<R, TK, 4, false, true>(a.c, kb, vb, b, line.slot(t), range, vblocks, a.d, w, 0,
-                                       l3 + kCodesAt + kCodes);
-#pragma unroll
-      for (int i = 0; i < kCodeCopies; ++i) vpair[i] = kpair[i];  // the same tile's
-    } else
+    if constexpr (kCoded)
+      copy_codes(t, vb, false);
+    else
       copy_tile<L, TK, 4, false, true>(a.c, kb, vb, b, line.slot(t), range, vblocks, a.d, w, 0,
                                        l3 + (kKeys + slot) * kBytes);
   };
@@ -294,10 +351,15 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
     }
   };
   if (t0 < t1) {
-    fetch_blocks(a.c, b, line.slot(t0), range.hi, kblocks);
+    if constexpr (kCoded) {
+      if (a.c.table && a.c.run >= 16) ids = numbers(t0);
+      __builtin_amdgcn_s_waitcnt(0);
+    } else {
+      fetch_blocks(a.c, b, line.slot(t0), range.hi, kblocks);
+    }
     copy_keys(t0, 0);
     if constexpr (kCoded) {
-      vm_wait<0>();
+      __builtin_amdgcn_s_waitcnt(0);
       convert(true, lds);
     }
 #pragma unroll
@@ -318,12 +380,22 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
   const float c2 = CAP == Cap::none ? a.scale2 : 1.f;
   int kslot = 0, vslot = 0;  // of tile t
   auto after = [](int slot, int n, int by) { return slot + by >= n ? slot + by - n : slot + by; };
+  // tiles that all waves' middle loops have, the first one and its turn apart
+  int steady0 = 0, steady1 = 0;
+  if constexpr (kCoded) {
+    steady0 = max(t0, max(line.before, (range.alo + TK - 1) / TK - line.skip));
+    steady1 = min(t1, line.until(range.ahi));
+  }
   auto arrive = [&](int t) __attribute__((always_inline)) {
     // tile t's values and tile t + 1's keys have landed, those of kDepth - 1
     // more tiles may be in flight, and every wave is done with tile t - 1
     if constexpr (kCoded) {
-      vm_wait<0>();
-      tile_barrier();  // the rows that are written are free
+      __builtin_amdgcn_s_waitcnt(0);  // the wave's codes and scales are here
+      // Rows that are written have to be free: with three tiles of keys they are.
+      // With two, those of tile t - 1 may still be read by waves that have just
+      // entered a loop with it, or are at an edge; not by those that went on in
+      // the middle one.
+      if (kKeys == 2 && !(t - 1 > steady0 && t - 1 < steady1)) tile_barrier();
       if (t + 1 < t1) convert(true, lds + after(kslot, kKeys, 1) * kBytes);
       convert(false, lds + (kKeys + vslot) * kBytes);
       if (t + 1 < t1) copy_values(t + 1, 0);
@@ -427,15 +499,16 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
     next_slots();
   }
 
-  const int unit = h * fp.strips + strip;
-  float* part = fp.pieces + (static_cast<size_t>(unit) * fp.splits + split) * piece_floats(kChunkRows, DP);
+  // a view's unit of one piece needs no join
+  const bool whole = kView ? pieces == 1 : fp.splits == 1;
+  float* part = fp.pieces + (static_cast<size_t>(first) + split * step) * piece_floats(kChunkRows, DP);
   if (fp.splits > 1 && split == 0 && threadIdx.x == 0) {
     int from, to;
     seeing(a, c, r0, from, to);
-    *head = JoinHead{fp.splits, valid, c.q0, r0, h, unit * fp.splits, from, to, b};
+    *head = JoinHead{whole ? 0 : pieces, valid, c.q0, r0, h, first, from, to, b, step};
   }
   const int r = w * 32 + n;
-  if (fp.splits == 1) {
+  if (whole) {
     if (r < valid) store_out<T, NB>(a, qr, h, acc, st);
   } else {
     const float l = half_sum(st.l);
@@ -466,7 +539,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
       own = careful_row<T, DP>(a, b, h, qu, u.lo, u.hi, (t1 - t0) * NS, slot, sm, o);
     if (!own) continue;
     const int pr = w * 32 + r;
-    if (fp.splits > 1) {
+    if (!whole) {
       if (lane == 0) reinterpret_cast<float2*>(part)[pr] = float2{sm.m2, sm.l};
 #pragma unroll
       for (int i = 0; i < DP / 64; ++i)
@@ -805,7 +878,7 @@ __global__ void __launch_bounds__(256) forward_join(A a, ForwardPlan fp) {
   const size_t size = piece_floats(unit_rows, DP);
   // decode: piece 0 is slot 1 of its workgroup, the others slot 0 of the next ones
   auto piece = [&](int p) __attribute__((always_inline)) {
-    const size_t at = fp.decode ? (p == 0 ? hd.first : hd.first - 1 + 2 * static_cast<size_t>(p)) : hd.first + p;
+    const size_t at = fp.decode ? (p == 0 ? hd.first : hd.first - 1 + 2 * static_cast<size_t>(p)) : hd.first + static_cast<size_t>(p) * hd.step;
     return fp.pieces + at * size;
   };
   // the grid has the rows that the caller's bound on new tokens gives

@@ -2,6 +2,7 @@
 // before and in a window, and tiles of caches of 8 bits.
 #pragma once
 
+#include "attn_forward.h"
 #include "attn_tile.h"
 #include "attn_view.h"
 
@@ -70,6 +71,13 @@ __device__ __forceinline__ ViewReach reach(const AttnView& a, const Context& c, 
   return r;
 }
 
+// The 16 slots that are copied for slots j .. j + 15: themselves where the unit
+// sees any of them, else those around the nearest that it does.
+__device__ __forceinline__ int sixteen(const ViewReach& r, int j) {
+  const bool seen = j < r.sink || (j + 16 > r.lo && j < r.hi && r.lo < r.hi);
+  return seen ? j : r.nearest(j) & ~15;
+}
+
 // A unit's tiles: those of the sinks that lie before the window, then its own.
 template <int TK>
 struct ViewLine {
@@ -98,6 +106,89 @@ template <int TK>
 struct LineOf<TK, AttnView> {
   using type = ViewLine<TK>;
 };
+
+// A workgroup's piece of the chunk kernel's work: strips (128 query rows of a KV
+// head) are cut into pieces of about the same number of tiles, as many as there
+// are workgroups beyond one a strip, by every context's length.  Equal numbers of
+// pieces for all took the longest context's time: trees of 64 nodes, 8 contexts
+// of 800 to 8k slots, heads 28 / 4 x 128, 120 us.  b < 0: nothing to do.
+struct ChunkShare {
+  int strips;         // of a head, all contexts'
+  int h, b, qt, strip;
+  int piece, pieces;  // of the strip
+  int first, step;    // index of its first piece, and from one to the next
+};
+
+template <int TK>
+__device__ __forceinline__ ChunkShare chunk_share(const AttnView& a, bool split) {
+  const int lane = threadIdx.x % 64;
+  int cnt = 0, tiles = 0;  // strips of the lane's context, and their tiles
+  auto look = [&](int b0) __attribute__((always_inline)) {
+    cnt = tiles = 0;
+    if (b0 + lane < a.batch) {
+      const Context c = context(a, b0 + lane);
+      const int rows = c.m * a.group;
+      cnt = (rows + kChunkRows - 1) / kChunkRows;
+      if (split && rows > 0) tiles = ViewLine<TK>(reach(a, c, 0, rows - 1)).count;
+    }
+  };
+  auto sum_of = [&](int64_t x) __attribute__((always_inline)) {
+    const int64_t y = wave_sum(x);
+    return static_cast<int64_t>(static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<int>(y >> 32), 63)) << 32 |
+                                static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(y), 63)));
+  };
+  ChunkShare s{};
+  s.b = -1;
+  int64_t all = 0, strips = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    look(b0);
+    all += sum_of(static_cast<int64_t>(cnt) * tiles);
+    strips += sum_of(cnt);
+  }
+  s.strips = static_cast<int>(strips);
+  // sum of ceil(tiles / per) <= strips + all / per
+  const int64_t more = static_cast<int64_t>(gridDim.x) - strips * a.hkv;
+  const int64_t per = split && more > 0 ? max<int64_t>((all * a.hkv + more - 1) / more, 1) : INT32_MAX;
+  auto pieces_of = [&](int t) __attribute__((always_inline)) {
+    return static_cast<int>(max<int64_t>((t + per - 1) / per, 1));
+  };
+  int64_t groups = strips;  // workgroups of a head
+  if (split) {
+    groups = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+      if (a.batch > 64) look(b0);
+      groups += sum_of(static_cast<int64_t>(cnt) * pieces_of(tiles));
+    }
+  }
+  // consecutive workgroups of an XCD share a head's cache, and a context's tiles;
+  // those with nothing to do are the last ones, so that no XCD has more than others
+  const int used = static_cast<int>(groups * a.hkv);
+  if (static_cast<int>(blockIdx.x) >= used) return s;
+  const int id = xcd_remap(blockIdx.x, used);
+  s.h = static_cast<int>(id / groups);
+  int64_t into = id - s.h * groups, before = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    if (a.batch > 64) look(b0);
+    const int n = pieces_of(tiles);
+    const int64_t mine = static_cast<int64_t>(cnt) * n, upto = wave_sum(mine), strips_upto = wave_sum(cnt);
+    const uint64_t past = __ballot(upto > into);
+    if (past) {
+      const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      const int in_context = static_cast<int>(into - (__shfl(upto, f) - __shfl(mine, f))), strips_b = __shfl(cnt, f);
+      s.b = b0 + f;
+      s.pieces = __shfl(n, f);
+      s.piece = in_context / strips_b;
+      s.qt = strips_b - 1 - in_context % strips_b;  // later strips, which see more, first
+      s.strip = static_cast<int>(before + __shfl(strips_upto, f)) - strips_b + s.qt;
+      s.first = id - s.piece * strips_b;
+      s.step = strips_b;
+      return s;
+    }
+    into -= __shfl(upto, 63);
+    before += __shfl(strips_upto, 63);
+  }
+  return s;
+}
 
 // What a lane's query sees of the slots of its 16 scores: bit 8 (v / 4) + v % 4
 // stands for register v.
