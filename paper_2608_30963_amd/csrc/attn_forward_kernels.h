@@ -287,32 +287,63 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
     }
     return 0;
   };
+  // where the last asked keys' rows begin, and so their values'
+  int64_t code_at[kCodeCopies] = {};
+  bool code_runs = false;
   auto copy_codes = [&](int t, const char* from, bool keys) __attribute__((always_inline)) {
     if constexpr (kCoded) {
-      const int j0 = line.slot(t);
       const bool table = a.c.table != nullptr;
-      const bool runs = a.c.run >= 16 && (table || max(range.nearest(j0 + TK - 1) | 15, j0 + TK - 1) < a.c.capacity);
-      if (runs && table && t - base >= 64 / kSixteens) {
-        base = t;
-        ids = numbers(t);
-        __builtin_amdgcn_s_waitcnt(0);
+      if (keys) {
+        const int j0 = line.slot(t);
+        const bool inside = range.inside(j0, TK);
+        code_runs = a.c.run >= 16 && (table || inside || max(range.nearest(j0 + TK - 1) | 15, j0 + TK - 1) < a.c.capacity);
+        if (code_runs && table && t - base >= 64 / kSixteens) {
+          base = t;
+          ids = numbers(t);
+          __builtin_amdgcn_s_waitcnt(0);
+        }
+        const int64_t st = static_cast<uint32_t>(a.c.st);
+        int64_t pair_at[kCodeCopies];
+        if (inside && a.c.run >= TK) {
+          const int32_t block = table ? __builtin_amdgcn_readlane(ids, (t - base) * kSixteens) : b;
+          const int slot = (table ? j0 - fdiv(a.c.bs, j0) * static_cast<int>(a.c.bs.d) : j0) + w * R::kRowsPerCopy;
+          const int64_t at = block * a.c.sb + slot * st, pair = block * a.scale.sb + slot * a.scale.st;
+#pragma unroll
+          for (int i = 0; i < kCodeCopies; ++i) {
+            code_at[i] = at + i * kCodeStep * st;
+            pair_at[i] = pair + (i * kCodeStep + sub) * a.scale.st;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kCodeCopies; ++i) {
+            const int row0 = i * kCodeStep + w * R::kRowsPerCopy;
+            int j = range.nearest(j0 + row0 + sub);
+            int32_t block = b;
+            if (code_runs) {
+              j = (inside ? j0 + (row0 & ~15) : sixteen(range, j0 + (row0 & ~15))) + row0 % 16;
+              if (table) block = __builtin_amdgcn_readlane(ids, (t - base) * kSixteens + row0 / 16);
+              const int slot = table ? j - fdiv(a.c.bs, j) * static_cast<int>(a.c.bs.d) : j;
+              code_at[i] = block * a.c.sb + slot * st;
+              j += sub;
+            } else {
+              block = cache_block(a.c, b, j);
+              __builtin_amdgcn_s_waitcnt(0);
+            }
+            pair_at[i] = scale_offset(a.c, a.scale, block, j);
+          }
+        }
+        // loaded here, not where paths part: where they meet the compiler would wait
+#pragma unroll
+        for (int i = 0; i < kCodeCopies; ++i) kpair[i] = a.scale.p[pair_at[i] + h * a.scale.sh];
       }
 #pragma unroll
       for (int i = 0; i < kCodeCopies; ++i) {
-        const int row0 = i * kCodeStep + w * R::kRowsPerCopy;
         const uint32_t to = l3 + kCodesAt + (keys ? 0 : kCodes) + (i * 4 + w) * 1024;
-        if (runs) {
-          const int j = (range.inside(j0, TK) ? j0 + (row0 & ~15) : sixteen(range, j0 + (row0 & ~15))) + row0 % 16;
-          const int32_t block = table ? __builtin_amdgcn_readlane(ids, (t - base) * kSixteens + row0 / 16) : b;
-          const uint32_t slot = table ? j - fdiv(a.c.bs, j) * a.c.bs.d : j;
-          const int64_t at = block * a.c.sb + static_cast<int64_t>(static_cast<uint64_t>(slot) * static_cast<uint32_t>(a.c.st));
-          if (code0 < a.d) copy16(from + at, sub * static_cast<uint32_t>(a.c.st) + code0, to);
-          if (keys) kpair[i] = a.scale.p[block * a.scale.sb + h * a.scale.sh + slot * a.scale.st + sub * a.scale.st];
+        if (code_runs) {
+          if (code0 < a.d) copy16(from + code_at[i], sub * static_cast<uint32_t>(a.c.st) + code0, to);
         } else {
-          const int j = range.nearest(j0 + row0 + sub);
-          const int32_t block = cache_block(a.c, b, j);
-          if (keys) kpair[i] = a.scale.p[scale_offset(a.c, a.scale, block, j) + h * a.scale.sh];
-          const char* at = from + cache_offset(a.c, block, j) + code0;
+          const int j = range.nearest(line.slot(t) + i * kCodeStep + w * R::kRowsPerCopy + sub);
+          const char* at = from + cache_offset(a.c, cache_block(a.c, b, j), j) + code0;
           __builtin_amdgcn_s_waitcnt(0);
           if (code0 < a.d) copy16(at, to);
         }
