@@ -9,26 +9,27 @@ namespace {
 
 constexpr int kChunk = 128;  // slots of a workgroup's turn
 
-// 16 numbers of a row.
+// The numbers of a lane, 16 bytes of a row.
 template <typename T>
-struct Numbers {
-  static constexpr int kPieces = sizeof(T);  // of 16 bytes
-  uint4 x[kPieces];
+struct Piece {
+  static constexpr int n = 16 / sizeof(T);
+  T x[n];
 };
 
-template <typename T>
-__device__ __forceinline__ void widen(const Numbers<T>& in, float (&x)[16]) {
-  const T* p = reinterpret_cast<const T*>(in.x);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = load_f32<T>(p + i);
-}
+// As many codes.
+template <int N>
+struct Codes {
+  uint32_t x[N / 4];
+};
 
-// A slot's key and value rows to codes, or back.  G lanes a slot, 16 numbers of
-// each row a lane; lanes past head_dim stay idle.
+// A slot's key and value rows to codes, or back: G lanes a slot, 16 bytes of plain
+// numbers each, so that a wave reads and writes whole lines; lanes past head_dim
+// stay idle.  A workgroup takes kChunk slots of a head, kAhead rows a lane at a time.
 template <typename T, typename C, int G, bool PACK>
 __global__ void __launch_bounds__(256) convert_kernel(PackArgs a, int chunks) {
+  constexpr int N = Piece<T>::n, kSlots = 256 / G, kTurns = kChunk / kSlots, kAhead = kTurns < 4 ? kTurns : 4;
   const int lane = threadIdx.x % G, sub = threadIdx.x / G;
-  const bool active = lane * 16 < a.d;
+  const bool active = lane * N < a.d;
   const int64_t sets = int64_t(a.layers) * a.batch * a.heads;
   for (int64_t id = blockIdx.x; id < sets * chunks; id += gridDim.x) {
     const int64_t set = id / chunks;
@@ -39,70 +40,92 @@ __global__ void __launch_bounds__(256) convert_kernel(PackArgs a, int chunks) {
     const int64_t l = lb / a.batch;
     const int n = min(min(max(a.tokens[b], 0), a.plain.capacity), a.coded.capacity);
     const int j1 = min(n, j0 + kChunk);
-    for (int j = j0 + sub; j - sub < j1; j += 256 / G) {
-      const bool there = j < j1;
-      const int jc = min(j, j1 - 1);
-      const int32_t pb = cache_block(a.plain, b, jc), cb = cache_block(a.coded, b, jc);
-      const int64_t pat = cache_offset(a.plain, pb, jc) + l * a.plain.sl + h * a.plain.sh;
-      const int64_t cat = cache_offset(a.coded, cb, jc) + l * a.coded.sl + h * a.coded.sh;
-      const int slot = a.coded.table ? jc - fdiv(a.coded.bs, jc) * static_cast<int>(a.coded.bs.d) : jc;
-      uint32_t* pair = a.scale.p + l * a.scale.sl + cb * a.scale.sb + h * a.scale.sh + slot * a.scale.st;
+#pragma unroll 1
+    for (int jt = j0; jt < j1; jt += kAhead * kSlots) {
+      T* plain[kAhead][2];
+      char* coded[kAhead][2];
+      uint32_t* pair[kAhead];
+      bool there[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int j = jt + i * kSlots + sub, jc = min(j, j1 - 1);
+        there[i] = j < j1;
+        const int32_t pb = cache_block(a.plain, b, jc), cb = cache_block(a.coded, b, jc);
+        const int64_t pat = cache_offset(a.plain, pb, jc) + l * a.plain.sl + h * a.plain.sh + lane * N;
+        const int64_t cat = cache_offset(a.coded, cb, jc) + l * a.coded.sl + h * a.coded.sh + lane * N;
+        plain[i][0] = reinterpret_cast<T*>(a.plain.k) + pat;
+        plain[i][1] = reinterpret_cast<T*>(a.plain.v) + pat;
+        coded[i][0] = a.coded.k + cat;
+        coded[i][1] = a.coded.v + cat;
+        pair[i] = a.scale.p + l * a.scale.sl + h * a.scale.sh + scale_offset(a.coded, a.scale, cb, jc);
+      }
       if constexpr (PACK) {
-        uint32_t scales = 0;
+        Piece<T> in[kAhead][2] = {};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          Numbers<T> in{};
-          if (active) in = *reinterpret_cast<const Numbers<T>*>((e ? a.plain.v : a.plain.k) + (pat + lane * 16) * int64_t(sizeof(T)));
-          float x[16];
-          widen(in, x);
-          float top = 0.f;
-          bool odd = false;
+        for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            odd |= (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u;
-            x[i] = fminf(fmaxf(x[i], -0x1p127f), 0x1p127f);
-            top = fmaxf(top, fabsf(x[i]));
+          for (int e = 0; e < 2; ++e)
+            if (active && there[i]) in[i][e] = *reinterpret_cast<const Piece<T>*>(plain[i][e]);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          uint32_t scales = 0;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x[N];
+            uint32_t top = 0;  // bits of the largest magnitude: an infinity's or NaN's are the largest
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+              x[k] = load_f32<T>(&in[i][e].x[k]);
+              top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+            }
+#pragma unroll
+            for (int k = 1; k < G; k <<= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), k)));
+            const bool odd = top >= 0x7f800000u;
+            if (__builtin_expect(top > 0x7f000000u, 0)) {
+#pragma unroll
+              for (int k = 0; k < N; ++k) x[k] = odd ? 0.f : fminf(fmaxf(x[k], -0x1p127f), 0x1p127f);
+              top = 0x7f000000u;
+            }
+            const int ex = scale_exponent<C>(__uint_as_float(top));
+            const float inv = power_of_two(-ex);
+            Codes<N> out;
+#pragma unroll
+            for (int k = 0; k < N / 4; ++k) {
+              float y[4];
+#pragma unroll
+              for (int z = 0; z < 4; ++z) y[z] = x[4 * k + z] * inv;
+              out.x[k] = encode4<C>(y);
+            }
+            scales |= (odd ? 0x7fc0u : __float_as_uint(power_of_two(ex)) >> 16) << 16 * e;
+            if (active && there[i]) *reinterpret_cast<Codes<N>*>(coded[i][e]) = out;
           }
-          int odds = odd;
-#pragma unroll
-          for (int i = 1; i < G; i <<= 1) {
-            top = fmaxf(top, __shfl_xor(top, i));
-            odds |= __shfl_xor(odds, i);
-          }
-          const int ex = scale_exponent<C>(top);
-          const float inv = odds ? 0.f : power_of_two(-ex);
-          uint32_t u[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float y[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = odds ? 0.f : x[4 * i + k] * inv;
-            u[i] = encode4<C>(y);
-          }
-          scales |= (odds ? 0x7fc0u : __float_as_uint(power_of_two(ex)) >> 16) << 16 * e;
-          if (active && there)
-            *reinterpret_cast<uint4*>((e ? a.coded.v : a.coded.k) + cat + lane * 16) = uint4{u[0], u[1], u[2], u[3]};
+          if (lane == 0 && there[i]) *pair[i] = scales;
         }
-        if (lane == 0 && there) *pair = scales;
       } else {
-        if (!there || !active) continue;
-        const uint32_t scales = *pair;
+        Codes<N> in[kAhead][2] = {};
+        uint32_t scales[kAhead] = {};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint4 in = *reinterpret_cast<const uint4*>((e ? a.coded.v : a.coded.k) + cat + lane * 16);
-          const uint32_t u[4] = {in.x, in.y, in.z, in.w};
-          const float f = e ? value_scale(scales) : key_scale(scales);
-          Numbers<T> out;
-          T* o = reinterpret_cast<T*>(out.x);
+        for (int i = 0; i < kAhead; ++i) {
+          if (!active || !there[i]) continue;
+          scales[i] = *pair[i];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float y[4];
-            decode4<C>(u[i], f, y);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) o[4 * i + k] = store_cvt<T>(y[k]);
-          }
-          *reinterpret_cast<Numbers<T>*>((e ? a.plain.v : a.plain.k) + (pat + lane * 16) * int64_t(sizeof(T))) = out;
+          for (int e = 0; e < 2; ++e) in[i][e] = *reinterpret_cast<const Codes<N>*>(coded[i][e]);
         }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float f = e ? value_scale(scales[i]) : key_scale(scales[i]);
+            Piece<T> out;
+#pragma unroll
+            for (int k = 0; k < N / 4; ++k) {
+              float y[4];
+              decode4<C>(in[i][e].x[k], f, y);
+#pragma unroll
+              for (int z = 0; z < 4; ++z) out.x[4 * k + z] = store_cvt<T>(y[z]);
+            }
+            if (active && there[i]) *reinterpret_cast<Piece<T>*>(plain[i][e]) = out;
+          }
       }
     }
   }
@@ -119,9 +142,10 @@ hipError_t run(const PackArgs& a, bool pack, int n_cu, hipStream_t st) {
 
 template <typename T, typename C>
 hipError_t by_width(const PackArgs& a, bool pack, int n_cu, hipStream_t st) {
-  return a.d <= 64    ? run<T, C, 4>(a, pack, n_cu, st)
-         : a.d <= 128 ? run<T, C, 8>(a, pack, n_cu, st)
-                      : run<T, C, 16>(a, pack, n_cu, st);
+  constexpr int N = Piece<T>::n;
+  return a.d <= 64    ? run<T, C, 64 / N>(a, pack, n_cu, st)
+         : a.d <= 128 ? run<T, C, 128 / N>(a, pack, n_cu, st)
+                      : run<T, C, 256 / N>(a, pack, n_cu, st);
 }
 
 }  // namespace

@@ -234,6 +234,43 @@ __device__ __forceinline__ int few_steps(const AttnView& a, const Context& c, in
   return max(1, (line.count + Few<S, DP>::kWaves - 1) / Few<S, DP>::kWaves);
 }
 
+// A workgroup's equal range of the line, as line_share's; sums over the lanes, and
+// the divisions of all but the largest calls, in 32 bits.
+template <typename Steps>
+__device__ __forceinline__ Share few_share(const AttnView& a, Steps steps_of) {
+  const int lane = threadIdx.x % 64;
+  int64_t line = 0;
+  int mine = 0, upto = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    mine = b0 + lane < a.batch ? steps_of(b0 + lane) : 0;
+    upto = a.batch == 1 ? __builtin_amdgcn_readfirstlane(mine) : lanes_upto(mine);
+    line += __builtin_amdgcn_readlane(upto, 63);
+  }
+  Share sh{};
+  const int64_t whole = line * a.hkv;
+  const bool small = whole <= INT32_MAX;
+  sh.per = small ? (static_cast<uint32_t>(whole) + gridDim.x - 1) / gridDim.x : (whole + gridDim.x - 1) / gridDim.x;
+  sh.s0 = min<int64_t>(whole, blockIdx.x * sh.per);
+  sh.s1 = min(whole, sh.s0 + sh.per);
+  if (sh.s0 >= sh.s1) return sh;
+  sh.h = small ? static_cast<uint32_t>(sh.s0) / static_cast<uint32_t>(line) : static_cast<int>(sh.s0 / line);
+  int64_t into = sh.s0 - sh.h * line;
+  for (int b0 = 0;; b0 += 64) {
+    if (a.batch > 64) {
+      mine = b0 + lane < a.batch ? steps_of(b0 + lane) : 0;
+      upto = lanes_upto(mine);
+    }
+    const uint64_t past = __ballot(upto > into);
+    if (past) {
+      const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      sh.b = b0 + f;
+      sh.step = static_cast<int>(into) - (__builtin_amdgcn_readlane(upto, f) - __builtin_amdgcn_readlane(mine, f));
+      return sh;
+    }
+    into -= __builtin_amdgcn_readlane(upto, 63);
+  }
+}
+
 template <typename S, int DP, Cap CAP>
 __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroups)) forward_few(AttnView a, ForwardPlan fp) {
   using L = FewTile<S, DP>;
@@ -247,11 +284,11 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroup
 
   // a unit is one step of the line where units are not split
   const bool whole = fp.splits == 1;
-  const Share share = line_share(a, [&](int b) {
+  const Share share = few_share(a, [&](int b) {
     const Context c = context(a, b);
     const int qts = (c.m * a.group + kFewRows - 1) / kFewRows;
-    if (whole) return static_cast<int64_t>(qts);
-    int64_t s = 0;
+    if (whole) return qts;
+    int s = 0;
     for (int qt = 0; qt < qts; ++qt) s += few_steps<S, DP>(a, c, qt);
     return s;
   });

@@ -10,6 +10,28 @@ using namespace kvx;
 
 namespace {
 
+// cos and sin of r revolutions, |r| <= 1/2: by the nearest quarter and Taylor's
+// series of the rest, at most pi / 4 (up to the 11th and 12th power: 7e-12).
+__device__ __forceinline__ void turn64(double r, double& c, double& s) {
+  const double q = rint(4.0 * r), y = __builtin_fma(4.0, r, -q) * 1.5707963267948966, z = y * y;
+  double a = -1.0 / 39916800, b = 1.0 / 479001600;
+  a = __builtin_fma(a, z, 1.0 / 362880);
+  b = __builtin_fma(b, z, -1.0 / 3628800);
+  a = __builtin_fma(a, z, -1.0 / 5040);
+  b = __builtin_fma(b, z, 1.0 / 40320);
+  a = __builtin_fma(a, z, 1.0 / 120);
+  b = __builtin_fma(b, z, -1.0 / 720);
+  a = __builtin_fma(a, z, -1.0 / 6);
+  b = __builtin_fma(b, z, 1.0 / 24);
+  b = __builtin_fma(b, z, -0.5);
+  a = __builtin_fma(a * z, y, y);
+  b = __builtin_fma(b, z, 1.0);
+  const int k = static_cast<int>(q) & 3;
+  const double u = k & 1 ? b : a, v = k & 1 ? a : b;  // sin, cos up to their signs
+  s = k & 2 ? -u : u;
+  c = (k + 1) & 2 ? -v : v;
+}
+
 struct Append8Args {
   AttnArgs a;  // c: the codes
   ScaleArgs scale;
@@ -41,7 +63,7 @@ __global__ void __launch_bounds__(256) append8_kernel(Append8Args g, int heads_s
     const int p = a.pos ? a.pos[g.axis[e] * static_cast<int64_t>(a.rows) + row] : slot;
     double r = static_cast<double>(p) * g.freq[e];
     r -= rint(r);
-    sincospi(2.0 * r, &sn[i], &cs[i]);
+    turn64(r, cs[i], sn[i]);
   }
   const bool stored = slot >= 0 && slot < a.c.capacity && row < c.q0 + c.m;
   const int32_t block = stored ? cache_block(a.c, b, slot) : 0;

@@ -25,14 +25,14 @@ __global__ void __launch_bounds__(256) tree_kernel(TreeArgs a) {
   __syncthreads();
   for (int i = threadIdx.x; i < m; i += 256) {
     const int64_t row = static_cast<int64_t>(q0) + i;
+    // how far the path leads is known before it is walked only for a window's sinks
     int depth = 0;
-    if (i < nodes)
+    if (a.window > 0 && i < nodes)
       for (int k = up[i]; k >= 0; k = up[k]) ++depth;
     uint32_t* mask = a.mask + row * a.words;
-    int word = a.words - 1;
+    int word = a.words - 1, before = 0;
     uint32_t bits = 0;
-    int k = i < nodes ? i : -1;
-    for (int before = 0; k >= 0; ++before, k = up[k]) {
+    for (int k = i < nodes ? i : -1; k >= 0; ++before, k = up[k]) {
       while (word > k >> 5) {
         mask[word--] = bits;
         bits = 0;
@@ -40,6 +40,7 @@ __global__ void __launch_bounds__(256) tree_kernel(TreeArgs a) {
       if (a.window == 0 || before < a.window || p0 + depth - before < a.sink) bits |= 1u << (k & 31);
     }
     for (; word >= 0; --word, bits = 0) mask[word] = bits;
+    depth = max(before - 1, 0);
     if (a.depth) a.depth[row] = depth;
     if (a.pos) {
       const int pos = p0 + depth + (a.shift ? a.shift[b] : 0);

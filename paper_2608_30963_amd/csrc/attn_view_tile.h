@@ -119,6 +119,17 @@ struct ChunkShare {
   int first, step;    // index of its first piece, and from one to the next
 };
 
+// Inclusive sum over a wave's lanes.
+__device__ __forceinline__ int lanes_upto(int x) {
+  const int lane = threadIdx.x % 64;
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) {
+    const int y = __shfl_up(x, i);
+    if (lane >= i) x += y;
+  }
+  return x;
+}
+
 template <int TK>
 __device__ __forceinline__ ChunkShare chunk_share(const AttnView& a, bool split) {
   const int lane = threadIdx.x % 64;
@@ -132,60 +143,73 @@ __device__ __forceinline__ ChunkShare chunk_share(const AttnView& a, bool split)
       if (split && rows > 0) tiles = ViewLine<TK>(reach(a, c, 0, rows - 1)).count;
     }
   };
-  auto sum_of = [&](int64_t x) __attribute__((always_inline)) {
-    const int64_t y = wave_sum(x);
-    return static_cast<int64_t>(static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<int>(y >> 32), 63)) << 32 |
-                                static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(y), 63)));
-  };
   ChunkShare s{};
   s.b = -1;
-  int64_t all = 0, strips = 0;
+  // tiles of all strips, not less than they are: 64 bits' worth in fp32
+  float all = 0.f;
+  int strips = 0, strips_upto = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     look(b0);
-    all += sum_of(static_cast<int64_t>(cnt) * tiles);
-    strips += sum_of(cnt);
+    strips_upto = lanes_upto(cnt);
+    strips += __builtin_amdgcn_readlane(strips_upto, 63);
+    if (split) {
+      float x = static_cast<float>(cnt) * static_cast<float>(tiles);
+#pragma unroll
+      for (int i = 32; i; i >>= 1) x += __shfl_xor(x, i);
+      all += x;
+    }
   }
-  s.strips = static_cast<int>(strips);
-  // sum of ceil(tiles / per) <= strips + all / per
-  const int64_t more = static_cast<int64_t>(gridDim.x) - strips * a.hkv;
-  const int64_t per = split && more > 0 ? max<int64_t>((all * a.hkv + more - 1) / more, 1) : INT32_MAX;
-  auto pieces_of = [&](int t) __attribute__((always_inline)) {
-    return static_cast<int>(max<int64_t>((t + per - 1) / per, 1));
-  };
-  int64_t groups = strips;  // workgroups of a head
-  if (split) {
-    groups = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 64) {
-      if (a.batch > 64) look(b0);
-      groups += sum_of(static_cast<int64_t>(cnt) * pieces_of(tiles));
+  s.strips = strips;
+  int per = INT32_MAX, groups = strips, upto = strips_upto;  // groups: workgroups of a head
+  auto pieces_of = [&](int t) __attribute__((always_inline)) { return max(1, (t - 1) / per + 1); };
+  const int more = static_cast<int>(gridDim.x) - strips * a.hkv;
+  if (split && more > 0) {
+    // the least tiles a piece that the grid may have room for, somewhat more, and
+    // what it has room for: sum of ceil(tiles / per) <= strips + all / per
+    all *= a.hkv * 1.0001f;
+    for (int turn = 0; turn < 3; ++turn) {
+      const float share = turn < 2 ? all / gridDim.x * (turn ? 1.15f : 1.f) : all / more;
+      per = __builtin_amdgcn_readfirstlane(static_cast<int>(min(share + 1.f, 1e9f)));
+      groups = 0;
+      for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        if (a.batch > 64) look(b0);
+        upto = lanes_upto(cnt * pieces_of(tiles));
+        groups += __builtin_amdgcn_readlane(upto, 63);
+      }
+      if (groups * a.hkv <= static_cast<int>(gridDim.x)) break;
     }
   }
   // consecutive workgroups of an XCD share a head's cache, and a context's tiles;
   // those with nothing to do are the last ones, so that no XCD has more than others
-  const int used = static_cast<int>(groups * a.hkv);
+  const int used = groups * a.hkv;
   if (static_cast<int>(blockIdx.x) >= used) return s;
   const int id = xcd_remap(blockIdx.x, used);
-  s.h = static_cast<int>(id / groups);
-  int64_t into = id - s.h * groups, before = 0;
+  s.h = id / groups;
+  int into = id - s.h * groups, before = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    if (a.batch > 64) look(b0);
-    const int n = pieces_of(tiles);
-    const int64_t mine = static_cast<int64_t>(cnt) * n, upto = wave_sum(mine), strips_upto = wave_sum(cnt);
+    int n = pieces_of(tiles);
+    if (a.batch > 64) {
+      look(b0);
+      n = pieces_of(tiles);
+      upto = lanes_upto(cnt * n);
+      strips_upto = lanes_upto(cnt);
+    }
     const uint64_t past = __ballot(upto > into);
     if (past) {
       const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
-      const int in_context = static_cast<int>(into - (__shfl(upto, f) - __shfl(mine, f))), strips_b = __shfl(cnt, f);
+      const int strips_b = __builtin_amdgcn_readlane(cnt, f);
+      s.pieces = __builtin_amdgcn_readlane(n, f);
+      const int in_context = into - (__builtin_amdgcn_readlane(upto, f) - strips_b * s.pieces);
       s.b = b0 + f;
-      s.pieces = __shfl(n, f);
       s.piece = in_context / strips_b;
       s.qt = strips_b - 1 - in_context % strips_b;  // later strips, which see more, first
-      s.strip = static_cast<int>(before + __shfl(strips_upto, f)) - strips_b + s.qt;
+      s.strip = before + __builtin_amdgcn_readlane(strips_upto, f) - strips_b + s.qt;
       s.first = id - s.piece * strips_b;
       s.step = strips_b;
       return s;
     }
-    into -= __shfl(upto, 63);
-    before += __shfl(strips_upto, 63);
+    into -= __builtin_amdgcn_readlane(upto, 63);
+    before += __builtin_amdgcn_readlane(strips_upto, 63);
   }
   return s;
 }
