@@ -22,14 +22,19 @@ struct Codes {
   uint32_t x[N / 4];
 };
 
-// A slot's key and value rows to codes, or back: G lanes a slot, 16 bytes of plain
+// Slots' key and value rows to codes, or back: G lanes a slot, 16 bytes of plain
 // numbers each, so that a wave reads and writes whole lines; lanes past head_dim
-// stay idle.  A workgroup takes kChunk slots of a head, kAhead rows a lane at a time.
+// stay idle.  A workgroup's turn is kChunk slots of a head, a wave's 16 of them,
+// whose rows are all asked for before the first is worked on.  Bound by memory.
+// Where 16 slots from a multiple of 16 on lie in one block of both caches, a
+// wave's rows have one base; else every lane finds its own.
 template <typename T, typename C, int G, bool PACK>
 __global__ void __launch_bounds__(256) convert_kernel(PackArgs a, int chunks) {
-  constexpr int N = Piece<T>::n, kSlots = 256 / G, kTurns = kChunk / kSlots, kAhead = kTurns < 4 ? kTurns : 4;
-  const int lane = threadIdx.x % G, sub = threadIdx.x / G;
-  const bool active = lane * N < a.d;
+  constexpr int N = Piece<T>::n, kRows = 64 / G;              // slots of a wave's instruction
+  constexpr int kAhead = 16 / kRows < 4 ? 16 / kRows : 4;     // of them at a time
+  const int lane = threadIdx.x % 64, piece = lane % G, sub = lane / G;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const bool active = piece * N < a.d, based = a.plain.run >= 16 && a.coded.run >= 16;
   const int64_t sets = int64_t(a.layers) * a.batch * a.heads;
   for (int64_t id = blockIdx.x; id < sets * chunks; id += gridDim.x) {
     const int64_t set = id / chunks;
@@ -39,93 +44,92 @@ __global__ void __launch_bounds__(256) convert_kernel(PackArgs a, int chunks) {
     const int b = static_cast<int>(lb % a.batch);
     const int64_t l = lb / a.batch;
     const int n = min(min(max(a.tokens[b], 0), a.plain.capacity), a.coded.capacity);
-    const int j1 = min(n, j0 + kChunk);
+    const int64_t plain0 = l * a.plain.sl + h * a.plain.sh, coded0 = l * a.coded.sl + h * a.coded.sh;
+    const int64_t pair0 = l * a.scale.sl + h * a.scale.sh;
 #pragma unroll 1
-    for (int jt = j0; jt < j1; jt += kAhead * kSlots) {
-      T* plain[kAhead][2];
-      char* coded[kAhead][2];
-      uint32_t* pair[kAhead];
-      bool there[kAhead];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int j = jt + i * kSlots + sub, jc = min(j, j1 - 1);
-        there[i] = j < j1;
-        const int32_t pb = cache_block(a.plain, b, jc), cb = cache_block(a.coded, b, jc);
-        const int64_t pat = cache_offset(a.plain, pb, jc) + l * a.plain.sl + h * a.plain.sh + lane * N;
-        const int64_t cat = cache_offset(a.coded, cb, jc) + l * a.coded.sl + h * a.coded.sh + lane * N;
-        plain[i][0] = reinterpret_cast<T*>(a.plain.k) + pat;
-        plain[i][1] = reinterpret_cast<T*>(a.plain.v) + pat;
-        coded[i][0] = a.coded.k + cat;
-        coded[i][1] = a.coded.v + cat;
-        pair[i] = a.scale.p + l * a.scale.sl + h * a.scale.sh + scale_offset(a.coded, a.scale, cb, jc);
+    for (int jw = j0 + 16 * w; jw < min(n, j0 + kChunk); jw += 64) {
+      const int rows = min(16, n - jw);
+      int64_t pb = plain0, cb = coded0, sb = pair0;  // of slot jw
+      if (based) {
+        const int32_t p = cache_block(a.plain, b, jw), c = cache_block(a.coded, b, jw);
+        pb += cache_offset(a.plain, p, jw);
+        cb += cache_offset(a.coded, c, jw);
+        sb += scale_offset(a.coded, a.scale, c, jw);
       }
-      if constexpr (PACK) {
-        Piece<T> in[kAhead][2] = {};
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (active && there[i]) in[i][e] = *reinterpret_cast<const Piece<T>*>(plain[i][e]);
+#pragma unroll 1
+      for (int r0 = 0; r0 < rows; r0 += kAhead * kRows) {
+        int64_t pat[kAhead], cat[kAhead], sat[kAhead];
+        bool there[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-          uint32_t scales = 0;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float x[N];
-            uint32_t top = 0;  // bits of the largest magnitude: an infinity's or NaN's are the largest
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-              x[k] = load_f32<T>(&in[i][e].x[k]);
-              top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-            }
-#pragma unroll
-            for (int k = 1; k < G; k <<= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), k)));
-            const bool odd = top >= 0x7f800000u;
-            if (__builtin_expect(top > 0x7f000000u, 0)) {
-#pragma unroll
-              for (int k = 0; k < N; ++k) x[k] = odd ? 0.f : fminf(fmaxf(x[k], -0x1p127f), 0x1p127f);
-              top = 0x7f000000u;
-            }
-            const int ex = scale_exponent<C>(__uint_as_float(top));
-            const float inv = power_of_two(-ex);
-            Codes<N> out;
-#pragma unroll
-            for (int k = 0; k < N / 4; ++k) {
-              float y[4];
-#pragma unroll
-              for (int z = 0; z < 4; ++z) y[z] = x[4 * k + z] * inv;
-              out.x[k] = encode4<C>(y);
-            }
-            scales |= (odd ? 0x7fc0u : __float_as_uint(power_of_two(ex)) >> 16) << 16 * e;
-            if (active && there[i]) *reinterpret_cast<Codes<N>*>(coded[i][e]) = out;
+          const int r = r0 + i * kRows + sub;
+          there[i] = r < rows;
+          if (based) {
+            pat[i] = pb + static_cast<int64_t>(r * static_cast<uint64_t>(a.plain.st));
+            cat[i] = cb + static_cast<int64_t>(r * static_cast<uint64_t>(a.coded.st));
+            sat[i] = sb + r * a.scale.st;
+          } else {
+            const int j = jw + min(r, rows - 1);
+            const int32_t p = cache_block(a.plain, b, j), c = cache_block(a.coded, b, j);
+            pat[i] = plain0 + cache_offset(a.plain, p, j);
+            cat[i] = coded0 + cache_offset(a.coded, c, j);
+            sat[i] = pair0 + scale_offset(a.coded, a.scale, c, j);
           }
-          if (lane == 0 && there[i]) *pair[i] = scales;
+          pat[i] += piece * N;
+          cat[i] += piece * N;
         }
-      } else {
-        Codes<N> in[kAhead][2] = {};
-        uint32_t scales[kAhead] = {};
+        T* const pk[2] = {reinterpret_cast<T*>(a.plain.k), reinterpret_cast<T*>(a.plain.v)};
+        char* const ck[2] = {a.coded.k, a.coded.v};
+        if constexpr (PACK) {
+          Piece<T> in[kAhead][2] = {};
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          if (!active || !there[i]) continue;
-          scales[i] = *pair[i];
+          for (int i = 0; i < kAhead; ++i)
+            if (active && there[i])
 #pragma unroll
-          for (int e = 0; e < 2; ++e) in[i][e] = *reinterpret_cast<const Codes<N>*>(coded[i][e]);
-        }
+              for (int e = 0; e < 2; ++e) in[i][e] = *reinterpret_cast<const Piece<T>*>(pk[e] + pat[i]);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
+          for (int i = 0; i < kAhead; ++i) {
+            uint32_t scales = 0;
+            Codes<N> out[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float f = e ? value_scale(scales[i]) : key_scale(scales[i]);
-            Piece<T> out;
+            for (int e = 0; e < 2; ++e) {
+              float x[N];
 #pragma unroll
-            for (int k = 0; k < N / 4; ++k) {
-              float y[4];
-              decode4<C>(in[i][e].x[k], f, y);
-#pragma unroll
-              for (int z = 0; z < 4; ++z) out.x[4 * k + z] = store_cvt<T>(y[z]);
+              for (int k = 0; k < N; ++k) x[k] = load_f32<T>(&in[i][e].x[k]);
+              scales |= encode_row<C, G>(x, out[e].x) << 16 * e;
             }
-            if (active && there[i]) *reinterpret_cast<Piece<T>*>(plain[i][e]) = out;
+            if (active && there[i]) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) *reinterpret_cast<Codes<N>*>(ck[e] + cat[i]) = out[e];
+              if (piece == 0) a.scale.p[sat[i]] = scales;
+            }
           }
+        } else {
+          Codes<N> in[kAhead][2] = {};
+          uint32_t scales[kAhead] = {};
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i)
+            if (active && there[i]) {
+              scales[i] = a.scale.p[sat[i]];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) in[i][e] = *reinterpret_cast<const Codes<N>*>(ck[e] + cat[i]);
+            }
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float f = e ? value_scale(scales[i]) : key_scale(scales[i]);
+              Piece<T> out;
+              if constexpr (N == 8) {
+                out = __builtin_bit_cast(Piece<T>, code_numbers<C>(in[i][e].x[0], in[i][e].x[1], f));
+              } else {
+                float y[4];
+                decode4<C>(in[i][e].x[0], f, y);
+                out = __builtin_bit_cast(Piece<T>, y);
+              }
+              if (active && there[i]) *reinterpret_cast<Piece<T>*>(pk[e] + pat[i]) = out;
+            }
+        }
       }
     }
   }
@@ -135,7 +139,7 @@ template <typename T, typename C, int G>
 hipError_t run(const PackArgs& a, bool pack, int n_cu, hipStream_t st) {
   const int chunks = (std::min(a.plain.capacity, a.coded.capacity) + kChunk - 1) / kChunk;
   const int64_t items = int64_t(a.layers) * a.batch * a.heads * chunks;
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, 8 * int64_t(n_cu))));
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, 128 * int64_t(n_cu))));
   return pack ? launch_on(convert_kernel<T, C, G, true>, grid, dim3(256), st, a, chunks)
               : launch_on(convert_kernel<T, C, G, false>, grid, dim3(256), st, a, chunks);
 }

@@ -69,17 +69,24 @@ __global__ void __launch_bounds__(256) append8_kernel(Append8Args g, int heads_s
   const int32_t block = stored ? cache_block(a.c, b, slot) : 0;
   const int64_t at = stored ? cache_offset(a.c, block, slot) : 0;
   const int in_block = a.c.table ? slot - fdiv(a.c.bs, max(slot, 0)) * static_cast<int>(a.c.bs.d) : slot;
-  const int nq = g.in[0] ? a.hq : 0, nk = g.in[1] ? a.hkv : 0;
-  for (int h = blockIdx.y; h < nq + 2 * nk; h += heads_step) {
+  const int nq = g.in[0] ? a.hq : 0, nk = g.in[1] ? a.hkv : 0, heads = stored ? nq + 2 * nk : nq;
+  // a head's numbers are asked for before the last one's are worked on
+  auto load = [&](int h, uint4 (&x)[2]) {
     const int which = h < nq ? 0 : h < nq + nk ? 1 : 2;
-    if (which > 0 && !stored) continue;  // all lanes of a row
     const int hh = h - (which == 0 ? 0 : which == 1 ? nq : nq + nk);
     const bf16_t* src = reinterpret_cast<const bf16_t*>(g.in[which]) + row * g.sr[which] + hh * g.sh[which] + e0;
-    uint4 x[2] = {};
-    if (active) {
+    x[0] = x[1] = uint4{0, 0, 0, 0};
+    if (h < heads && active) {
       x[0] = *reinterpret_cast<const uint4*>(src);
       x[1] = *reinterpret_cast<const uint4*>(src + half);
     }
+  };
+  uint4 x[2], next[2];
+  load(blockIdx.y, x);
+  for (int h = blockIdx.y; h < heads; h += heads_step) {  // all lanes of a row
+    load(h + heads_step, next);
+    const int which = h < nq ? 0 : h < nq + nk ? 1 : 2;
+    const int hh = h - (which == 0 ? 0 : which == 1 ? nq : nq + nk);
     const bf16_t* xs = reinterpret_cast<const bf16_t*>(x);
     if (which == 0) {
       bf16_t y[16];
@@ -95,51 +102,32 @@ __global__ void __launch_bounds__(256) append8_kernel(Append8Args g, int heads_s
         *reinterpret_cast<uint4*>(dst) = reinterpret_cast<const uint4*>(y)[0];
         *reinterpret_cast<uint4*>(dst + half) = reinterpret_cast<const uint4*>(y)[1];
       }
-      continue;
-    }
-    float y[16];
+    } else {
+      float y[16];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float u = load_f32<bf16_t>(xs + i), w = load_f32<bf16_t>(xs + 8 + i);
-      y[i] = u;
-      y[8 + i] = w;
-      if (which == 1) {
-        y[i] = static_cast<float>(u * cs[i] - w * sn[i]);
-        y[8 + i] = static_cast<float>(w * cs[i] + u * sn[i]);
+      for (int i = 0; i < 8; ++i) {
+        const float u = load_f32<bf16_t>(xs + i), w = load_f32<bf16_t>(xs + 8 + i);
+        y[i] = u;
+        y[8 + i] = w;
+        if (which == 1) {
+          y[i] = static_cast<float>(u * cs[i] - w * sn[i]);
+          y[8 + i] = static_cast<float>(w * cs[i] + u * sn[i]);
+        }
+      }
+      uint32_t u[4];
+      const uint32_t scale = encode_row<C, G>(y, u);
+      if (active) {
+        char* dst = (which == 1 ? a.c.k : a.c.v) + at + hh * a.c.sh + e0;
+        *reinterpret_cast<uint2*>(dst) = uint2{u[0], u[1]};
+        *reinterpret_cast<uint2*>(dst + half) = uint2{u[2], u[3]};
+      }
+      if (lane == 0) {
+        uint16_t* pair = reinterpret_cast<uint16_t*>(g.scale.p + block * g.scale.sb + hh * g.scale.sh + in_block * g.scale.st);
+        pair[which - 1] = static_cast<uint16_t>(scale);
       }
     }
-    float top = 0.f;
-    int odd = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      odd |= (__float_as_uint(y[i]) & 0x7f800000u) == 0x7f800000u;
-      y[i] = fminf(fmaxf(y[i], -0x1p127f), 0x1p127f);
-      top = fmaxf(top, fabsf(y[i]));
-    }
-#pragma unroll
-    for (int i = 1; i < G; i <<= 1) {
-      top = fmaxf(top, __shfl_xor(top, i));
-      odd |= __shfl_xor(odd, i);
-    }
-    const int ex = scale_exponent<C>(top);
-    const float inv = power_of_two(-ex);
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float z[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) z[k] = odd ? 0.f : y[4 * i + k] * inv;
-      u[i] = encode4<C>(z);
-    }
-    if (active) {
-      char* dst = (which == 1 ? a.c.k : a.c.v) + at + hh * a.c.sh + e0;
-      *reinterpret_cast<uint2*>(dst) = uint2{u[0], u[1]};
-      *reinterpret_cast<uint2*>(dst + half) = uint2{u[2], u[3]};
-    }
-    if (lane == 0) {
-      uint16_t* pair = reinterpret_cast<uint16_t*>(g.scale.p + block * g.scale.sb + hh * g.scale.sh + in_block * g.scale.st);
-      pair[which - 1] = odd ? 0x7fc0 : static_cast<uint16_t>(__float_as_uint(power_of_two(ex)) >> 16);
-    }
+    x[0] = next[0];
+    x[1] = next[1];
   }
 }
 

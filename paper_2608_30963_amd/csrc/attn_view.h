@@ -111,14 +111,16 @@ __device__ __forceinline__ int scale_exponent(float top) {
 
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
 
-// Codes of four numbers that are already divided by their scale.
+// Codes of four numbers that are already divided by their scale.  Integers: beside
+// 1.5 * 2^23 a number is rounded to one, whose low byte is the sum's.
 template <typename C>
 __device__ __forceinline__ uint32_t encode4(const float (&x)[4]) {
   if constexpr (std::is_same<C, code_i8>::value) {
-    uint32_t u = 0;
+    uint32_t y[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u |= (static_cast<uint32_t>(static_cast<int>(rintf(x[i]))) & 255u) << 8 * i;
-    return u;
+    for (int i = 0; i < 4; ++i) y[i] = __float_as_uint(x[i] + 12582912.f);
+    const uint32_t lo = __builtin_amdgcn_perm(y[1], y[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(y[3], y[2], 0x04000c0c);
+    return lo | hi;
   } else {
     int u = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
     return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], u, true));
@@ -140,6 +142,32 @@ __device__ __forceinline__ void decode4(uint32_t u, float scale, float (&x)[4]) 
   }
 }
 
+// Eight codes as bf16, which holds them exactly.
+template <typename C>
+__device__ __forceinline__ bf16x8 code_numbers(uint32_t a, uint32_t b, float scale = 1.f) {
+  union {
+    uint32_t u[4];
+    bf16x8 x;
+  } r;
+  const uint32_t w[2] = {a, b};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (std::is_same<C, code_e4m3>::value) {
+      // the instruction takes the scale's exponent, and gives NaN for a NaN
+      r.u[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false));
+      r.u[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true));
+    } else {
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = static_cast<float>(static_cast<signed char>(w[i] >> 8 * e)) * scale;
+      // their upper halves: the lower ones are zero
+      r.u[2 * i] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302);
+      r.u[2 * i + 1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302);
+    }
+  }
+  return r.x;
+}
+
 // One number of a row.
 template <typename S>
 __device__ __forceinline__ float number(const S* p, float scale) {
@@ -150,6 +178,54 @@ __device__ __forceinline__ float number(const S* p, float scale) {
   } else {
     return load_f32<S>(p);
   }
+}
+
+// The largest x of G lanes (a power of two of them side by side), in all of them.
+template <int G>
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+  auto other = [&](auto ctrl) {
+    return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  // lanes 1 and 2 on within four, mirrored within 8 and 16, rows and halves swapped
+  if constexpr (G > 1) x = max(x, other(std::integral_constant<int, 0xb1>{}));
+  if constexpr (G > 2) x = max(x, other(std::integral_constant<int, 0x4e>{}));
+  if constexpr (G > 4) x = max(x, other(std::integral_constant<int, 0x141>{}));
+  if constexpr (G > 8) x = max(x, other(std::integral_constant<int, 0x140>{}));
+  if constexpr (G > 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+  }
+  if constexpr (G > 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+  }
+  return x;
+}
+
+// Codes of a lane's share of a row: G lanes' numbers x (of which lanes past the
+// row's end have zeros).  Returns the bf16 of the row's scale.  x is used up.
+template <typename C, int G, int N>
+__device__ __forceinline__ uint32_t encode_row(float (&x)[N], uint32_t (&u)[N / 4]) {
+  uint32_t top = 0;  // bits of the largest magnitude: an infinity's or NaN's are the largest
+#pragma unroll
+  for (int k = 0; k < N; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+  top = group_max<G>(top);
+  const bool odd = top >= 0x7f800000u;
+  if (__builtin_expect(top > 0x7f000000u, 0)) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = odd ? 0.f : fminf(fmaxf(x[k], -0x1p127f), 0x1p127f);
+    top = 0x7f000000u;
+  }
+  const int ex = scale_exponent<C>(__uint_as_float(top));
+  const float inv = power_of_two(-ex);
+#pragma unroll
+  for (int k = 0; k < N / 4; ++k) {
+    float y[4];
+#pragma unroll
+    for (int z = 0; z < 4; ++z) y[z] = x[4 * k + z] * inv;
+    u[k] = encode4<C>(y);
+  }
+  return odd ? 0x7fc0u : __float_as_uint(power_of_two(ex)) >> 16;
 }
 
 __device__ __forceinline__ float key_scale(uint32_t pair) { return __uint_as_float(pair << 16); }

@@ -313,32 +313,6 @@ __device__ __forceinline__ bool careful_row(const AttnView& a, int b, int h, con
 // Codes in LDS
 // ---------------------------------------------------------------------------
 
-// Eight codes as bf16, which holds them exactly.
-template <typename C>
-__device__ __forceinline__ bf16x8 code_numbers(uint32_t a, uint32_t b, float scale = 1.f) {
-  union {
-    uint32_t u[4];
-    bf16x8 x;
-  } r;
-  const uint32_t w[2] = {a, b};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if constexpr (std::is_same<C, code_e4m3>::value) {
-      // the instruction takes the scale's exponent, and gives NaN for a NaN
-      r.u[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false));
-      r.u[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true));
-    } else {
-      float f[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[e] = static_cast<float>(static_cast<signed char>(w[i] >> 8 * e)) * scale;
-      // their upper halves: the lower ones are zero
-      r.u[2 * i] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302);
-      r.u[2 * i + 1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302);
-    }
-  }
-  return r.x;
-}
-
 // Rows of codes as they come, for what turns them into a Tile<bf16_t, DP>.
 template <int DP>
 struct CodeRows {
