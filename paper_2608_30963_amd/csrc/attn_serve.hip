@@ -136,7 +136,7 @@ hipError_t launch_append8(const kvx_attn* at, const Append8Args& g, int total_he
   const int d = at->model.head_dim, lanes = d <= 64 ? 4 : d <= 128 ? 8 : 16;
   const int64_t groups = (int64_t(g.a.rows) * lanes + 255) / 256;
   int split = 1;
-  while (split < total_heads && groups * split < 4 * at->n_cu) ++split;
+  while (split < total_heads && groups * split < 2 * at->n_cu) ++split;
   const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>(split));
   return lanes == 4   ? launch_on(append8_kernel<C, 4>, grid, dim3(256), st, g, split)
          : lanes == 8 ? launch_on(append8_kernel<C, 8>, grid, dim3(256), st, g, split)
