@@ -169,9 +169,9 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
   const int lane = threadIdx.x % 64, n = lane % 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 
-  int h, b = -1, qt = 0, split, strip, pieces = fp.splits, first, step;
+  ChunkShare sh;
   if constexpr (kView) {
-    const ChunkShare sh = chunk_share<TK>(a, fp.splits > 1);
+    sh = chunk_share<TK>(a, fp.splits > 1);
     if (fp.splits > 1 && blockIdx.x == 0) {
       // strips that the caller's bounds allow for and that are not there
       const int none = fp.strips - sh.strips;
@@ -179,27 +179,17 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
         fp.heads[i / none * fp.strips + sh.strips + i % none].pieces = 0;
     }
     if (__builtin_amdgcn_readfirstlane(sh.b) < 0) return;
-    h = __builtin_amdgcn_readfirstlane(sh.h);
-    b = __builtin_amdgcn_readfirstlane(sh.b);
-    qt = __builtin_amdgcn_readfirstlane(sh.qt);
-    strip = __builtin_amdgcn_readfirstlane(sh.strip);
-    split = __builtin_amdgcn_readfirstlane(sh.piece);
-    pieces = __builtin_amdgcn_readfirstlane(sh.pieces);
-    first = __builtin_amdgcn_readfirstlane(sh.first);
-    step = __builtin_amdgcn_readfirstlane(sh.step);
   } else {
     // (head, piece, strip): consecutive units of an XCD share a head's cache;
     // later strips, which see more, first
     int id = xcd_remap(blockIdx.x, gridDim.x);
-    h = id / (fp.strips * fp.splits);
-    id -= h * fp.strips * fp.splits;
-    split = id / fp.strips;
-    strip = fp.strips - 1 - id % fp.strips;
-    first = (h * fp.strips + strip) * fp.splits;
-    step = 1;
+    sh.h = id / (fp.strips * fp.splits);
+    id -= sh.h * fp.strips * fp.splits;
+    sh.piece = id / fp.strips;
+    sh.strip = fp.strips - 1 - id % fp.strips;
 
     // the strip's context: 64 contexts a step
-    int before = 0;
+    int b = -1, before = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
       int cnt = 0;
       if (b0 + lane < a.batch) {
@@ -212,22 +202,27 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
         const int y = __shfl_up(sum, i);
         if (lane >= i) sum += y;
       }
-      const uint64_t past = __ballot(before + sum > strip);
+      const uint64_t past = __ballot(before + sum > sh.strip);
       if (past) {
         const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
         b = b0 + f;
-        qt = strip - before - (__shfl(sum, f) - __shfl(cnt, f));
+        sh.qt = sh.strip - before - (__shfl(sum, f) - __shfl(cnt, f));
         break;
       }
       before += __shfl(sum, 63);
     }
     if (b < 0) {
-      if (fp.splits > 1 && split == 0 && threadIdx.x == 0) fp.heads[h * fp.strips + strip].pieces = 0;
+      if (fp.splits > 1 && sh.piece == 0 && threadIdx.x == 0) fp.heads[sh.h * fp.strips + sh.strip].pieces = 0;
       return;
     }
-    b = __builtin_amdgcn_readfirstlane(b);
-    qt = __builtin_amdgcn_readfirstlane(qt);
+    sh.b = b;
   }
+  const int h = __builtin_amdgcn_readfirstlane(sh.h), b = __builtin_amdgcn_readfirstlane(sh.b);
+  const int qt = __builtin_amdgcn_readfirstlane(sh.qt), strip = __builtin_amdgcn_readfirstlane(sh.strip);
+  const int split = __builtin_amdgcn_readfirstlane(sh.piece);
+  const int pieces = kView ? __builtin_amdgcn_readfirstlane(sh.pieces) : fp.splits;
+  const int first = kView ? __builtin_amdgcn_readfirstlane(sh.first) : (h * fp.strips + strip) * fp.splits;
+  const int step = kView ? __builtin_amdgcn_readfirstlane(sh.step) : 1;
   JoinHead* head = fp.heads + h * fp.strips + strip;
   const Context c = context(a, b);
   const int r0 = qt * kChunkRows, valid = min(kChunkRows, c.m * a.group - r0);
