@@ -82,6 +82,24 @@ VIEWS = [
     ("tree_i8_256", "bf16", "i8", 8, 4, 256, 16, [(20, 300)], dict(tree=1, cap=30.0, window=100, sink=4)),
     ("tree_no_depth", "bf16", "", 8, 2, 128, 16, [(40, 500)], dict(tree=1, depth=False)),
     ("tree_before_first", "bf16", "", 4, 2, 64, 16, [(20, 12), (5, 0)], dict(tree=3)),
+    # more contexts than a wave has lanes, pieces of chunks by their lengths
+    ("tree_many", "bf16", "i8", 4, 1, 64, 16, [(9 + i % 30, 50 + 37 * i % 400) for i in range(90)],
+     dict(tree=1)),
+    ("chunk_many", "bf16", "", 4, 1, 64, 16, [(9 + i % 30, 50 + 37 * i % 400) for i in range(90)],
+     dict(window=40, sink=5)),
+    ("chunk_uneven", "bf16", "e4m3", 8, 2, 128, 16, [(20, 3000), (20, 40), (0, 5), (20, 700)], {}),
+    ("one_of_many", "bf16", "i8", 8, 2, 128, 64, [(1, 20000)] + [(1, 3)] * 5, {}),
+    # contiguous caches whose last 16 slots are not all there, at an edge of the window
+    ("contiguous_37", "bf16", "i8", 8, 2, 128, 0, [(1, 37), (1, 20)], dict(window=9, sink=2)),
+    ("contiguous_101", "bf16", "", 8, 2, 128, 0, [(1, 101), (1, 5), (1, 97)], dict(window=30, sink=3)),
+    ("contiguous_chunk_77", "bf16", "e4m3", 8, 2, 128, 0, [(20, 77), (12, 61)], dict(window=30, sink=3)),
+    ("group_16", "bf16", "i8", 16, 1, 128, 16, [(1, 700)], {}),
+    ("group_17", "bf16", "i8", 17, 1, 128, 16, [(1, 700)], dict(window=300, sink=9)),
+    ("group_17_e4m3", "bf16", "e4m3", 17, 1, 256, 16, [(1, 333)], dict(cap=20.0)),
+    ("group_32", "bf16", "", 32, 1, 128, 16, [(1, 700)], dict(window=300, sink=9)),
+    ("cap_large", "bf16", "i8", 4, 2, 128, 16, [(1, 200), (1, 40)], dict(cap=1000.0)),
+    ("cap_large_chunk", "bf16", "e4m3", 4, 2, 128, 16, [(40, 200)], dict(cap=1000.0)),
+    ("few_nodes_window", "bf16", "e4m3", 4, 2, 128, 16, [(8, 300), (3, 9)], dict(tree=2, window=20, sink=4)),
 ]
 
 
@@ -925,3 +943,109 @@ def test_offsets_past_32_bits():
         T.cuda.synchronize()
         check_rows("", "bf16", d, 0.0, _f64(q), _f64(out), _f64(lse), rows[0], rows[1], V.sight(m, n))
     att.close()
+
+
+def test_rows_of_no_context_stay():
+    """Rows behind the last context's, and outputs of other contexts, are left as they were."""
+    T = U.torch()
+    for m in (1, 40):
+        cache = Cache8([50, 70], 2, 64, "i8", 16)
+        att = _attention("bf16", 2, 64, 4)
+        rows = 2 * m + 5
+        q = _rows(rows, 4, 64, "bf16", 1)
+        out, lse = T.full_like(q, 7.0), T.full((rows, 4), 7.0, device="cuda")
+        att.forward(kvx.make_attn_io(cache.struct, _int([50, 70]), q, out=out, lse=lse, layer=1, max_new=m,
+                                     q_start=_int([0, m, 2 * m])), att.workspace())
+        T.cuda.synchronize()
+        assert (out[2 * m:] == 7.0).all() and (lse[2 * m:] == 7.0).all()
+        assert not (out[:2 * m] == 7.0).all(-1).any()
+        att.close()
+
+
+def test_more_new_tokens_than_said():
+    """max_new chooses the kernel: too small a one changes no more than roundings."""
+    T = U.torch()
+    for m, said in ((40, 1), (9, 1), (40, 5)):
+        cache, q, starts, tokens, kw, sights = _problem("bf16", "i8", 8, 2, 128, 16, [(m, 300), (3, 90)],
+                                                        dict(window=100, sink=4))
+        kw["max_new"] = said
+        att = _attention("bf16", 2, 128, 8)
+        out, lse = T.zeros_like(q), T.zeros(starts[-1], 8, device="cuda")
+        att.forward(kvx.make_attn_io(cache.struct, tokens, q, out=out, lse=lse, **kw), att.workspace())
+        T.cuda.synchronize()
+        for b in range(2):
+            sl = slice(starts[b], starts[b + 1])
+            check_rows(f"{m} {said}", "bf16", 128, 0.0, _f64(q)[sl], _f64(out)[sl], _f64(lse)[sl],
+                       cache.f64(0, 1, b), cache.f64(1, 1, b), sights[b])
+        att.close()
+
+
+def test_masks_and_depths_may_be_anything():
+    """Bits of nodes that are not there, and depths outside of the tree, are no reads out
+    of range: bits past the last node see nothing, depths count as the nearest that may be."""
+    T = U.torch()
+    n, m = 90, 20
+    cache, q, starts, tokens, kw, sights = _problem("bf16", "", 8, 2, 64, 16, [(m, n)], dict(tree=1))
+    att = _attention("bf16", 2, 64, 8)
+    ws, outs = att.workspace(), []
+    for spoil in (0, -(1 << 20), 1 << 30):
+        if spoil:
+            kw["tree"] |= -(1 << m)  # bits 20..31
+            kw["depth"][:] = spoil
+        out, lse = T.zeros_like(q), T.zeros(m, 8, device="cuda")
+        att.forward(kvx.make_attn_io(cache.struct, tokens, q, out=out, lse=lse, **kw), ws)
+        T.cuda.synchronize()
+        outs.append((out, lse))
+    for o, l in outs[1:]:  # without a window, depths change nothing
+        assert T.equal(o, outs[0][0]) and T.equal(l, outs[0][1])
+    att.close()
+
+
+def test_garbage_behind_the_tokens():
+    """Slots past a context's tokens in the blocks that its last ones share: NaN, as a
+    fresh allocation may hold, at every length around a block's end."""
+    T = U.torch()
+    for code, d in (("", 128), ("", 256), ("i8", 128), ("e4m3", 128)):
+        for page in (16, 48, 0):
+            lens = [1, 15, 16, 17, 31, 32, 33, 47, 48, 49, 100]
+            cache = Cache8(lens, 2, d, code, page, extra=20) if code else \
+                Cache(lens, 2, d, "bf16", page, extra=20)
+            q = _rows(len(lens), 8, d, "bf16", 1)
+            att = _attention("bf16", 2, d, 8)
+            out, lse = T.zeros_like(q), T.zeros(len(lens), 8, device="cuda")
+            att.forward(kvx.make_attn_io(cache.struct, _int(lens), q, out=out, lse=lse, layer=1, window=20,
+                                         sink=3), att.workspace())
+            T.cuda.synchronize()
+            for b, n in enumerate(lens):
+                sl = slice(b, b + 1)
+                check_rows(f"{code} {page} {n}", "bf16", d, 0.0, _f64(q)[sl], _f64(out)[sl], _f64(lse)[sl],
+                           cache.f64(0, 1, b), cache.f64(1, 1, b), V.sight(1, n, 20, 3))
+            att.close()
+
+
+def test_two_streams_at_once():
+    """Two handles' calls on two streams, each with its workspace, give the bits that they
+    give one after the other."""
+    T = U.torch()
+    sides = []
+    for i in range(2):
+        cache, q, starts, tokens, kw, _ = _problem("bf16", "i8", 28, 4, 128, 16,
+                                                   [(1, 700 + 50 * i), (1, 90), (1, 3000)], dict(window=600, sink=4),
+                                                   seed=i)
+        att = _attention("bf16", 4, 128, 28)
+        out = T.zeros_like(q)
+        io = kvx.make_attn_io(cache.struct, tokens, q, out=out, **kw)
+        sides.append((cache, att, att.workspace(), out, io, T.cuda.Stream()))
+    T.cuda.synchronize()
+    alone = []
+    for _, att, ws, out, io, _ in sides:
+        att.forward(io, ws)
+        T.cuda.synchronize()
+        alone.append(out.clone())
+    for _ in range(20):
+        for _, att, ws, out, io, stream in sides:
+            att.forward(io, ws, stream)
+    T.cuda.synchronize()
+    for a, side in zip(alone, sides):
+        assert T.equal(a, side[3])
+        side[1].close()

@@ -1,0 +1,123 @@
+"""Calls of serving (kvx_serve.h) that are refused with a handle, before anything is run."""
+import ctypes as C
+
+import pytest
+
+from paper_2608_30963_amd import kvx
+from tests import gpu_util as U
+from tests.serve_util import Cache8
+from tests.test_attn_gpu import Cache, _int, _rows
+
+pytestmark = pytest.mark.gpu
+
+E, S, N = kvx.KVX_EINVAL, kvx.KVX_ESHAPE, kvx.KVX_EUNSUPPORTED
+
+
+def _refused(status, call):
+    with pytest.raises(kvx.KvxError) as e:
+        call()
+    assert e.value.status == status
+
+
+def test_statuses():
+    T = U.torch()
+    att = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_BF16)
+    wide = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_F32)
+    ws = att.workspace()
+    coded, plain = Cache8([40, 20], 2, 64, "i8", 16), Cache([40, 20], 2, 64, "bf16", 16)
+    f32 = Cache([40, 20], 2, 64, "f32", 16)
+    tokens, start = _int([40, 20]), _int([0, 3, 5])
+    q, k, v = (_rows(5, h, 64, "bf16", h) for h in (4, 2, 2))
+    out = T.zeros_like(q)
+    mask = T.zeros((5, 1), dtype=T.int32, device="cuda")
+
+    def io(cache=coded.struct, **kw):
+        base = dict(q_start=start, max_new=3, new_q=q, new_k=k, new_v=v, out=out)
+        base.update(kw)
+        return kvx.make_attn_io(cache, tokens, q, **base)
+
+    # 8 bits are the bf16 models'
+    _refused(N, lambda: kvx.kvx_attn_append_coded(wide.handle, io(), coded.struct))
+    one = io()
+    _refused(N, lambda: kvx.kvx_attn_forward_view(wide.handle, one, one.view, ws))
+    # views that say something else
+    _refused(E, lambda: att.forward(io(tree=mask, prefix=_int([1, 1])), ws))
+    _refused(S, lambda: att.forward(io(tree=mask, max_new=33), ws))
+    _refused(E, lambda: att.forward(io(plain.struct, sink=-1, window=4), ws))
+    _refused(E, lambda: att.forward(io(plain.struct, sink=-1), ws))
+    _refused(S, lambda: att.forward(io(), ws[:1024]))
+    _refused(E, lambda: att.forward(io(out=None), ws))
+    _refused(E, lambda: att.forward(io(layer=2), ws))
+    with pytest.raises(ValueError):
+        att.mass(io(lse=T.zeros(5, 4, device="cuda"), mass=T.zeros(2, 2, 64, device="cuda")))
+    # caches
+    for field, value, status in (("code", 2, E), ("scale", None, E), ("scale", coded.struct.scale + 2, N),
+                                 ("scale_stride", (C.c_int64 * 4)(1, -1, 1, 1), S),
+                                 ("scale_stride", (C.c_int64 * 4)(64, 32, 16, 0), S)):
+        held = getattr(coded.struct, field)
+        held = (C.c_int64 * 4)(*held) if field == "scale_stride" else held
+        setattr(coded.struct, field, value)
+        pack = kvx.make_pack_io(plain.struct, coded.struct, tokens)
+        acc = kvx.make_accept_io(coded.struct, tokens, _int([0, 1]).view(2, 1), _int([1, 1]), q_start=start)
+        for call in (lambda: att.append(io()), lambda: att.forward(io(), ws), lambda: att.pack(pack),
+                     lambda: att.unpack(pack), lambda: att.accept(acc)):
+            _refused(status, call)
+        setattr(coded.struct, field, held)
+    pack = kvx.make_pack_io(plain.struct, coded.struct, tokens)
+    att.pack(pack)
+    pack.cache.k = coded.struct.codes.v
+    _refused(E, lambda: att.pack(pack))
+    with pytest.raises(ValueError):  # another dtype than the model's
+        att.pack(kvx.make_pack_io(f32.struct, coded.struct, tokens))
+    wide.pack(kvx.make_pack_io(f32.struct, coded.struct, tokens))
+    # trees
+    parent = _int([-1, 0, 1, -1, 0])
+
+    def tree(**kw):
+        base = dict(q_start=start)
+        base.update(kw)
+        return kvx.make_tree_io(tokens, parent, base.pop("mask", mask), **base)
+
+    att.tree(tree())
+    _refused(N, lambda: att.tree(tree(mask=T.zeros((5, 65), dtype=T.int32, device="cuda"))))
+    _refused(E, lambda: att.tree(tree(window=-1)))
+    _refused(E, lambda: att.tree(tree(sink=-1)))
+    _refused(S, lambda: att.tree(tree(q_start=None)))
+    three = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_BF16, pair_axis=[0, 1, 2, 2] * 8)
+    with pytest.raises(ValueError):
+        three.tree(tree(pos=T.zeros((2, 5), dtype=T.int32, device="cuda")))
+    # paths
+    path, count = _int([0, 1, 0, 1]).view(2, 2), _int([1, 1])
+    _refused(E, lambda: att.accept(kvx.make_accept_io(plain.struct, tokens, path, count, q_start=start,
+                                                      tokens_out=tokens)))
+    acc = kvx.make_accept_io(plain.struct, tokens, path, count, q_start=start)
+    acc.max_path = 0
+    _refused(E, lambda: att.accept(acc))
+    deep = kvx.Attention(kvx.ModelShape(3, 2, 64, 1e4), 4, kvx.KVX_BF16)
+    with pytest.raises(ValueError):  # the cache has two layers
+        deep.accept(kvx.make_accept_io(plain.struct, tokens, path, count, q_start=start))
+    with pytest.raises(ValueError):
+        deep.pack(kvx.make_pack_io(plain.struct, coded.struct, tokens))
+    T.cuda.synchronize()
+    for a in (att, wide, three, deep):
+        a.close()
+
+
+def test_nothing_to_do():
+    """No contexts, or no rows: nothing is run, whatever else is given."""
+    att = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_BF16)
+    T = U.torch()
+    ws = att.workspace()
+    io, view, c8 = kvx.AttnIO(), kvx.AttnView(), kvx.Cache8()
+    view.sink, io.window = 3, 5
+    view.cache8 = C.addressof(c8)
+    kvx.kvx_attn_forward_view(att.handle, io, view, ws)
+    io.new_q = ws.data_ptr()
+    kvx.kvx_attn_append_coded(att.handle, io, c8)
+    kvx.kvx_attn_pack(att.handle, kvx.PackIO())
+    tree, acc = kvx.TreeIO(), kvx.AcceptIO()
+    tree.words = acc.max_path = 1
+    kvx.kvx_attn_tree(att.handle, tree)
+    kvx.kvx_attn_accept(att.handle, acc)
+    T.cuda.synchronize()
+    att.close()
