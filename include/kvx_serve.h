@@ -2,7 +2,7 @@
  * kvx_serve.h -- serving on a translated cache that is held in 8 bits, bounded
  * by a window with sinks, and decoded by drafted trees (gfx950 / MI355X).
  *
- *   kvx_attn_append_coded       new keys (rotated) and values into a cache of 8 bits
+ *   kvx_attn_append_coded  new keys (rotated) and values into a cache of 8 bits
  *   kvx_attn_pack          a cache into one of 8 bits, all layers
  *   kvx_attn_unpack        a cache of 8 bits into one of the model's dtype
  *   kvx_attn_tree          what the tokens of drafted trees see, by their parents
@@ -45,8 +45,8 @@ typedef struct {
 /* kvx_attn_append into a cache of 8 bits (io's own cache is ignored): keys are
  * rotated in 64 bits and rounded once, to their codes.  bf16 models only
  * (KVX_EUNSUPPORTED). */
-kvx_status kvx_attn_append_coded(const kvx_attn* attn, const kvx_attn_io* io, const kvx_cache8* cache8,
-                            void* stream);
+kvx_status kvx_attn_append_coded(const kvx_attn* attn, const kvx_attn_io* io,
+                                 const kvx_cache8* cache8, void* stream);
 
 /* One conversion of the first tokens[b] slots of every context, all layers. */
 typedef struct {
@@ -101,8 +101,7 @@ typedef struct {
 
 /* kvx_attn_forward under a view; NULL, or an empty one, is kvx_attn_forward
  * itself.  Numbers of 8 bits enter products exactly; a value's scale is applied
- * before the weight's rounding to bf16 or exactly after it.  Calls whose
- * workgroups would pass 2^32 threads are refused (KVX_EUNSUPPORTED). */
+ * before the weight's rounding to bf16 or exactly after it. */
 kvx_status kvx_attn_forward_view(const kvx_attn* attn, const kvx_attn_io* io,
                                  const kvx_attn_view* view, void* workspace,
                                  size_t workspace_bytes, void* stream);

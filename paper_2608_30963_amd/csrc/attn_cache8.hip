@@ -25,7 +25,10 @@ struct Codes {
 // Slots' key and value rows to codes, or back: G lanes a slot, 16 bytes of plain
 // numbers each, so that a wave reads and writes whole lines; lanes past head_dim
 // stay idle.  A workgroup's turn is kChunk slots of a head, a wave's 16 of them,
-// whose rows are all asked for before the first is worked on.  Bound by memory.
+// whose rows are all asked for before the first is worked on.  Bound by memory:
+// 28 layers of 4k slots, 2 heads x 128, bf16 to int8: 176 MB in 41.5 us, 4.2 TB/s; 26
+// layers, 4 contexts of up to 2k slots, 4 heads x 256, e4m3 to bf16: 887 MB in 201 us,
+// 4.4 TB/s (by 8 bytes of codes a lane and one row at a time: 289).
 // Where 16 slots from a multiple of 16 on lie in one block of both caches, a
 // wave's rows have one base; else every lane finds its own.
 template <typename T, typename C, int G, bool PACK>

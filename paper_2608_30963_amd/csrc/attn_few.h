@@ -6,7 +6,11 @@
 // fit a compute unit.  Lane (n, g) = (lane % 16, lane / 16) holds query n's
 // scores of slots 16 u + 4 g + v (register v of block u), which are the weights'
 // operand as they stand if the contraction over 32 slots takes them in that
-// order, and columns 16 db + 4 g + v of its sum.
+// order, and columns 16 db + 4 g + v of its sum.  Bound by memory: codes become
+// bf16 operands in registers, once a number.  Measured, kernel alone: 64 contexts of
+// up to 8k slots in int8, heads 28 / 4 x 128, 307 MB in 71 us, 4.3 TB/s (the ring of 32
+// rows: 139); one of 128k 37; 16 of up to 8k slots in bf16 through a window of 1024 with
+// sinks, heads 8 / 4 x 256, 67 MB in 19 us (61), of which start and end are 8.
 #pragma once
 
 #include "attn_forward.h"

@@ -101,13 +101,18 @@ hipError_t launch_view(const kvx_attn* at, const AttnView& a, int code, int max_
   const int64_t seen = most_seen(a, max_new);
   p.decode = int64_t(max_new) * at->group <= kDecodeRows || !launchable(units, 256);
   if (p.decode) {
+    // up to 16 query rows of 16 bits or fewer: half of the matrix work and twice the
+    // waves of the ring of 32 rows (attn_few.h has both's times); fp32
+    // stays with the ring
     p.grid = at->n_cu;
     p.few = int64_t(max_new) * at->group <= 16 && at->dtype == KVX_BF16;
     if (p.few) p.grid = at->n_cu * few_groups(padded_dim(at->model.head_dim), code < 0 ? 2 : 1);
     p.splits = seen <= 512 ? 1 : 0;
     p.join_rows = static_cast<int>(std::min(int64_t(max_new) * at->group, int64_t(kDecodeRows)));
   } else {
-    // with fewer strips than the card takes workgroups at a time they are cut
+    // with fewer strips than the card takes workgroups at a time they are cut, by
+    // every context's length: equal pieces of all strips took 120 us where these take 75
+    // (trees of 64 nodes, 8 contexts of 800 to 8k slots, heads 28 / 4 x 128)
     const int64_t slots = std::min(int64_t(at->n_cu) * resident(at), most_pieces(at));
     p.join_rows = kChunkRows;
     p.splits = units < slots ? 2 : 1;

@@ -46,8 +46,8 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const Q& q, int h,
 // sum.  Bound by the matrix units, and where heads are 256 wide by the LDS as
 // much: each of 4 waves reads all of a tile's keys and values for 32 rows, about
 // a thousand clocks, as its matrix work takes, and one wave a SIMD has to
-// overlap the two.  Measured: 4096 tokens after 12k, heads 64 / 8 x 128: 1.88 ms,
-// 1.02 PFLOP/s, where the card's power sets the clock (with zeros a fifth less
+// overlap the two.  Measured: 4096 tokens after 12k, heads 64 / 8 x 128: 1.85 ms,
+// 1.04 PFLOP/s, where the card's power sets the clock (with zeros a fifth less
 // time); 1531 tokens in 5627 slots, window 4096, heads 8 / 4 x 256, capped: 116 us,
 // 445 TFLOP/s; fp32, 3 contexts of up to 257 in 1024 slots, heads 12 / 2 x 128:
 // 56 us, 46 TFLOP/s of 154: a tile's scores, weights and products follow each
@@ -60,6 +60,16 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const Q& q, int h,
 // fills a compute unit, so that no other one hides the copies' latency, and
 // LDS has room.  The scores of tile t + 1 are formed beside the weights of tile t,
 // which need other units of the compute unit.
+//
+// Caches of 8 bits: codes are copied as they are, one tile ahead, and each wave
+// turns a quarter of a tile into the rows of bf16 that the loops read, so that a
+// number is converted once a workgroup.  Under a view a piece's start is found by
+// every context's length (chunk_share).  Measured: 1021 tokens in 8192 slots of e4m3,
+// heads 64 / 8 x 128: 314 us, 810 TFLOP/s (of bf16 330); trees of 64 nodes, 8 contexts
+// of up to 8k slots in int8, heads 28 / 4 x 128: 75 us (of bf16 64), 1.3 us a tile in
+// bf16 and some 17 that do not depend on the tiles (start, first copies, masked
+// tiles, 63 KB of instructions to fetch, the pieces' 64 KB); fp32, 3 contexts of up to 257 in
+// 2900 slots, window 500 with sinks, heads 12 / 2 x 128: 45 us.
 // ---------------------------------------------------------------------------
 
 template <typename T, int DP>
@@ -891,7 +901,9 @@ __global__ void __launch_bounds__((64 * Decode<S, DP>::kWaves), 1)
 // .., whose sums are then added in the waves' order.  Four for single tokens,
 // whose few rows have many pieces; one for chunks.  Bound by latency for single
 // tokens (28 rows of 64 pieces: 10 us) and by the pieces' reading for chunks (96
-// strips of 5 pieces x 256 columns, 63 MB: 15.5 us).
+// strips of 5 pieces x 256 columns, 63 MB: 15.5 us; trees of 64 nodes, heads 28 x 128,
+// 8 contexts in 256 pieces, 17 MB: 11.5, most of it the wait for what a row's pieces
+// and its context are).
 template <typename T, int DP, int W, typename A>
 __global__ void __launch_bounds__(256) forward_join(A a, ForwardPlan fp) {
   constexpr int PER = DP / 64;
@@ -959,7 +971,7 @@ __global__ void __launch_bounds__(256) forward_join(A a, ForwardPlan fp) {
 // Joins the pieces of units of few query rows.  SPREAD: units of hundreds of
 // pieces (few long contexts), a workgroup of 16 waves a row, which ask for all at
 // once and whose sums are added in the waves' order: 28 rows of 128 pieces 7.4
-// us, by 4 waves 15.8.  Otherwise a wave a row.
+// us, by 4 waves 15.8.  Otherwise a wave a row: 448 units of 7 rows 5.9 us.
 template <typename T, int DP, bool SPREAD>
 __global__ void __launch_bounds__(SPREAD ? 1024 : 256) few_join(AttnView a, ForwardPlan fp) {
   constexpr int PER = DP / 64, W = SPREAD ? 16 : 1;

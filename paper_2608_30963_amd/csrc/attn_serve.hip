@@ -45,7 +45,10 @@ struct Append8Args {
 // As append_kernel, with G lanes a row of which those past head_dim stay idle:
 // a row's largest magnitude is taken over them.  Keys are rotated in 64 bits, so
 // that their codes are those of the exact angles: an error in fp32 would move
-// numbers near the middle of two codes by a whole step.
+// numbers near the middle of two codes by a whole step.  Bound by memory and, where
+// tokens are many, the sines of 64 bits: 4 prompts, 11k tokens, heads 28 / 4 x 128, 92 MB
+// in 23.8 us, 3.9 TB/s (with the library's sine and cosine and a workgroup for all heads
+// of its rows: 32); one token 6 us, a launch and three loads that wait for each other.
 template <typename C, int G>
 __global__ void __launch_bounds__(256) append8_kernel(Append8Args g, int heads_step) {
   const AttnArgs& a = g.a;
