@@ -65,7 +65,9 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const Q& q, int h,
 // turns a quarter of a tile into the rows of bf16 that the loops read, so that a
 // number is converted once a workgroup.  Under a view a piece's start is found by
 // every context's length (chunk_share).  Measured: 1021 tokens in 8192 slots of e4m3,
-// heads 64 / 8 x 128: 314 us, 810 TFLOP/s (of bf16 330); trees of 64 nodes, 8 contexts
+// heads 64 / 8 x 128: 314 us, 810 TFLOP/s; called without a pause, which lowers the
+// clock, 375, of bf16 306: the conversion has no matrix work beside it but the other
+// workgroup's (38% of clocks are matrix work, in bf16 56%).  Trees of 64 nodes, 8 contexts
 // of up to 8k slots in int8, heads 28 / 4 x 128: 75 us (of bf16 64), 1.3 us a tile in
 // bf16 and some 17 that do not depend on the tiles (start, first copies, masked
 // tiles, 63 KB of instructions to fetch, the pieces' 64 KB); fp32, 3 contexts of up to 257 in
