@@ -119,7 +119,8 @@ typedef struct {
   const int32_t* count;      /* device [batch], taken into 0..min(m, max_path) */
   kvx_cache cache;           /* ignored with cache8 */
   const kvx_cache8* cache8;  /* or NULL */
-  int32_t* tokens_out;       /* device [batch] n - m + count, or NULL; not tokens itself */
+  int32_t* tokens_out;       /* device [batch] n - m + count, or NULL; not memory of
+                                tokens, count, path or q_start (KVX_EINVAL) */
 } kvx_accept_io;
 
 /* No two contexts may share a block of their new tokens. */

@@ -174,6 +174,12 @@ kvx_status prepare_cache8(const kvx_attn* at, const kvx_cache8* in, int32_t batc
   return KVX_OK;
 }
 
+// Whether n numbers at a and m at b share memory.
+bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + 4 * static_cast<uintptr_t>(m) && y < x + 4 * static_cast<uintptr_t>(n);
+}
+
 // KVX_VALIDATE=1: block ids of slots [from[b], to[b]) of every context.
 kvx_status validate_blocks(const kvx_cache& c, int32_t batch, const int64_t* from, const int64_t* to) {
   if (!c.block_table) return KVX_OK;
@@ -372,7 +378,13 @@ kvx_status kvx_attn_accept(const kvx_attn* at, const kvx_accept_io* io, void* st
   if (!at || !io) return KVX_EINVAL;
   if (io->batch < 0 || io->max_path < 1) return KVX_EINVAL;
   if (io->batch == 0) return KVX_OK;
-  if (!io->tokens || !io->path || !io->count || io->tokens_out == io->tokens) return KVX_EINVAL;
+  if (!io->tokens || !io->path || !io->count) return KVX_EINVAL;
+  // written while other workgroups still read these
+  if (overlap(io->tokens_out, io->batch, io->tokens, io->batch) ||
+      overlap(io->tokens_out, io->batch, io->count, io->batch) ||
+      overlap(io->tokens_out, io->batch, io->path, int64_t(io->batch) * io->max_path) ||
+      overlap(io->tokens_out, io->batch, io->q_start, io->batch + int64_t(1)))
+    return KVX_EINVAL;
   AcceptArgs a{};
   kvx_status s = io->cache8 ? prepare_cache8(at, io->cache8, io->batch, 0, a.c, a.scale)
                             : prepare_cache(at, io->cache, elem_size(at), io->batch, 0, a.c);

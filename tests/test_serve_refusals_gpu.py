@@ -90,6 +90,12 @@ def test_statuses():
     path, count = _int([0, 1, 0, 1]).view(2, 2), _int([1, 1])
     _refused(E, lambda: att.accept(kvx.make_accept_io(plain.struct, tokens, path, count, q_start=start,
                                                       tokens_out=tokens)))
+    both = _int([40, 20, 40])
+    for other in (dict(tokens=both[:2], tokens_out=both[1:]), dict(count=count, tokens_out=count),
+                  dict(path=both[:2].view(2, 1), tokens_out=both[1:]), dict(q_start=start, tokens_out=start[1:])):
+        given = dict(tokens=tokens, path=path, count=count, q_start=start)
+        given.update(other)
+        _refused(E, lambda: att.accept(kvx.make_accept_io(plain.struct, **given)))
     acc = kvx.make_accept_io(plain.struct, tokens, path, count, q_start=start)
     acc.max_path = 0
     _refused(E, lambda: att.accept(acc))
