@@ -374,14 +374,23 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
       copy_tile<L, TK, 4, false, true>(a.c, kb, vb, b, line.slot(t), range, vblocks, a.d, w, 0,
                                        l3 + (kKeys + slot) * kBytes);
   };
-  // the wave's codes become rows of keys (or values) at `to`
-  auto convert = [&](bool keys, char* to) __attribute__((always_inline)) {
+  // The wave's codes of tile t become rows of keys (or values) at `to`.  Runs bring
+  // slots that the unit does not see: as values they are zeros, so that what a fresh
+  // cache holds there is not taken for numbers to be careful of (1021 tokens in 8181
+  // slots of e4m3, heads 64 / 8 x 128, NaN behind them: 114 ms); as keys they are masked.
+  auto convert = [&](bool keys, int t, char* to) __attribute__((always_inline)) {
     if constexpr (kCoded) {
+      const int j0 = line.slot(t);
+      const bool edge = !keys && !range.inside(j0, TK);
 #pragma unroll
       for (int i = 0; i < kCodeCopies; ++i) {
-        const uint4 x = *reinterpret_cast<const uint4*>(lds + kCodesAt + (keys ? 0 : kCodes) + (i * 4 + w) * 1024 + lane * 16);
-        const float f = keys ? key_scale(kpair[i]) : value_scale(vpair[i]);
+        uint4 x = *reinterpret_cast<const uint4*>(lds + kCodesAt + (keys ? 0 : kCodes) + (i * 4 + w) * 1024 + lane * 16);
+        float f = keys ? key_scale(kpair[i]) : value_scale(vpair[i]);
         const int row = i * kCodeStep + w * R::kRowsPerCopy + lane / R::kChunks, chunk = 2 * (lane % R::kChunks);
+        if (edge && range.misses(j0 + row, 1)) {
+          x = uint4{0, 0, 0, 0};
+          f = 1.f;
+        }
         const int swz = keys ? L::key_swz(row) : L::value_swz(row);
         *reinterpret_cast<bf16x8*>(to + row * L::kRowBytes + (chunk ^ swz) * 16) = code_numbers<S>(x.x, x.y, f);
         *reinterpret_cast<bf16x8*>(to + row * L::kRowBytes + ((chunk + 1) ^ swz) * 16) = code_numbers<S>(x.z, x.w, f);
@@ -398,7 +407,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
     copy_keys(t0, 0);
     if constexpr (kCoded) {
       __builtin_amdgcn_s_waitcnt(0);
-      convert(true, lds);
+      convert(true, t0, lds);
     }
 #pragma unroll
     for (int i = 0; i < kDepth; ++i) {
@@ -434,8 +443,8 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
       // entered a loop with it, or are at an edge; not by those that went on in
       // the middle one.
       if (kKeys == 2 && !(t - 1 > steady0 && t - 1 < steady1)) tile_barrier();
-      if (t + 1 < t1) convert(true, lds + after(kslot, kKeys, 1) * kBytes);
-      convert(false, lds + (kKeys + vslot) * kBytes);
+      if (t + 1 < t1) convert(true, t + 1, lds + after(kslot, kKeys, 1) * kBytes);
+      convert(false, t, lds + (kKeys + vslot) * kBytes);
       if (t + 1 < t1) copy_values(t + 1, 0);
       if (t + 2 < t1) copy_keys(t + 2, 0);
       tile_barrier();
