@@ -11,6 +11,8 @@
 // up to 8k slots in int8, heads 28 / 4 x 128, 307 MB in 71 us, 4.3 TB/s (the ring of 32
 // rows: 139); one of 128k 37; 16 of up to 8k slots in bf16 through a window of 1024 with
 // sinks, heads 8 / 4 x 256, 67 MB in 19 us (61), of which start and end are 8.
+// With the join: 64 contexts of up to 8k slots, heads 8 / 4 x 256, int8 143 us, e4m3 139,
+// 4.6 TB/s (174 where registers of e4m3 were kept in scratch memory).
 #pragma once
 
 #include "attn_forward.h"
@@ -34,6 +36,15 @@ __device__ __forceinline__ float query_sum(float x) {
   float a, b;
   both_rows(x, a, b);
   return half_sum(a + b);
+}
+
+// The lane, formed anew: the compiler does not take what derives from it out of a
+// loop, where that would fill registers, be kept in scratch memory and be read back,
+// for which it waits, and so for every copy in flight.
+__device__ __forceinline__ int fresh_lane() {
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(lane));
+  return lane;
 }
 
 // A tile of 32 slots in LDS, rows of DP numbers of S.  16-byte chunk c of row r
@@ -151,7 +162,7 @@ struct FewTile {
   static __device__ __forceinline__ int odd_values(const char* v, uint32_t rows) {
     if constexpr (std::is_same<S, code_i8>::value) return 0;
     const uint32_t ones = kCoded ? 0x7f7f7f7fu : 0x7f807f80u, more = kCoded ? 0x01010101u : 0x00800080u;
-    const int lane = threadIdx.x % 64;
+    const int lane = fresh_lane();
     uint32_t any = 0, seen = 0;
 #pragma unroll
     for (int i = 0; i < 32 * kChunks / 64; ++i) {
@@ -163,6 +174,25 @@ struct FewTile {
     }
     const uint32_t top = kCoded ? 0x80808080u : 0x80008000u;
     return (__any(any & top) ? 1 : 0) | (__any(seen & top) ? 2 : 0);
+  }
+
+  // Values that are not finite become zero, in place: products of their own for
+  // them would keep a second set of sums.
+  static __device__ __forceinline__ void clear_odd_values(char* v) {
+    const uint32_t ones = kCoded ? 0x7f7f7f7fu : 0x7f807f80u, more = kCoded ? 0x01010101u : 0x00800080u;
+    const uint32_t top = kCoded ? 0x80808080u : 0x80008000u;
+    const int lane = threadIdx.x % 64;
+    auto clear = [&](uint32_t w) {
+      const uint32_t m = ((w & ones) + more) & top;
+      return w & ~(kCoded ? (m >> 7) * 0xffu : (m >> 15) * 0xffffu);
+    };
+#pragma unroll 1
+    for (int i = 0; i < 32 * kChunks / 64; ++i) {
+      uint4* const at = reinterpret_cast<uint4*>(v + (i * 64 + lane) * 16);
+      const uint4 x = *at;
+      *at = uint4{clear(x.x), clear(x.y), clear(x.z), clear(x.w)};
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 };
 
@@ -179,7 +209,7 @@ template <typename L, bool KEYS>
 __device__ __forceinline__ void few_copy(const CacheArgs& c, const char* from, int b, bool runs, const int (&first)[2],
                                          const int (&id)[2], int j0, const ViewReach& range, int d, uint32_t to) {
   constexpr int R = L::kRowsPerCopy, kHalf = L::kCopies / 2;  // copies of 16 rows
-  const int lane = threadIdx.x % 64, sub = lane / L::kChunks, bytes = d * L::kElem;
+  const int lane = fresh_lane(), sub = lane / L::kChunks, bytes = d * L::kElem;
   auto swz = [](int r) { return KEYS ? L::key_swz(r) : L::value_swz(r); };
   const int chunk = (lane % L::kChunks ^ swz(sub)) * 16;
   const uint32_t st = static_cast<uint32_t>(c.st) * L::kElem;
@@ -357,7 +387,7 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroup
       const int ahead = t + NST;
       // all has been asked for up to tile t + NST - 1
       const bool more = ahead - 1 < tiles, next = ahead < tiles;
-      const char* const stage = ring + (t + NST) % NST * F::kStage;
+      char* const stage = ring + (t + NST) % NST * F::kStage;
       const int j0 = slot_of(max(t, 0));
       f32x4 sc[2] = {};
       uint32_t pair[2][4] = {}, bits = ~0u;
@@ -473,34 +503,23 @@ __global__ void __launch_bounds__((64 * Few<S, DP>::kWaves), (Few<S, DP>::kGroup
           vm_wait<(NST - 1) * (kKeys + kValues)>();
         else
           vm_wait<0>();
-        const char* const v = stage + L::kBytes;
-        // values that the unit does not see count as zero; if it sees any that is not
-        // finite, rows are computed again
-        int strange = 0;
-        if (edge)
-          strange = L::odd_values(v, low_bits(range.hi - j0) & (~low_bits(range.lo - j0) | low_bits(range.sink - j0)));
-        odd |= strange > 1;
-        if (__builtin_expect(strange, 0)) {
+        char* const v = stage + L::kBytes;
+        // values that are not finite count as zero; if the unit sees any, rows are
+        // computed again
+        if (edge) {
+          const int strange = L::odd_values(v, reach_bits(range, j0));
+          odd |= strange > 1;
+          if (__builtin_expect(strange, 0)) L::clear_odd_values(v);
+        }
+        constexpr int kAhead = NB < 8 ? NB : 8;
+        typename L::Raw raw[kAhead];
 #pragma unroll
-          for (int db = 0; db < NB; ++db) {
-            bf16x8 x = L::value_numbers(L::value_raw(v, at, db));
+        for (int i = 0; i < kAhead; ++i) raw[i] = L::value_raw(v, at, i);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (!finite(static_cast<float>(x[e]))) x[e] = static_cast<__bf16>(0.f);
-            acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p, acc[db], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        } else {
-          constexpr int kAhead = NB < 8 ? NB : 8;
-          typename L::Raw raw[kAhead];
-#pragma unroll
-          for (int i = 0; i < kAhead; ++i) raw[i] = L::value_raw(v, at, i);
-#pragma unroll
-          for (int db = 0; db < NB; ++db) {
-            const bf16x8 x = L::value_numbers(raw[db % kAhead]);
-            if (db + kAhead < NB) raw[db % kAhead] = L::value_raw(v, at, db + kAhead);
-            acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p, acc[db], 0, 0, 0);
-          }
+        for (int db = 0; db < NB; ++db) {
+          const bf16x8 x = L::value_numbers(raw[db % kAhead]);
+          if (db + kAhead < NB) raw[db % kAhead] = L::value_raw(v, at, db + kAhead);
+          acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p, acc[db], 0, 0, 0);
         }
       }
       __builtin_amdgcn_sched_barrier(0);

@@ -71,6 +71,11 @@ __device__ __forceinline__ ViewReach reach(const AttnView& a, const Context& c, 
   return r;
 }
 
+// Which of the slots j0 .. j0 + 31 the unit sees, slot j0 + i in bit i.
+__device__ __forceinline__ uint32_t reach_bits(const ViewReach& r, int j0) {
+  return low_bits(r.hi - j0) & (~low_bits(r.lo - j0) | low_bits(r.sink - j0));
+}
+
 // The 16 slots that are copied for slots j .. j + 15: themselves where the unit
 // sees any of them, else those around the nearest that it does.
 __device__ __forceinline__ int sixteen(const ViewReach& r, int j) {
