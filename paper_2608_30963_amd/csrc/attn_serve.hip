@@ -32,6 +32,17 @@ __device__ __forceinline__ void turn64(double r, double& c, double& s) {
   c = (k + 1) & 2 ? -v : v;
 }
 
+// x in fp32, with an odd last bit where that is not x itself: what is rounded to
+// fewer bits after, or compared with a number of fewer, comes out as from x.  (The
+// nearest one would take x to the middle of two codes, or to the largest code.)
+__device__ __forceinline__ float to_odd(double x) {
+  const float near = static_cast<float>(x);
+  const double back = near;
+  uint32_t u = __float_as_uint(near);
+  u -= fabs(back) > fabs(x) ? 1 : 0;
+  return __uint_as_float(back == x ? u : u | 1u);
+}
+
 struct Append8Args {
   AttnArgs a;  // c: the codes
   ScaleArgs scale;
@@ -47,7 +58,7 @@ struct Append8Args {
 // that their codes are those of the exact angles: an error in fp32 would move
 // numbers near the middle of two codes by a whole step.  Bound by memory and, where
 // tokens are many, the sines of 64 bits: 4 prompts, 11k tokens, heads 28 / 4 x 128, 92 MB
-// in 23.8 us, 3.9 TB/s (with the library's sine and cosine and a workgroup for all heads
+// in 24.2 us, 3.8 TB/s (with the library's sine and cosine and a workgroup for all heads
 // of its rows: 32); one token 6 us, a launch and three loads that wait for each other.
 template <typename C, int G>
 __global__ void __launch_bounds__(256) append8_kernel(Append8Args g, int heads_step) {
@@ -113,8 +124,8 @@ __global__ void __launch_bounds__(256) append8_kernel(Append8Args g, int heads_s
         y[i] = u;
         y[8 + i] = w;
         if (which == 1) {
-          y[i] = static_cast<float>(u * cs[i] - w * sn[i]);
-          y[8 + i] = static_cast<float>(w * cs[i] + u * sn[i]);
+          y[i] = to_odd(u * cs[i] - w * sn[i]);
+          y[8 + i] = to_odd(w * cs[i] + u * sn[i]);
         }
       }
       uint32_t u[4];

@@ -2,6 +2,8 @@
 import numpy as np
 import pytest
 
+from oracle import attn as R
+from oracle import serve as V
 from paper_2608_30963_amd import kvx
 from tests import gpu_util as U
 from tests.serve_util import Cache8
@@ -91,3 +93,68 @@ def test_hidden_values_of_single_tokens(code, d):
             else:
                 assert (outs[0][i] == outs[1][i]).all(), (window, i)
         att.close()
+
+
+# (position, first, second of pair 0): turned, the first is past 127 (448) times a power of
+# two by less than half a step of fp32, and the row's largest number
+BORDERS = {"i8": [(359, 189.0, -508.0), (593, 186.0, 173.0), (870, 212.0, 215.0), (1076, 222.0, 253.0),
+                  (1126, 179.0, -478.0), (1525, 160.0, -222.0)],
+           "e4m3": [(204, 186.0, 207.0), (1783, 167.0, -251.0), (2110, 194.0, 404.0)]}
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_keys_are_rounded_once(code):
+    """Codes and scales of turned keys are those of the 64-bit numbers, also where fp32
+    rounds one to the middle of two codes, or a row's largest to the largest code of a
+    smaller scale.  (Sine and cosine are off by 2^-36, so that numbers as near to a border
+    may differ; none of these is.)"""
+    T = U.torch()
+    n, d = 40000, 64
+    x = T.randn(n, 1, d, generator=T.Generator().manual_seed(26)).bfloat16()
+    pos = np.random.default_rng(27).integers(0, 5000, (1, n)).astype(np.int32)
+    for i, (p, u, w) in enumerate(BORDERS[code]):
+        x[i] = 0.0
+        x[i, 0, 0], x[i, 0, d // 2], pos[0, i] = u, w, p
+    ref = R.rotate(x.double().numpy(), pos, 1e4 ** (-2.0 * np.arange(d // 2) / d), [0] * (d // 2))
+    want, scales = V.encode(ref, code)
+    twice, other = V.encode(ref.astype(np.float32), code)
+    assert (twice != want).any() and (other != scales).any()  # what is tested is there
+    for b, s in enumerate(other != scales):
+        assert s.any() == (b < len(BORDERS[code]))
+    cache = Cache8([n], 1, d, code, 0, layers=1)
+    att = kvx.Attention(kvx.ModelShape(1, 1, d, 1e4), 1, kvx.KVX_BF16)
+    x = x.cuda()
+    att.append(kvx.make_attn_io(cache.struct, _int([n]), None, new_k=x, new_v=x, q_start=_int([0, n]),
+                                max_new=n, pos=T.from_numpy(pos).cuda()))
+    T.cuda.synchronize()
+    c, s = cache.read(0, 0, 0, np.arange(n))
+    assert (s == scales).all(), np.argwhere(s != scales)[:9]
+    assert (c == want).all(), np.argwhere(c != want)[:9]
+    att.close()
+
+
+def test_keys_past_the_largest_number_of_fp32():
+    """A turned number that fp32 does not hold counts as 2^127, as any past it."""
+    T = U.torch()
+    d, top = 64, 3.3e38
+    x = T.zeros(2, 1, d, dtype=T.bfloat16)
+    x[0, 0, 0], x[0, 0, d // 2] = top, -top  # by 45 degrees: past fp32, and near zero
+    x[0, 0, 1] = 1e38
+    x[1, 0, 0] = float("inf")
+    inv = np.zeros(d // 2)
+    inv[0] = np.pi / 4
+    cache = Cache8([2], 1, d, "i8", 0, layers=1)
+    att = kvx.Attention(kvx.ModelShape(1, 1, d, 1e4), 1, kvx.KVX_BF16, inv_freq=inv)
+    x = x.cuda()
+    att.append(kvx.make_attn_io(cache.struct, _int([2]), None, new_k=x, new_v=x, q_start=_int([0, 2]),
+                                max_new=2, pos=_int([1, 1]).view(1, 2)))
+    T.cuda.synchronize()
+    c, s = cache.read(0, 0, 0, np.arange(2))
+    ref = x.double().cpu().numpy()
+    turned = ref.copy()
+    turned[0, 0, 0] = (ref[0, 0, 0] - ref[0, 0, d // 2]) * np.cos(np.pi / 4)
+    turned[0, 0, d // 2] = (ref[0, 0, 0] + ref[0, 0, d // 2]) * np.cos(np.pi / 4)
+    want, scales = V.encode(turned, "i8")
+    assert s[0, 0] == scales[0, 0] == 2.0 ** 121 and np.isnan(s[1, 0])
+    assert (c[0] == want[0]).all() and (c[1] == 0).all()
+    att.close()
