@@ -1080,8 +1080,9 @@ class Attention:
     def mass(self, io, stream=None):
         if getattr(io, "fits", None) is not self:
             self._fits(io)
-        if io.view is not None:
-            raise ValueError("weights are not formed under a view: 8 bits, sinks or a tree")
+        view = io.view
+        if view is not None and (view.cache8 or view.tree or (view.sink and io.window) or view.sink < 0):
+            raise ValueError("weights are not formed under a view: 8 bits, sinks of a window or a tree")
         kvx_attn_mass(self.handle, io, stream)
 
     def evict(self, io, stream=None):

@@ -7,7 +7,7 @@ from oracle import serve as V
 from paper_2608_30963_amd import kvx
 from tests import gpu_util as U
 from tests.serve_util import Cache8
-from tests.test_attn_gpu import _int, _rows
+from tests.test_attn_gpu import Cache, _int, _rows
 from tests.test_serve_gpu import _problem
 
 pytestmark = pytest.mark.gpu
@@ -157,4 +157,27 @@ def test_keys_past_the_largest_number_of_fp32():
     want, scales = V.encode(turned, "i8")
     assert s[0, 0] == scales[0, 0] == 2.0 ** 121 and np.isnan(s[1, 0])
     assert (c[0] == want[0]).all() and (c[1] == 0).all()
+    att.close()
+
+
+def test_weights_with_sinks_and_no_window():
+    """Sinks mean something to a window only: without one, weights are formed as without
+    them; with one they are refused."""
+    T = U.torch()
+    cache, tokens = Cache([90, 40], 2, 64, "bf16", 16), _int([90, 40])
+    q = _rows(2, 4, 64, "bf16", 1)
+    att = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_BF16)
+    ws, got = att.workspace(), []
+    for sink in (0, 4):
+        out, lse = T.zeros_like(q), T.zeros(2, 4, device="cuda")
+        mass = T.zeros(2, 2, 96, device="cuda")
+        io = kvx.make_attn_io(cache.struct, tokens, q, out=out, lse=lse, mass=mass, layer=1, sink=sink)
+        att.forward(io, ws)
+        att.mass(io)
+        T.cuda.synchronize()
+        got.append((out, lse, mass))
+    assert all(T.equal(a, b) for a, b in zip(*got)) and got[0][2].sum() > 0
+    for kw in (dict(sink=4, window=9), dict(sink=-1), dict(tree=T.zeros((2, 1), dtype=T.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            att.mass(kvx.make_attn_io(cache.struct, tokens, q, lse=lse, mass=mass, **kw))
     att.close()
