@@ -154,6 +154,8 @@ def main(argv=None):
     p.add_argument("--window", type=int, default=0, help="positions that a token sees, 0: all")
     p.add_argument("--sink", type=int, default=4, help="first positions that stay visible")
     a = p.parse_args(argv)
+    if a.steps < 1 or a.nodes < 1:
+        p.error("at least one tree of one node is wanted")
     shape, k, v, table, lengths = handoff(a.config, a.tokens, a.batch, a.steps * 8 + a.nodes + BLOCK)
     heads, cap = HEADS[a.config]
     d = Drafter(shape, heads, cap, k, v, table, lengths, a.nodes, window=a.window, sink=a.sink)
