@@ -26,7 +26,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from examples.decode import BLOCK, HEADS, Layers, handoff  # noqa: E402
+from examples.decode import HEADS, Layers, handoff  # noqa: E402
 from paper_2608_30963_amd import kvx  # noqa: E402
 
 VOCABULARY = 32
@@ -35,6 +35,14 @@ VOCABULARY = 32
 def tree_of(nodes, width):
     """Parents of a tree of `nodes` whose nodes have up to `width` children."""
     return [-1] + [(i - 1) // width for i in range(1, nodes)]
+
+
+def deepest_of(up):
+    """Nodes of the path to the last node, the longest in trees of tree_of."""
+    node, nodes = len(up) - 1, 1
+    while up[node] >= 0:
+        node, nodes = up[node], nodes + 1
+    return nodes
 
 
 class Drafter:
@@ -63,10 +71,7 @@ class Drafter:
         up = tree_of(nodes, width)
         self.parent = torch.tensor(up * self.batch, dtype=torch.int32, device="cuda")
         self.up = torch.tensor(up, device="cuda")
-        self.deepest = 1  # nodes of the longest path
-        while up[nodes - 1] >= 0 and nodes > 1:
-            nodes = up[nodes - 1] + 1
-            self.deepest += 1
+        self.deepest = deepest_of(up)
         starts = torch.arange(0, rows + 1, self.nodes, dtype=torch.int32, device="cuda")
         self.mask, self.depth, self.pos = ints(rows, -(-self.nodes // 32)), ints(rows), ints(1, rows)
         self.path, self.count, self.left = ints(self.batch, self.deepest), ints(self.batch), ints(self.batch)
@@ -156,7 +161,8 @@ def main(argv=None):
     a = p.parse_args(argv)
     if a.steps < 1 or a.nodes < 1:
         p.error("at least one tree of one node is wanted")
-    shape, k, v, table, lengths = handoff(a.config, a.tokens, a.batch, a.steps * 8 + a.nodes + BLOCK)
+    room = a.steps * deepest_of(tree_of(a.nodes, 2)) + a.nodes  # if whole paths are accepted
+    shape, k, v, table, lengths = handoff(a.config, a.tokens, a.batch, room)
     heads, cap = HEADS[a.config]
     d = Drafter(shape, heads, cap, k, v, table, lengths, a.nodes, window=a.window, sink=a.sink)
     g = torch.Generator("cuda").manual_seed(1)
