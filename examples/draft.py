@@ -54,6 +54,7 @@ class Drafter:
         self.att = kvx.Attention(shape, n_heads, kvx.KVX_BF16, softcap=softcap)
         self.batch, self.nodes, self.room = len(lengths), nodes, table.shape[1] * k.shape[3]
         self.tokens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+        self.most = max(lengths)  # tokens of the longest context, at most: known without the device
         self.k, self.v = torch.zeros_like(k, dtype=code), torch.zeros_like(v, dtype=code)
         self.scale = torch.zeros(k.shape[:-1] + (2,), dtype=torch.bfloat16, device="cuda")
         self.cache = kvx.make_cache8(self.k, self.v, self.scale, table)
@@ -128,8 +129,11 @@ class Drafter:
     def step(self, drafted, eager=False):
         """Reads the trees `drafted` [batch][nodes] of tokens; the accepted nodes and the
         token that the target chooses after them (both valid until the next step)."""
-        if int(self.tokens.max()) + self.nodes > self.room:
-            raise ValueError(f"a tree of {self.nodes} does not fit {self.room} slots")
+        if self.most + self.nodes > self.room:
+            self.most = int(self.tokens.max())
+            if self.most + self.nodes > self.room:
+                raise ValueError(f"a tree of {self.nodes} does not fit {self.room} slots")
+        self.most += self.deepest
         self.drafted.copy_(drafted)
         if eager:
             self._step()
@@ -167,19 +171,19 @@ def main(argv=None):
     d = Drafter(shape, heads, cap, k, v, table, lengths, a.nodes, window=a.window, sink=a.sink)
     g = torch.Generator("cuda").manual_seed(1)
     root = torch.zeros(a.batch, dtype=torch.int64, device="cuda")
-    total, began = 0, None
+    total, began = torch.zeros((), dtype=torch.int64, device="cuda"), None
     for i in range(a.steps):
         drafted = torch.randint(0, VOCABULARY, (a.batch, a.nodes), device="cuda", generator=g)
         drafted[:, 0] = root
         count, last = d.step(drafted)
         root = last.clone()
-        total += int(count.sum())
+        total += count.sum()
         if i == 0:
             torch.cuda.synchronize()
             began = time.perf_counter()
     torch.cuda.synchronize()
     spent = (time.perf_counter() - began) / max(1, a.steps - 1)
-    print(f"{lengths} translated tokens, {a.steps} trees of {a.nodes}: {total} tokens accepted, "
+    print(f"{lengths} translated tokens, {a.steps} trees of {a.nodes}: {int(total)} tokens accepted, "
           f"{d.tokens.tolist()} cached, {spent * 1e3:.3f} ms a tree and batch")
     d.close()
 
