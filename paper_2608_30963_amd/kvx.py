@@ -1021,7 +1021,7 @@ class Attention:
         if getattr(io, "view", None) is not None:
             given += [t for t in io.view.tensors if hasattr(t, "data_ptr")]
         for c in caches:
-            k = getattr(c, "tensors", (None,))[0]
+            k, _, table = getattr(c, "tensors", (None,) * 3)
             if not hasattr(k, "data_ptr"):
                 continue
             given.append(k)
@@ -1033,11 +1033,17 @@ class Attention:
             if not any(c.stride) and (k.dim() != 5 or (k.shape[2], k.shape[4]) != (heads, d)):
                 raise ValueError(f"the cache has shape {tuple(k.shape)}, the model {heads} KV "
                                  f"heads of {d}")
-            if isinstance(io, (PackIO, AcceptIO)) and not any(c.stride) and \
-                    (int(k.shape[0]) < int(m.n_layers) or
+            layers = int(m.n_layers)
+            if isinstance(io, AttnIO):  # a layer that the model lacks is the library's to refuse
+                layers = min(io.layer + 1, layers)
+            if not any(c.stride) and \
+                    (int(k.shape[0]) < layers or
                      (c.block_table is None and int(k.shape[1]) < io.batch)):
-                raise ValueError(f"the cache has shape {tuple(k.shape)}, the model {m.n_layers} "
-                                 f"layers, the call {io.batch} contexts")
+                raise ValueError(f"the cache has shape {tuple(k.shape)}, the call {layers} layers "
+                                 f"and {io.batch} contexts")
+            if hasattr(table, "shape") and int(table.shape[0]) < io.batch:
+                raise ValueError(f"the block table has shape {tuple(table.shape)}, the call "
+                                 f"{io.batch} contexts")
         if not all(t.is_cuda for t in given):
             raise ValueError("tensors must be on a GPU")
         if isinstance(io, EvictIO):
