@@ -321,9 +321,7 @@ __device__ __forceinline__ bool careful_row(const AttnView& a, int b, int h, con
 // Rows of codes as they come, for what turns them into a Tile<bf16_t, DP>.
 template <int DP>
 struct CodeRows {
-  static constexpr int kElem = 1, kChunks = DP / 16, kRowBytes = DP, kRowsPerCopy = 64 / kChunks;
-  static __device__ __forceinline__ constexpr int key_swz(int) { return 0; }
-  static __device__ __forceinline__ constexpr int value_swz(int) { return 0; }
+  static constexpr int kChunks = DP / 16, kRowsPerCopy = 64 / kChunks;
 };
 
 // Rows of codes that operands are read from (as Tile).  A lane reads 16 codes of
