@@ -7,8 +7,8 @@ from oracle import serve as V
 from paper_2608_30963_amd import kvx
 from tests import gpu_util as U
 from tests.serve_util import Cache8
-from tests.test_attn_gpu import Cache, _int, _rows
-from tests.test_serve_gpu import _problem
+from tests.test_attn_gpu import Cache, _f64, _int, _rows
+from tests.test_serve_gpu import _problem, check_rows
 
 pytestmark = pytest.mark.gpu
 
@@ -181,3 +181,63 @@ def test_weights_with_sinks_and_no_window():
         with pytest.raises(ValueError):
             att.mass(kvx.make_attn_io(cache.struct, tokens, q, lse=lse, mass=mass, **kw))
     att.close()
+
+
+@pytest.mark.parametrize("sink", [4, 16])
+def test_sinks_reach_their_blocks_only(sink, monkeypatch):
+    """Output and log-sum-exp where the blocks between sinks and window are none."""
+    T = U.torch()
+    cache, q = Cache([200], 2, 64, "bf16", 16), _rows(1, 4, 64, "bf16", 1)
+    att = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_BF16)
+    monkeypatch.setenv("KVX_VALIDATE", "1")
+    cache.table[0, 1:5] = 10 ** 6  # not read through
+    out, lse = T.zeros_like(q), T.full((1, 4), float("nan"), device="cuda")
+    att.forward(kvx.make_attn_io(cache.struct, _int([200]), q, out=out, lse=lse, layer=1, window=100, sink=sink),
+                att.workspace())
+    T.cuda.synchronize()
+    check_rows(f"{sink}", "bf16", 64, 0.0, _f64(q), _f64(out), _f64(lse), cache.f64(0, 1, 0),
+               cache.f64(1, 1, 0), V.sight(1, 200, 100, sink))
+    att.close()
+
+
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_appends_past_the_capacity_change_nothing(code, page):
+    """Neither codes nor scales, of any block, layer or head."""
+    T = U.torch()
+    n, m = 96, 9
+    for grown in (m, 60, 10 ** 6):
+        cache = Cache8([n, 40], 2, 64, code, page)
+        held = [t.clone() for t in cache.base]
+        att = kvx.Attention(kvx.ModelShape(2, 2, 64, 1e4), 4, kvx.KVX_BF16)
+        x = [_rows(m, 2, 64, "bf16", 5 + i) for i in range(2)]
+        att.append(kvx.make_attn_io(cache.struct, _int([n + grown, 40]), None, layer=1, max_new=m,
+                                    q_start=_int([0, m, m]), new_k=x[0], new_v=x[1]))
+        T.cuda.synchronize()
+        for t, o in zip(cache.base, held):
+            bits = T.int16 if t.dtype == T.bfloat16 else T.uint8
+            assert T.equal(t.view(bits), o.view(bits)), grown
+        att.close()
+
+
+def test_packing_what_was_unpacked():
+    """int8: the same codes and scales.  e4m3: the same numbers, of which a row's largest may
+    come under half the scale."""
+    T = U.torch()
+    for code in ("i8", "e4m3"):
+        first, again = (Cache8([900], 2, 128, code, 16, layers=1, seed=s) for s in (0, 1))
+        plain, back = (Cache([900], 2, 128, "bf16", 16, layers=1) for _ in range(2))
+        att = kvx.Attention(kvx.ModelShape(1, 2, 128, 1e4), 4, kvx.KVX_BF16)
+        tokens, other = _int([900]), 0
+        att.unpack(kvx.make_pack_io(plain.struct, first.struct, tokens))
+        att.pack(kvx.make_pack_io(plain.struct, again.struct, tokens))
+        att.unpack(kvx.make_pack_io(back.struct, again.struct, tokens))
+        T.cuda.synchronize()
+        for kv in range(2):
+            assert T.equal(plain.read(kv, 0, 0, 900), back.read(kv, 0, 0, 900))
+            a, b = (c.read(kv, 0, 0, np.arange(900)) for c in (first, again))
+            same = (a[1] == b[1])
+            assert (a[0][same] == b[0][same]).all() and (b[1][~same] * 2 == a[1][~same]).all()
+            other += (~same).sum()
+        assert (other > 0) == (code == "e4m3")
+        att.close()
