@@ -294,6 +294,15 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
     }
     return 0;
   };
+  // Runs of 16 slots bring some that the unit does not see, of which a fresh cache may
+  // hold anything: as keys they are masked, and as values no reason to compute rows
+  // again (1021 tokens in 8181 slots, heads 64 / 8 x 128, NaN behind them: 114 ms).  They
+  // become zeros on their way, by their scale where codes are always numbers, by both
+  // in e4m3; or, where that costs the loops registers and time, odd ones that the unit
+  // sees are looked for in the end.  Measured (us; neither, zeros, looked for), heads 64 /
+  // 8, int8, unless said otherwise: x 128 361, 357, 373; trees of 64 nodes 89, 89, 95; cap 50
+  // 515, 504, 514; cap 1000 577, 640, 602 (e4m3 536, 593, 540); x 64 244, 254, 245.
+  constexpr bool kZeros = DP > 64 && CAP != Cap::tanh;
   // where the last asked keys' rows begin, and so their values'
   int64_t code_at[kCodeCopies] = {};
   bool code_runs = false;
@@ -354,7 +363,13 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
           __builtin_amdgcn_s_waitcnt(0);
           if (code0 < a.d) copy16(at, to);
         }
-        if (!keys) vpair[i] = kpair[i];  // the same tile's, whose keys are here
+        if (!keys) {
+          vpair[i] = kpair[i];  // the same tile's, whose keys are here
+          if constexpr (kZeros && std::is_same<S, code_i8>::value)
+            if (!range.inside(line.slot(t), TK) &&
+                range.misses(line.slot(t) + i * kCodeStep + w * R::kRowsPerCopy + sub, 1))
+              vpair[i] = 0;
+        }
       }
     }
   };
@@ -374,10 +389,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
       copy_tile<L, TK, 4, false, true>(a.c, kb, vb, b, line.slot(t), range, vblocks, a.d, w, 0,
                                        l3 + (kKeys + slot) * kBytes);
   };
-  // The wave's codes of tile t become rows of keys (or values) at `to`.  Runs bring
-  // slots that the unit does not see: as values they are zeros, so that what a fresh
-  // cache holds there is not taken for numbers to be careful of (1021 tokens in 8181
-  // slots of e4m3, heads 64 / 8 x 128, NaN behind them: 114 ms); as keys they are masked.
+  // the wave's codes of tile t become rows of keys (or values) at `to`
   auto convert = [&](bool keys, int t, char* to) __attribute__((always_inline)) {
     if constexpr (kCoded) {
       const int j0 = line.slot(t);
@@ -387,10 +399,11 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
         uint4 x = *reinterpret_cast<const uint4*>(lds + kCodesAt + (keys ? 0 : kCodes) + (i * 4 + w) * 1024 + lane * 16);
         float f = keys ? key_scale(kpair[i]) : value_scale(vpair[i]);
         const int row = i * kCodeStep + w * R::kRowsPerCopy + lane / R::kChunks, chunk = 2 * (lane % R::kChunks);
-        if (edge && range.misses(j0 + row, 1)) {
-          x = uint4{0, 0, 0, 0};
-          f = 1.f;
-        }
+        if constexpr (kZeros && std::is_same<S, code_e4m3>::value)
+          if (edge && range.misses(j0 + row, 1)) {
+            x = uint4{0, 0, 0, 0};
+            f = 1.f;
+          }
         const int swz = keys ? L::key_swz(row) : L::value_swz(row);
         *reinterpret_cast<bf16x8*>(to + row * L::kRowBytes + (chunk ^ swz) * 16) = code_numbers<S>(x.x, x.y, f);
         *reinterpret_cast<bf16x8*>(to + row * L::kRowBytes + ((chunk + 1) ^ swz) * 16) = code_numbers<S>(x.z, x.w, f);
@@ -571,6 +584,15 @@ __global__ void __launch_bounds__(256, DP * sizeof(Numbers<S>) <= 256 ? 2 : 1)
     }
   }
   if (!odd) return;
+  if constexpr (kCoded && !kZeros) {
+    bool seen = false;
+#pragma unroll 1
+    for (int x = t0; x < t1 && !seen; ++x) {
+      if ((line.slot(x) >= mine.alo && x < tm) || mine.misses(line.slot(x), TK)) continue;  // not at an edge
+      seen = odd_codes<S>(a, b, h, range, line.slot(x), TK);
+    }
+    if (!seen) return;
+  }
   vm_wait<0>();  // the rows that change are written again
 #pragma unroll 1
   for (int r = 0; r < rows_w; ++r) {

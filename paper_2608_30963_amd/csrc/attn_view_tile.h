@@ -408,6 +408,28 @@ struct CodeTile {
   }
 };
 
+// Whether values of slots j0 .. j0 + n - 1 that the unit sees are no numbers (n is at
+// most a wave's lanes).
+template <typename C>
+__device__ __forceinline__ bool odd_codes(const AttnView& a, int b, int h, const ViewReach& range, int j0, int n) {
+  const int j = j0 + static_cast<int>(threadIdx.x % 64);
+  bool odd = false;
+  if (j < j0 + n && !range.misses(j, 1)) {
+    const int32_t block = cache_block(a.c, b, j);
+    odd = !finite(value_scale(a.scale.p[scale_offset(a.c, a.scale, block, j) + h * a.scale.sh]));
+    if constexpr (!std::is_same<C, code_i8>::value) {
+      const char* v = a.c.v + h * a.c.sh + cache_offset(a.c, block, j);
+#pragma unroll 1
+      for (int e = 0; e < a.d; e += 16) {
+        const uint4 x = *reinterpret_cast<const uint4*>(v + e);
+        const uint32_t low = 0x7f7f7f7fu, one = 0x01010101u;  // seven set bits pass into the eighth
+        odd |= ((((x.x & low) + one) | ((x.y & low) + one) | ((x.z & low) + one) | ((x.w & low) + one)) & 0x80808080u) != 0;
+      }
+    }
+  }
+  return __any(odd);
+}
+
 // The tile that single tokens' kernel reads.
 template <typename S, int DP>
 struct TileOf {

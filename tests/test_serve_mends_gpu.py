@@ -27,15 +27,16 @@ def _least_ms(call, turns=5):
     return min(times)
 
 
-@pytest.mark.parametrize("d,page", [(128, 16), (128, 0), (256, 16), (64, 48)])
+@pytest.mark.parametrize("d,page,cap", [(128, 16, 0.0), (128, 0, 0.0), (256, 16, 0.0), (64, 48, 0.0),
+                                        (128, 16, 1000.0), (256, 0, 500.0), (64, 16, 50.0), (96, 7, 50.0)])
 @pytest.mark.parametrize("code", ["i8", "e4m3"])
-def test_what_lies_behind_the_tokens_costs_nothing(code, d, page):
+def test_what_lies_behind_the_tokens_costs_nothing(code, d, page, cap):
     """Slots past a context's tokens that hold NaN scales and codes that are no numbers,
     or zeros: the same bits, and no row is computed a second time (which took two hundred
     times as long)."""
     T = U.torch()
     lens, m = [2003, 1029], 140
-    att = kvx.Attention(kvx.ModelShape(2, 2, d, 1e4), 8, kvx.KVX_BF16)
+    att = kvx.Attention(kvx.ModelShape(2, 2, d, 1e4), 8, kvx.KVX_BF16, softcap=cap)
     ws, outs, took = att.workspace(), [], []
     q = _rows(2 * m, 8, d, "bf16", 1)
     for garbage in (False, True):
@@ -240,4 +241,48 @@ def test_packing_what_was_unpacked():
             assert (a[0][same] == b[0][same]).all() and (b[1][~same] * 2 == a[1][~same]).all()
             other += (~same).sum()
         assert (other > 0) == (code == "e4m3")
+        att.close()
+
+
+@pytest.mark.parametrize("cap", [0.0, 50.0, 1000.0])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_hidden_values_of_chunks(code, d, cap):
+    """Values that are no numbers in what a chunk sees in part (its last tokens, through a
+    window), behind its tokens and before its window: rows that do not see them keep their
+    bits, rows that see one are NaN."""
+    T = U.torch()
+    m, n = 70, 333
+    for window, sink, bad, behind in ((0, 0, [n - 1], False), (0, 0, [n - 40], True), (90, 5, [190, n - 20], True),
+                                      (90, 5, [50, 100], False), (90, 5, [3], True), (0, 0, [], True)):
+        cache, q, starts, tokens, kw, sights = _problem("bf16", code, 4, 2, d, 16, [(m, n), (40, 50)],
+                                                        dict(window=window, sink=sink), extra=30)
+        att = kvx.Attention(kvx.ModelShape(2, 2, d, 1e4), 4, kvx.KVX_BF16, softcap=cap)
+        ws, outs = att.workspace(), []
+        blk, slot = cache.place(0, np.arange(n, n + 30))
+        held = [t[:, blk, :, slot].clone() for t in (*cache.dev, cache.dscale)]
+        for spoiled in (False, True):
+            if not spoiled or not behind:  # finite numbers behind
+                for t in cache.dev:
+                    t[:, blk, :, slot] = 0
+                cache.dscale[:, blk, :, slot] = 1.0
+            else:
+                for t, x in zip((*cache.dev, cache.dscale), held):
+                    t[:, blk, :, slot] = x
+            for i, j in enumerate(bad if spoiled else []):
+                at, s = (int(x[0]) for x in cache.place(0, [j]))
+                if code == "i8" or i % 2:
+                    cache.dscale[1, at, :, s, 1] = float("nan")
+                else:
+                    cache.dev[1][1, at, :, s] = 255
+            out = T.zeros_like(q)
+            att.forward(kvx.make_attn_io(cache.struct, tokens, q, out=out, **kw), ws)
+            T.cuda.synchronize()
+            outs.append(_f64(out))
+        assert np.isfinite(outs[0]).all() and (outs[0][m:] == outs[1][m:]).all()
+        for i in range(m):
+            if sights[0][i, bad].any():
+                assert np.isnan(outs[1][i]).all(), (window, i)
+            else:
+                assert (outs[0][i] == outs[1][i]).all(), (window, i)
         att.close()
