@@ -48,7 +48,8 @@ typedef struct {
 kvx_status kvx_attn_append_coded(const kvx_attn* attn, const kvx_attn_io* io,
                                  const kvx_cache8* cache8, void* stream);
 
-/* One conversion of the first tokens[b] slots of every context, all layers. */
+/* One conversion of the first tokens[b] slots of every context, all layers; of slots
+ * past either cache's capacity nothing is read or written. */
 typedef struct {
   int32_t batch;
   const int32_t* tokens;     /* device [batch] */
@@ -96,7 +97,8 @@ typedef struct {
                                 window and sink leave it, and of the new tokens those
                                 of its mask.  io's prefix has to be NULL */
   int32_t tree_words;        /* >= 1, 32 tree_words >= max_new */
-  const int32_t* depth;      /* device [rows], taken into 0..m - 1; NULL: i */
+  const int32_t* depth;      /* device [rows], taken into 0..m - 1; NULL: i; with a tree
+                                only */
 } kvx_attn_view;
 
 /* kvx_attn_forward under a view; NULL, or an empty one, is kvx_attn_forward
